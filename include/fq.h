@@ -434,6 +434,81 @@ int fq_prefill_forward(const fq_layer *layers, int L, const uint8_t *bitvec, con
                        void *k_cache, void *v_cache, int Tmax, const float *rope, void *workspace,
                        size_t workspace_bytes, void *stream);
 
+/*
+ * Serving several sequences out of one pool of cache pages (Section "Introduction": the memory that a hosted model may
+ * take varies while it serves; its key/value cache is the other part of it).  Real decoder blocks as above, with
+ *   - keys and values in pools [pages][n_kv_heads][page][128] fp16, `page` positions a page (16, 32, 64, 128 or 256);
+ *   - a ragged batch: of sequence b, seq_len[b] positions are in the pages table[b][0], table[b][1], ... and its last
+ *     q_start[b+1] - q_start[b] positions are tokens of this call (none, one, or a chunk of a prompt), rows q_start[b]...
+ *     of the call's arrays;
+ *   - n_heads query heads, n_kv_heads key/value heads (a divisor): query head h reads key/value head h / (n_heads / n_kv_heads).
+ * The arrays of the batch are device memory, so that a captured call can be replayed with other lengths; the host
+ * states bounds for them.  What the arrays say beyond those bounds is cut to them, and a page number outside the pool is
+ * taken for the nearest one inside: results are then wrong, but no access leaves the buffers.  Entries of the table behind
+ * a sequence's last page are not used.  max_q and max_len decide how a call is divided (and with the sizes what workspace
+ * it needs): state what the arrays hold, or what they will hold at most.
+ */
+typedef struct {
+    const int32_t *q_start; /* device [seqs + 1]: first token of every sequence; the last entry is tokens */
+    const int32_t *seq_len; /* device [seqs]: positions of every sequence, the tokens of the call included */
+    const int32_t *table;   /* device [seqs][table_stride]: pages of every sequence, in order */
+    int seqs;               /* 1..65535 */
+    int tokens;             /* rows of the call's arrays */
+    int max_q;              /* most tokens of one sequence */
+    int max_len;            /* most positions of one sequence, at most table_stride * page */
+    int table_stride;
+    int page;               /* positions of a page */
+    int pages;              /* pages of the pools */
+} fq_paged_batch;
+
+/*
+ * Norm of every query and key head, position rotation and the write into the pages, in one pass:
+ *   x = q[m][h]; x = x / sqrt(mean(x^2) + eps) * q_gain (if there is one); q_out[m][h] = rope(x, positions[m]);
+ * the same for k with k_gain, into place slots[m] % page of page slots[m] / page; v[m] is copied there as it is.
+ * fp32 in between, one rounding.  q, k, v fp16, device: row m at m * ldq (ldk, ldv) elements, multiples of 8 (columns of
+ * one product, for instance); q_gain, k_gain fp16 [128] or NULL; positions, slots int32 [tokens]; a slot outside the pools (-1)
+ * marks a token that is not cached; a position outside the table takes its nearest row.  q_out fp16 [tokens][n_heads * 128]
+ * (may be q if that is contiguous).  Two tokens of one slot leave either.
+ */
+int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, int tokens, int n_heads,
+                    int n_kv_heads, const int32_t *positions, const int32_t *slots, const float *rope, int rope_rows,
+                    const void *q_gain, const void *k_gain, float eps, void *q_out, void *k_pages, void *v_pages, int page,
+                    int pages, void *stream);
+
+/*
+ * Attention of the batch's tokens over their sequences' pages, which hold the tokens' own keys and values already: token
+ * i of the n of a sequence of S positions sees the positions t <= S - n + i, and per query head
+ *   out = sum_t p[t] V[t],  p = softmax_t(scale * q . K[t]);  lse = log sum_t exp(scale * q . K[t])  (NULL: not wanted).
+ * A row that sees nothing (n > S) is 0 with lse -inf.  q fp16, row m at m * ldq elements (a multiple of 8); out fp16
+ * [tokens][n_heads * 128]; lse fp32 [tokens][n_heads].
+ * With weights_out (fp32 [seqs][n_kv_heads][weights_stride], else NULL), what every position has received is added up:
+ *   weights_out[b][h][t] = (t < S - n ? weights[b][h][t] : 0) + sum of p[t] over the tokens and the query heads of h,
+ * t < S; weights may be weights_out, or NULL for zeros.  Sums are taken in a fixed order.
+ * workspace: device scratch of fq_attn_paged_workspace_bytes(batch, n_heads, n_kv_heads, weights_out != NULL) bytes
+ * (may be 0, and NULL then), 16-byte aligned, contents undefined afterwards.
+ */
+size_t fq_attn_paged_workspace_bytes(const fq_paged_batch *batch, int n_heads, int n_kv_heads, int with_weights);
+int fq_attn_paged(const fq_paged_batch *batch, const void *q, int ldq, int n_heads, int n_kv_heads, const void *k_pages,
+                  const void *v_pages, float scale, void *out, float *lse, const float *weights, float *weights_out,
+                  int weights_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Cut every sequence of the batch to `keep` positions, for each key/value head on its own: its last `recent` positions stay,
+ * and of the others the keep - recent with the largest weights (equal ones: the lower position; NaN counts as largest).
+ * What stays keeps its order and is copied to the pages that dst_table names, for pages may be shared by sequences; the
+ * caller frees the old ones.  A sequence of at most `keep` positions is copied whole.  Keys are stored rotated, so
+ * later tokens go on with their true positions, at slots behind new_len.
+ * seq_len, table, pages of the batch: where to copy from (its tokens do not matter).  weights fp32
+ * [seqs][n_kv_heads][weights_stride].  dst_table int32 [seqs][dst_stride], pages of k_out and v_out (dst_pages of them;
+ * they may be k_pages and v_pages, the pages other ones than are read).  kept int32 [seqs][n_kv_heads][keep], written:
+ * the positions that stay, then -1.  new_len int32 [seqs], written.  weights_out fp32
+ * [seqs][n_kv_heads][weights_out_stride], written: the weights of what stays; NULL: not wanted; not `weights` itself.
+ */
+int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void *v_pages, int n_kv_heads,
+                   const float *weights, int weights_stride, int keep, int recent, const int32_t *dst_table,
+                   int dst_stride, int dst_pages, void *k_out, void *v_out, int32_t *kept, int32_t *new_len,
+                   float *weights_out, int weights_out_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

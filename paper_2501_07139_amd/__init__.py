@@ -45,6 +45,12 @@ class fq_layer(ctypes.Structure):
     _fields_ = [("m", fq_matrix * 7)]
 
 
+class fq_paged_batch(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("table", ctypes.c_void_p), ("seqs", ctypes.c_int),
+                ("tokens", ctypes.c_int), ("max_q", ctypes.c_int), ("max_len", ctypes.c_int), ("table_stride", ctypes.c_int),
+                ("page", ctypes.c_int), ("pages", ctypes.c_int)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python paper_2501_07139_amd/build.py`")
@@ -92,6 +98,10 @@ def _load() -> ctypes.CDLL:
         "fq_prefill_workspace_bytes": (sz, [ci, ci, ci]),
         "fq_attn_prefill": (ci, [vp, vp, vp, ci, vp, vp, ci, ci, vp, vp, vp, sz, vp]),
         "fq_prefill_forward": (ci, [ctypes.POINTER(fq_layer), ci, vp, vp, ci, vp, vp, vp, ci, vp, vp, sz, vp]),
+        "fq_qk_norm_rope": (ci, [vp, ci, vp, ci, vp, ci, ci, ci, ci, vp, vp, vp, ci, vp, vp, ctypes.c_float, vp, vp, vp, ci, ci, vp]),
+        "fq_attn_paged_workspace_bytes": (sz, [ctypes.POINTER(fq_paged_batch), ci, ci, ci]),
+        "fq_attn_paged": (ci, [ctypes.POINTER(fq_paged_batch), vp, ci, ci, ci, vp, vp, ctypes.c_float, vp, vp, vp, vp, ci, vp, sz, vp]),
+        "fq_cache_evict": (ci, [ctypes.POINTER(fq_paged_batch), vp, vp, ci, vp, ci, ci, ci, vp, ci, ci, vp, vp, vp, vp, vp, ci, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -127,7 +137,8 @@ EXPORTS = ("fq_last_error", "fq_version", "fq_quantize_rtn", "fq_packed_bytes", 
            "fq_attn_prefill_workspace_bytes", "fq_prefill_workspace_bytes", "fq_attn_prefill", "fq_prefill_forward",
            "fq_init", "fq_dense_f16_tile", "fq_rope_table", "fq_stack_forward_noalloc", "fq_set_decode_mode",
            "fq_decode_give_up_ticks", "fq_async_error", "fq_clear_async_error", "fq_decode_partition", "fq_decode_persistent",
-           "fq_decode_persistent_launches", "fq_qlinear_route", "fq_qlinear_tall_tile", "fq_dense_route")
+           "fq_decode_persistent_launches", "fq_qlinear_route", "fq_qlinear_tall_tile", "fq_dense_route",
+           "fq_qk_norm_rope", "fq_attn_paged_workspace_bytes", "fq_attn_paged", "fq_cache_evict")
 
 
 # The calls below that small ones are made of go through _bind where nothing is to be allocated; it answers None to whatever it does
@@ -633,3 +644,189 @@ def fq_prefill_forward(stack: Stack, bitvec, x, k_cache, v_cache, rope, out=None
     _check(_lib.fq_prefill_forward(stack.table, stack.L, _hp(bitvec), _dp(x), T, _dp(out), _dp(k_cache), _dp(v_cache),
                                    Tmax, _dp(rope), _dp(workspace), workspace.numel(), _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------ paged cache
+PAGE_SIZES = (16, 32, 64, 128, 256)
+
+
+class PagedBatch:
+    """A ragged batch over a paged cache: what the calls below share for one step of a program that serves several sequences.
+
+    q_lens: tokens of every sequence in this call (the last ones of the sequence); seq_lens: its positions, those tokens
+    included; table: [sequences, pages of the longest] page numbers, what stands behind a sequence's last page is not used;
+    page, pages: positions of a page, pages of the pools.  positions: of every token, for the rotation; from the lengths if
+    not given (after an eviction they run ahead of the lengths, and are to be given).  All of it goes to the device in one copy.
+    """
+
+    def __init__(self, q_lens, seq_lens, table, page: int, pages: int, positions=None, device="cuda"):
+        q_lens, seq_lens = (np.asarray(a, dtype=np.int64).reshape(-1) for a in (q_lens, seq_lens))
+        table = np.atleast_2d(np.asarray(table, dtype=np.int64))
+        seqs = len(q_lens)
+        if page not in PAGE_SIZES or not 0 < pages <= (2 ** 31 - 1) // page:
+            raise FqError(-2, f"PagedBatch: {pages} pages of {page} positions (pages of {PAGE_SIZES}, 2^31 - 1 positions at most)")
+        if not 1 <= seqs <= 65535 or len(seq_lens) != seqs or table.ndim != 2 or table.shape[0] != seqs or table.shape[1] < 1:
+            raise FqError(-2, f"PagedBatch: {seqs} q_lens, {len(seq_lens)} seq_lens, table {table.shape}")
+        if q_lens.min() < 0 or seq_lens.min() < 0 or seq_lens.max() > min(table.shape[1] * page, 1 << 30) or q_lens.sum() >= 1 << 29:
+            raise FqError(-2, "PagedBatch: lengths must be at least 0 and fit the table")
+        used = np.arange(table.shape[1])[None, :] * page < seq_lens[:, None]
+        if ((table < 0) | (table >= pages))[used].any():
+            raise FqError(-2, f"PagedBatch: a page that is used lies outside 0..{pages - 1}")
+        tokens = int(q_lens.sum())
+        q_start = np.concatenate(([0], np.cumsum(q_lens)))
+        seq = np.repeat(np.arange(seqs), q_lens)
+        place = np.arange(tokens) - q_start[seq] + (seq_lens - q_lens)[seq]  # of every token in its sequence; below 0: not in it
+        at = np.maximum(place, 0)
+        slots = np.where(place < 0, -1, table[seq, at // page] * page + at % page) if tokens else np.zeros(0, dtype=np.int64)
+        positions = at if positions is None else np.asarray(positions, dtype=np.int64).reshape(-1)
+        if len(positions) != tokens:
+            raise FqError(-2, f"PagedBatch: {len(positions)} positions for {tokens} tokens")
+        parts, offset = (q_start, seq_lens, np.where(used, table, -1).reshape(-1), positions, slots), [0]
+        for a in parts:  # each from a 16-byte boundary on
+            offset.append(offset[-1] + (len(a) + 3) // 4 * 4)
+        host = np.zeros(offset[-1], dtype=np.int32)
+        for a, o in zip(parts, offset):
+            host[o:o + len(a)] = a
+        self._all = torch.from_numpy(host).to(device)
+        view = [self._all[o:o + len(a)] for a, o in zip(parts, offset)]
+        self.q_start, self.seq_len, self.table, self.positions, self.slots = view[0], view[1], view[2].view(seqs, -1), view[3], view[4]
+        self.seqs, self.tokens, self.page, self.pages = seqs, tokens, page, pages
+        self.max_q, self.max_len, self.device = int(q_lens.max()), int(seq_lens.max()), self._all.device
+        self.struct = fq_paged_batch(_dp(self.q_start), _dp(self.seq_len), _dp(self.table), seqs, tokens, self.max_q, self.max_len,
+                                     table.shape[1], page, pages)
+
+
+def _rows(t, width: int, what: str):
+    """fp16 rows [tokens, width], contiguous in a row; (tensor, elements from row to row)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16 or t.dim() != 2:
+        raise TypeError(f"{what} must be a device tensor [tokens, width] of torch.float16")
+    if t.shape[1] != width or (t.shape[0] and width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be [tokens, {width}] with contiguous rows, got {tuple(t.shape)}")
+    return t.stride(0) if t.shape[0] > 1 else (width + 7) // 8 * 8
+
+
+def _pools(batch, k_pages, v_pages, pages: int, what: str):
+    k_pages, v_pages = _dev(k_pages, torch.float16, "k_pages"), _dev(v_pages, torch.float16, "v_pages")
+    if k_pages.dim() != 4 or tuple(k_pages.shape[2:]) != (batch.page, 128) or v_pages.shape != k_pages.shape:
+        raise ValueError(f"{what}: pools [pages, n_kv_heads, {batch.page}, 128]")
+    if pages >= 0 and k_pages.shape[0] != pages:
+        raise ValueError(f"{what}: pools of {k_pages.shape[0]} pages, the batch has {pages}")
+    return k_pages.shape[1]
+
+
+def _same_device(what: str, device, *tensors):
+    if any(t is not None and t.device != device for t in tensors):
+        raise ValueError(f"{what}: all tensors must be on {device}")
+
+
+def _fresh(shape, dtype, device, stream):
+    """A tensor made by a call for work on `stream`: told to the allocator, so that its memory is not given away before."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None and t.numel():
+        s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+        if s != torch.cuda.current_stream(device):
+            s.wait_stream(torch.cuda.current_stream(device))  # its memory may still be in use by what was queued here
+            t.record_stream(s)
+    return t
+
+
+def fq_qk_norm_rope(q, k, v, batch: PagedBatch, rope, k_pages, v_pages, q_gain=None, k_gain=None, eps: float = 1e-5, out=None,
+                    stream=None):
+    """q, k, v fp16 [tokens, 128 heads] (rows may be columns of one product) -> rotated q; k and v go into the batch's slots."""
+    n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_qk_norm_rope")
+    width = q.shape[-1]
+    ld = [_rows(t, w, n) for t, w, n in ((q, width, "q"), (k, 128 * n_kv, "k"), (v, 128 * n_kv, "v"))]
+    rope = _dev(rope, torch.float32, "rope")
+    if width % 128 or any(t.shape[0] != batch.tokens for t in (q, k, v)):
+        raise ValueError(f"fq_qk_norm_rope: q, k, v [{batch.tokens}, 128 heads]")
+    if rope.dim() != 3 or tuple(rope.shape[1:]) != (64, 2):
+        raise ValueError("fq_qk_norm_rope: rope must be [positions, 64, 2]")
+    for gain in (q_gain, k_gain):
+        if gain is not None and _dev(gain, torch.float16, "gain").numel() != 128:
+            raise ValueError("fq_qk_norm_rope: gains [128]")
+    if out is None:
+        out = _fresh((batch.tokens, width), torch.float16, q.device, stream)
+    if _dev(out, torch.float16, "out").shape != q.shape:
+        raise ValueError("fq_qk_norm_rope: out must have the shape of q")
+    _same_device("fq_qk_norm_rope", batch.device, q, k, v, rope, k_pages, v_pages, q_gain, k_gain, out)
+    if batch.tokens:
+        _check(_lib.fq_qk_norm_rope(_dp(q), ld[0], _dp(k), ld[1], _dp(v), ld[2], batch.tokens, width // 128, n_kv, _dp(batch.positions),
+                                    _dp(batch.slots), _dp(rope), rope.shape[0], _dp(q_gain), _dp(k_gain), eps, _dp(out), _dp(k_pages),
+                                    _dp(v_pages), batch.page, batch.pages, _stream(stream)))
+    return out
+
+
+def fq_attn_paged_workspace_bytes(batch: PagedBatch, n_heads: int, n_kv_heads: int, with_weights: bool = False) -> int:
+    return _lib.fq_attn_paged_workspace_bytes(batch.struct, n_heads, n_kv_heads, int(with_weights))
+
+
+def fq_attn_paged(q, batch: PagedBatch, k_pages, v_pages, scale: Optional[float] = None, out=None, lse=None, weights=None,
+                  weights_out=None, workspace=None, stream=None):
+    """q fp16 [tokens, 128 heads] over the pages of the batch's sequences; scale: 1 / sqrt(128) if not given.
+
+    lse fp32 [tokens, heads] and weights_out fp32 [sequences, kv heads, >= positions of the longest] are written if given;
+    weights (of that shape, may be weights_out) are added to what the positions receive."""
+    n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_attn_paged")
+    width = q.shape[-1]
+    ldq = _rows(q, width, "q")
+    heads = width // 128
+    if width % 128 or q.shape[0] != batch.tokens or heads % n_kv:
+        raise ValueError(f"fq_attn_paged: q [{batch.tokens}, 128 heads], heads a multiple of {n_kv}")
+    if out is None:
+        out = _fresh((batch.tokens, width), torch.float16, q.device, stream)
+    if _dev(out, torch.float16, "out").shape != q.shape:
+        raise ValueError("fq_attn_paged: out must have the shape of q")
+    if lse is not None and tuple(_dev(lse, torch.float32, "lse").shape) != (batch.tokens, heads):
+        raise ValueError(f"fq_attn_paged: lse [{batch.tokens}, {heads}]")
+    wstride = 0
+    if weights_out is not None:
+        wstride = _weights(weights_out, batch, n_kv, "weights_out")
+        if weights is not None and _weights(weights, batch, n_kv, "weights") != wstride:
+            raise ValueError("fq_attn_paged: weights and weights_out must have one shape")
+    elif weights is not None:
+        raise ValueError("fq_attn_paged: weights without weights_out")
+    if workspace is None:
+        nbytes = fq_attn_paged_workspace_bytes(batch, heads, n_kv, weights_out is not None)
+        workspace = _fresh((nbytes,), torch.uint8, q.device, stream) if nbytes else None
+    _same_device("fq_attn_paged", batch.device, q, k_pages, v_pages, out, lse, weights, weights_out, workspace)
+    _check(_lib.fq_attn_paged(batch.struct, _dp(q), ldq, heads, n_kv, _dp(k_pages), _dp(v_pages), 128 ** -0.5 if scale is None else scale,
+                              _dp(out), _dp(lse), _dp(weights), _dp(weights_out), wstride, _dp(workspace),
+                              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def _weights(t, batch, n_kv: int, what: str) -> int:
+    if _dev(t, torch.float32, what).dim() != 3 or tuple(t.shape[:2]) != (batch.seqs, n_kv) or t.shape[2] < batch.max_len:
+        raise ValueError(f"{what} must be [{batch.seqs}, {n_kv}, >= {batch.max_len}], got {tuple(t.shape)}")
+    return t.shape[2]
+
+
+def fq_cache_evict(batch: PagedBatch, weights, k_pages, v_pages, dst_table, keep: int, recent: int, k_out=None, v_out=None, kept=None,
+                   new_len=None, weights_out=None, stream=None):
+    """Cut every sequence to `keep` positions a head, into the pages of dst_table (int32 [sequences, pages], device) of k_out, v_out (the
+    same pools if not given).  Returns (kept int32 [sequences, kv heads, keep], new_len int32 [sequences]); weights_out fp32
+    [sequences, kv heads, >= keep] takes the weights of what stays."""
+    n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_cache_evict")
+    if (k_out is None) != (v_out is None):
+        raise ValueError("fq_cache_evict: k_out and v_out go together")
+    k_out, v_out = (k_pages, v_pages) if k_out is None else (k_out, v_out)
+    if _pools(batch, k_out, v_out, -1, "fq_cache_evict") != n_kv:
+        raise ValueError("fq_cache_evict: k_out must have the heads of k_pages")
+    _weights(weights, batch, n_kv, "weights")
+    if _dev(dst_table, torch.int32, "dst_table").dim() != 2 or dst_table.shape[0] != batch.seqs:
+        raise ValueError(f"fq_cache_evict: dst_table [{batch.seqs}, pages]")
+    if keep <= 0:
+        raise FqError(-2, f"fq_cache_evict: keep={keep}")
+    if kept is None:
+        kept = _fresh((batch.seqs, n_kv, keep), torch.int32, k_pages.device, stream)
+    if new_len is None:
+        new_len = _fresh((batch.seqs,), torch.int32, k_pages.device, stream)
+    if tuple(_dev(kept, torch.int32, "kept").shape) != (batch.seqs, n_kv, keep) or _dev(new_len, torch.int32, "new_len").numel() != batch.seqs:
+        raise ValueError(f"fq_cache_evict: kept [{batch.seqs}, {n_kv}, {keep}], new_len [{batch.seqs}]")
+    if weights_out is not None and tuple(_dev(weights_out, torch.float32, "weights_out").shape[:2]) != (batch.seqs, n_kv):
+        raise ValueError(f"fq_cache_evict: weights_out [{batch.seqs}, {n_kv}, >= {keep}]")
+    _same_device("fq_cache_evict", batch.device, weights, k_pages, v_pages, dst_table, k_out, v_out, kept, new_len, weights_out)
+    _check(_lib.fq_cache_evict(batch.struct, _dp(k_pages), _dp(v_pages), n_kv, _dp(weights), weights.shape[2], keep, recent, _dp(dst_table),
+                               dst_table.shape[1], k_out.shape[0], _dp(k_out), _dp(v_out), _dp(kept), _dp(new_len), _dp(weights_out),
+                               0 if weights_out is None else weights_out.shape[2], _stream(stream)))
+    return kept, new_len

@@ -758,3 +758,141 @@ extern "C" int fq_prefill_forward(const fq_layer *layers, int L, const uint8_t *
     }
     return FQ_OK;
 }
+
+// ------------------------------------------------------------------ paged cache
+namespace {
+
+int page_log2(int page) // 4..8, or -1
+{
+    for (int l = 4; l <= 8; ++l)
+        if (page == 1 << l)
+            return l;
+    return -1;
+}
+
+int check_pool(const char *fn, int page, int pages, int n_kv_heads)
+{
+    if (page_log2(page) < 0)
+        return fq_fail(FQ_ERR_SHAPE, "%s: pages of %d positions (16, 32, 64, 128 or 256)", fn, page);
+    if (pages <= 0 || (long long)pages * page > INT32_MAX)
+        return fq_fail(FQ_ERR_SHAPE, "%s: %d pages of %d positions (at most 2^31 - 1 positions)", fn, pages, page);
+    if (n_kv_heads <= 0 || n_kv_heads > 65535)
+        return fq_fail(FQ_ERR_SHAPE, "%s: n_kv_heads=%d", fn, n_kv_heads);
+    return FQ_OK;
+}
+
+int check_heads(const char *fn, int tokens, int n_heads, int n_kv_heads)
+{
+    if (n_kv_heads <= 0 || n_heads <= 0 || n_heads % n_kv_heads != 0 || (long long)tokens * n_heads > INT32_MAX / 4)
+        return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d n_heads=%d n_kv_heads=%d (n_heads a multiple of n_kv_heads, tokens * n_heads "
+                       "below 2^29)", fn, tokens, n_heads, n_kv_heads);
+    return FQ_OK;
+}
+
+int check_batch(const char *fn, const fq_paged_batch *b, int n_kv_heads)
+{
+    if (!b || !b->q_start || !b->seq_len || !b->table)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL batch or array of it", fn);
+    if (int rc = check_pool(fn, b->page, b->pages, n_kv_heads))
+        return rc;
+    if (b->seqs <= 0 || b->seqs > 65535 || b->tokens < 0 || b->max_q < 0 || b->max_q > b->tokens || (long long)b->max_q * b->seqs < b->tokens)
+        return fq_fail(FQ_ERR_SHAPE, "%s: seqs=%d tokens=%d max_q=%d (need max_q <= tokens <= seqs * max_q)", fn, b->seqs, b->tokens, b->max_q);
+    if (b->table_stride <= 0 || b->max_len < 0 || b->max_len > (1 << 30) || b->max_len > (long long)b->table_stride * b->page)
+        return fq_fail(FQ_ERR_SHAPE, "%s: max_len=%d table_stride=%d (need max_len <= table_stride * page, at most 2^30)", fn, b->max_len,
+                       b->table_stride);
+    return FQ_OK;
+}
+
+bool stride_ok(int ld, int width) { return ld >= width && ld % 8 == 0; }
+
+} // namespace
+
+extern "C" int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, int tokens, int n_heads, int n_kv_heads,
+                               const int32_t *positions, const int32_t *slots, const float *rope, int rope_rows, const void *q_gain,
+                               const void *k_gain, float eps, void *q_out, void *k_pages, void *v_pages, int page, int pages, void *stream)
+{
+    const char *fn = "fq_qk_norm_rope";
+    if (!q || !k || !v || !positions || !slots || !rope || !q_out || !k_pages || !v_pages)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    if (int rc = check_pool(fn, page, pages, n_kv_heads))
+        return rc;
+    if (int rc = check_heads(fn, tokens, n_heads, n_kv_heads))
+        return rc;
+    if (tokens < 0 || n_heads > 65535 || rope_rows <= 0 || !(eps >= 0.f))
+        return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d n_heads=%d rope_rows=%d eps=%g", fn, tokens, n_heads, rope_rows, eps);
+    if (!stride_ok(ldq, n_heads * 128) || !stride_ok(ldk, n_kv_heads * 128) || !stride_ok(ldv, n_kv_heads * 128))
+        return fq_fail(FQ_ERR_SHAPE, "%s: ldq=%d ldk=%d ldv=%d (at least the row, multiples of 8)", fn, ldq, ldk, ldv);
+    if (q_out == q && ldq != n_heads * 128)
+        return fq_fail(FQ_ERR_SHAPE, "%s: q_out is q, whose rows are not contiguous", fn);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(rope) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(q_out) ||
+        !aligned16(k_pages) || !aligned16(v_pages))
+        return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    if (tokens == 0)
+        return FQ_OK;
+    return check_hip(fq_launch_qk_norm_rope(q, ldq, k, ldk, v, ldv, tokens, n_heads, n_kv_heads, positions, slots, rope, rope_rows, q_gain, k_gain,
+                                            eps, q_out, k_pages, v_pages, page_log2(page), pages, static_cast<fq_stream>(stream)),
+                     "fq_qk_norm_rope launch");
+}
+
+extern "C" size_t fq_attn_paged_workspace_bytes(const fq_paged_batch *batch, int n_heads, int n_kv_heads, int with_weights)
+{
+    const char *fn = "fq_attn_paged_workspace_bytes";
+    if (check_batch(fn, batch, n_kv_heads) || check_heads(fn, batch->tokens, n_heads, n_kv_heads))
+        return 0;
+    return align_up(fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, with_weights != 0));
+}
+
+extern "C" int fq_attn_paged(const fq_paged_batch *batch, const void *q, int ldq, int n_heads, int n_kv_heads, const void *k_pages,
+                             const void *v_pages, float scale, void *out, float *lse, const float *weights, float *weights_out,
+                             int weights_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *fn = "fq_attn_paged";
+    if (int rc = check_batch(fn, batch, n_kv_heads))
+        return rc;
+    if (int rc = check_heads(fn, batch->tokens, n_heads, n_kv_heads))
+        return rc;
+    if (!k_pages || !v_pages || (batch->tokens > 0 && (!q || !out)))
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    if (!stride_ok(ldq, n_heads * 128))
+        return fq_fail(FQ_ERR_SHAPE, "%s: ldq=%d (at least the row, a multiple of 8)", fn, ldq);
+    if (!(scale > 0.f) || scale > 1e30f)
+        return fq_fail(FQ_ERR_SHAPE, "%s: scale=%g (must be positive and finite)", fn, scale);
+    if (weights && !weights_out)
+        return fq_fail(FQ_ERR_NULL, "%s: weights without weights_out", fn);
+    if (weights_out && weights_stride < batch->max_len)
+        return fq_fail(FQ_ERR_SHAPE, "%s: weights_stride=%d below max_len=%d", fn, weights_stride, batch->max_len);
+    const size_t need = fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, weights_out != nullptr);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fq_fail(FQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace))
+        return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    return check_hip(fq_launch_attn_paged(*batch, q, ldq, n_heads, n_kv_heads, k_pages, v_pages, scale, out, lse, weights, weights_out,
+                                          weights_stride, workspace, static_cast<fq_stream>(stream)), "fq_attn_paged launch");
+}
+
+extern "C" int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void *v_pages, int n_kv_heads, const float *weights,
+                              int weights_stride, int keep, int recent, const int32_t *dst_table, int dst_stride, int dst_pages, void *k_out,
+                              void *v_out, int32_t *kept, int32_t *new_len, float *weights_out, int weights_out_stride, void *stream)
+{
+    const char *fn = "fq_cache_evict";
+    if (int rc = check_batch(fn, batch, n_kv_heads))
+        return rc;
+    if (!k_pages || !v_pages || !weights || !dst_table || !k_out || !v_out || !kept || !new_len)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    if (weights_out == weights)
+        return fq_fail(FQ_ERR_SHAPE, "%s: weights_out must not be weights", fn);
+    if (keep <= 0 || keep > (1 << 30) || recent < 0 || recent > keep)
+        return fq_fail(FQ_ERR_SHAPE, "%s: keep=%d recent=%d (need 0 <= recent <= keep, 0 < keep)", fn, keep, recent);
+    if (int rc = check_pool(fn, batch->page, dst_pages, n_kv_heads))
+        return rc;
+    const int most = batch->max_len < keep ? batch->max_len : keep;
+    if (weights_stride < batch->max_len || (weights_out && weights_out_stride < most) || dst_stride <= 0 ||
+        (long long)dst_stride * batch->page < most)
+        return fq_fail(FQ_ERR_SHAPE, "%s: weights_stride=%d weights_out_stride=%d dst_stride=%d for %d positions cut to %d", fn, weights_stride,
+                       weights_out_stride, dst_stride, batch->max_len, most);
+    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_out) || !aligned16(v_out))
+        return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    return check_hip(fq_launch_cache_evict(*batch, k_pages, v_pages, n_kv_heads, weights, weights_stride, keep, recent, dst_table, dst_stride,
+                                           dst_pages, k_out, v_out, kept, new_len, weights_out, weights_out_stride,
+                                           static_cast<fq_stream>(stream)), "fq_cache_evict launch");
+}

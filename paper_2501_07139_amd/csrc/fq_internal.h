@@ -104,6 +104,16 @@ int fq_launch_attn_decode(const void *q, const void *k, const void *v, void *k_c
 size_t fq_attn_prefill_scratch_bytes(int T, int n_heads);
 int fq_launch_attn_prefill(const void *q, const void *k, const void *v, int T, void *k_cache, void *v_cache,
                            int Tmax, int n_heads, const float *rope, void *out, void *workspace, fq_stream st);
+// Paged cache (fq_paged_cache.hip, fq_paged_attn.hip): page_log2 of a power of two, heads a multiple of kv_heads.
+int fq_launch_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, int tokens, int heads, int kv_heads,
+                           const int32_t *positions, const int32_t *slots, const float *rope, int rope_rows, const void *q_gain,
+                           const void *k_gain, float eps, void *q_out, void *k_pages, void *v_pages, int page_log2, int pages, fq_stream st);
+size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights);
+int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int heads, int kv_heads, const void *k, const void *v, float scale,
+                         void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st);
+int fq_launch_cache_evict(const fq_paged_batch &batch, const void *k, const void *v, int kv_heads, const float *weights, int weights_stride, int keep,
+                          int recent, const int32_t *dst_table, int dst_stride, int dst_pages, void *k_out, void *v_out, int32_t *kept,
+                          int32_t *new_len, float *weights_out, int weights_out_stride, fq_stream st);
 int fq_launch_glue(int op, const void *a, const void *b, const void *c, int M, int H, void *out, fq_stream st);
 // Two steps in one pass: op 6: aux = a + b, out = rms(aux); op 7: aux = rms(a + b), out = rms(aux).
 int fq_launch_glue2(int op, const void *a, const void *b, int M, int H, void *aux, void *out, fq_stream st);

@@ -1,0 +1,270 @@
+// Around the attention over a paged cache: what writes its rows and what thins them out.  Bound by the bytes they move, or by the launch.
+#include "fq_paged.h"
+
+namespace {
+
+// ------------------------------------------------------- norm, rotation, write
+// Per token and head of 128 (q and k): x / sqrt(mean x^2 + eps) * gain where there is a gain, then the adjacent pairs turned by the
+// position's angles; fp32 throughout, one rounding.  v is copied.  Sixteen lanes hold a row, eight values each.
+struct RopeArgs {
+    const _Float16 *q, *k, *v;
+    const int *positions, *slots;
+    const float *rope;
+    const _Float16 *q_gain, *k_gain;
+    _Float16 *q_out, *k_pages, *v_pages;
+    int ldq, ldk, ldv, tokens, heads, kv_heads, rope_rows, page_log2, slots_end;
+    float eps;
+};
+
+constexpr int ROPE_ROWS = 16; // rows a workgroup of 256 threads
+
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeArgs p)
+{
+    const int m = blockIdx.y, r = threadIdx.x & 15;
+    const int row = blockIdx.x * ROPE_ROWS + (threadIdx.x >> 4); // head of q, then of k, then of v
+    if (row >= p.heads + 2 * p.kv_heads)
+        return;
+    const bool is_q = row < p.heads, is_v = row >= p.heads + p.kv_heads;
+    const int head = is_q ? row : (is_v ? row - p.heads - p.kv_heads : row - p.heads);
+    const _Float16 *src = (is_q ? p.q + (size_t)m * p.ldq : is_v ? p.v + (size_t)m * p.ldv : p.k + (size_t)m * p.ldk) + head * PD + 8 * r;
+    h8 x = *reinterpret_cast<const h8 *>(src);
+    if (!is_v) {
+        const int pos = min(max(p.positions[m], 0), p.rope_rows - 1);
+        const f4 lo = *reinterpret_cast<const f4 *>(p.rope + (size_t)pos * PD + 8 * r);
+        const f4 hi = *reinterpret_cast<const f4 *>(p.rope + (size_t)pos * PD + 8 * r + 4);
+        const _Float16 *gain = is_q ? p.q_gain : p.k_gain;
+        float t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            t[e] = (float)x[e];
+        if (gain) {
+            const h8 g = *reinterpret_cast<const h8 *>(gain + 8 * r);
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                ss = fmaf(t[e], t[e], ss);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1)
+                ss += __shfl_xor(ss, o, 64);
+            const float inv = 1.0f / sqrtf(ss * (1.0f / PD) + p.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                t[e] = t[e] * inv * (float)g[e];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float c = i < 2 ? lo[2 * i] : hi[2 * i - 4], s = i < 2 ? lo[2 * i + 1] : hi[2 * i - 3];
+            x[2 * i] = (_Float16)(t[2 * i] * c - t[2 * i + 1] * s);
+            x[2 * i + 1] = (_Float16)(t[2 * i] * s + t[2 * i + 1] * c);
+        }
+    }
+    if (is_q) {
+        *reinterpret_cast<h8 *>(p.q_out + ((size_t)m * p.heads + head) * PD + 8 * r) = x;
+        return;
+    }
+    const int slot = p.slots[m];
+    if (slot < 0 || slot >= p.slots_end)
+        return; // a token that is not cached
+    const size_t at = (((size_t)(slot >> p.page_log2) * p.kv_heads + head) << p.page_log2) | (size_t)(slot & ((1 << p.page_log2) - 1));
+    *reinterpret_cast<h8 *>((is_v ? p.v_pages : p.k_pages) + at * PD + 8 * r) = x;
+}
+
+// ------------------------------------------------------------------- eviction
+// Of a head's len positions the last `recent` stay, and of the others the keep - recent that weigh most (equal weights: the lower
+// position).  Selecting kernel, one workgroup per (sequence, head): the weight that the last one kept has is found eight bits at a
+// time (radix selection over keys that order like the weights), then one pass in order numbers what stays.
+struct EvictArgs {
+    PagedSeqs s;
+    const _Float16 *k, *v;
+    const float *weights;
+    _Float16 *k_out, *v_out;
+    const int *dst_table;
+    int *kept, *new_len;
+    float *weights_out;
+    int kv_heads, weights_stride, weights_out_stride, keep, recent, dst_stride, dst_pages;
+};
+
+constexpr int SEL = 1024;
+
+// Larger weight, larger key; -0 and 0 alike; NaN above everything, as it says nothing against its position.
+__device__ __forceinline__ uint32_t weight_key(float w)
+{
+    if (w != w)
+        return 0xffffffffu;
+    const uint32_t u = __builtin_bit_cast(uint32_t, w + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(SEL) void evict_select_kernel(EvictArgs p)
+{
+    __shared__ int hist[256];
+    __shared__ int found[2];
+    __shared__ int wave_gt[SEL / 64], wave_eq[SEL / 64];
+    const int head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int len = min(max(p.s.seq_len[b], 0), p.s.max_len);
+    const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
+    const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
+    int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
+    float *wo = p.weights_out ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
+    if (head == 0 && tid == 0)
+        p.new_len[b] = m;
+    uint32_t prefix = 0;
+    int left = need; // how many of the keys that match the prefix so far are kept
+    if (need > 0 && need < old) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            if (tid < 256)
+                hist[tid] = 0;
+            __syncthreads();
+            const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
+            for (int t = tid; t < old; t += SEL) {
+                const uint32_t key = weight_key(w[t]);
+                if ((key & mask) == prefix)
+                    atomicAdd(&hist[(key >> shift) & 255], 1);
+            }
+            __syncthreads();
+            if (tid < 256) {
+                int above = 0;
+                for (int d = tid + 1; d < 256; ++d)
+                    above += hist[d];
+                if (above < left && left <= above + hist[tid]) { // one thread
+                    found[0] = tid;
+                    found[1] = left - above;
+                }
+            }
+            __syncthreads();
+            prefix |= (uint32_t)found[0] << shift;
+            left = found[1];
+            __syncthreads();
+        }
+    }
+    // in order: a key above the last one kept stays, equal ones while they last
+    const bool all = need >= old, none = need <= 0;
+    int gt_before = 0, eq_before = 0;
+    for (int t0 = 0; t0 < len; t0 += SEL) {
+        const int t = t0 + tid;
+        const float weight = t < len ? w[t] : 0.f;
+        const uint32_t key = weight_key(weight);
+        const bool gt = t < len && (t >= old || all || (!none && key > prefix));
+        const bool eq = t < old && !all && !none && key == prefix;
+        const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
+        if (lane == 0) {
+            wave_gt[wave] = (int)__popcll(gts);
+            wave_eq[wave] = (int)__popcll(eqs);
+        }
+        __syncthreads();
+        int g = gt_before, e = eq_before;
+        for (int i = 0; i < SEL / 64; ++i) {
+            if (i == wave) {
+                const unsigned long long lower = (1ull << lane) - 1;
+                const int ge = g + (int)__popcll(gts & lower), ee = e + (int)__popcll(eqs & lower);
+                if (gt || (eq && ee < left)) {
+                    const int at = ge + min(ee, left);
+                    if (at < m) {
+                        kept[at] = t;
+                        if (wo)
+                            wo[at] = weight;
+                    }
+                }
+            }
+            g += wave_gt[i];
+            e += wave_eq[i];
+        }
+        gt_before = g;
+        eq_before = e;
+        __syncthreads();
+    }
+    for (int t = m + tid; t < p.keep; t += SEL)
+        kept[t] = -1;
+}
+
+// Copies the rows that stay, in order, sixteen lanes a row of keys and its row of values.
+__global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs p)
+{
+    const int head = blockIdx.y, b = blockIdx.z, r = threadIdx.x & 15;
+    const int j = blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int m = min(min(max(p.s.seq_len[b], 0), p.s.max_len), p.keep);
+    if (j >= m)
+        return;
+    const int t = max(p.kept[((size_t)b * p.kv_heads + head) * p.keep + j], 0);
+    const size_t from = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, head, b, t) * PD + 8 * r;
+    const size_t to = pool_row(p.dst_table, p.dst_stride, p.s.page_log2, p.dst_pages, p.kv_heads, head, b, j) * PD + 8 * r;
+    const h8 k = *reinterpret_cast<const h8 *>(p.k + from), v = *reinterpret_cast<const h8 *>(p.v + from);
+    *reinterpret_cast<h8 *>(p.k_out + to) = k;
+    *reinterpret_cast<h8 *>(p.v_out + to) = v;
+}
+
+} // namespace
+
+int fq_launch_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, int tokens, int heads, int kv_heads,
+                           const int32_t *positions, const int32_t *slots, const float *rope, int rope_rows, const void *q_gain,
+                           const void *k_gain, float eps, void *q_out, void *k_pages, void *v_pages, int page_log2, int pages, fq_stream st)
+{
+    RopeArgs a;
+    a.q = static_cast<const _Float16 *>(q);
+    a.k = static_cast<const _Float16 *>(k);
+    a.v = static_cast<const _Float16 *>(v);
+    a.positions = positions;
+    a.slots = slots;
+    a.rope = rope;
+    a.q_gain = static_cast<const _Float16 *>(q_gain);
+    a.k_gain = static_cast<const _Float16 *>(k_gain);
+    a.q_out = static_cast<_Float16 *>(q_out);
+    a.k_pages = static_cast<_Float16 *>(k_pages);
+    a.v_pages = static_cast<_Float16 *>(v_pages);
+    a.ldq = ldq;
+    a.ldk = ldk;
+    a.ldv = ldv;
+    a.tokens = tokens;
+    a.heads = heads;
+    a.kv_heads = kv_heads;
+    a.rope_rows = rope_rows;
+    a.page_log2 = page_log2;
+    a.slots_end = pages << page_log2;
+    a.eps = eps;
+    for (int m0 = 0; m0 < tokens; m0 += 65535) { // the second extent of a grid ends there
+        RopeArgs part = a;
+        part.tokens = tokens - m0 < 65535 ? tokens - m0 : 65535;
+        part.q += (size_t)m0 * ldq;
+        part.k += (size_t)m0 * ldk;
+        part.v += (size_t)m0 * ldv;
+        part.positions += m0;
+        part.slots += m0;
+        part.q_out += (size_t)m0 * heads * PD;
+        hipLaunchKernelGGL(qk_norm_rope_kernel, dim3((heads + 2 * kv_heads + ROPE_ROWS - 1) / ROPE_ROWS, part.tokens), dim3(256), 0, st, part);
+        if (int rc = (int)hipGetLastError())
+            return rc;
+    }
+    return 0;
+}
+
+int fq_launch_cache_evict(const fq_paged_batch &batch, const void *k, const void *v, int kv_heads, const float *weights, int weights_stride, int keep,
+                          int recent, const int32_t *dst_table, int dst_stride, int dst_pages, void *k_out, void *v_out, int32_t *kept,
+                          int32_t *new_len, float *weights_out, int weights_out_stride, fq_stream st)
+{
+    EvictArgs a;
+    a.s = paged_seqs(batch);
+    a.k = static_cast<const _Float16 *>(k);
+    a.v = static_cast<const _Float16 *>(v);
+    a.weights = weights;
+    a.k_out = static_cast<_Float16 *>(k_out);
+    a.v_out = static_cast<_Float16 *>(v_out);
+    a.dst_table = dst_table;
+    a.kept = kept;
+    a.new_len = new_len;
+    a.weights_out = weights_out;
+    a.kv_heads = kv_heads;
+    a.weights_stride = weights_stride;
+    a.weights_out_stride = weights_out_stride;
+    a.keep = keep;
+    a.recent = recent;
+    a.dst_stride = dst_stride;
+    a.dst_pages = dst_pages;
+    hipLaunchKernelGGL(evict_select_kernel, dim3(kv_heads, batch.seqs), dim3(SEL), 0, st, a);
+    if (int rc = (int)hipGetLastError())
+        return rc;
+    const int most = batch.max_len < keep ? batch.max_len : keep;
+    if (most == 0)
+        return 0;
+    hipLaunchKernelGGL(evict_copy_kernel, dim3((most + 15) / 16, kv_heads, batch.seqs), dim3(256), 0, st, a);
+    return (int)hipGetLastError();
+}

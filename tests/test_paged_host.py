@@ -1,0 +1,148 @@
+"""Paged cache, host side: the batch that Python lays out, and what the entry points refuse (no GPU needed)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2501_07139_amd as fq
+from oracle import paged_ref
+
+
+def batch(**changes):
+    b = fq.fq_paged_batch(q_start=16, seq_len=16, table=16, seqs=2, tokens=5, max_q=3, max_len=100, table_stride=8, page=16, pages=40)
+    for k, v in changes.items():
+        setattr(b, k, v)
+    return b
+
+
+def test_batch_lays_out_lengths_positions_and_slots():
+    table = [[5, 2, -1], [1, 7, 3], [0, 0, 0], [4, -7, 99]]
+    b = fq.PagedBatch([1, 4, 0, 3], [17, 35, 0, 2], table, 16, 8, device="cpu")
+    assert (b.seqs, b.tokens, b.max_q, b.max_len) == (4, 8, 4, 35)
+    assert b.q_start.tolist() == [0, 1, 5, 5, 8] and b.seq_len.tolist() == [17, 35, 0, 2]
+    assert b.table.tolist() == [[5, 2, -1], [1, 7, 3], [-1, -1, -1], [4, -1, -1]]
+    assert b.positions.tolist() == [16, 31, 32, 33, 34, 0, 0, 1]
+    # the last sequence has three tokens and two positions: its first token is in no slot
+    assert b.slots.tolist() == [32, 7 * 16 + 15, 48, 49, 50, -1, 64, 65]
+    assert all(t.data_ptr() % 16 == 0 for t in (b.q_start, b.seq_len, b.table, b.positions, b.slots))
+    s = b.struct
+    assert (s.seqs, s.tokens, s.max_q, s.max_len, s.table_stride, s.page, s.pages) == (4, 8, 4, 35, 3, 16, 8)
+    assert s.table == b.table.data_ptr() and s.q_start == b.q_start.data_ptr() and s.seq_len == b.seq_len.data_ptr()
+    given = fq.PagedBatch([2], [2], [[0]], 16, 1, positions=[70, 71], device="cpu")
+    assert given.positions.tolist() == [70, 71] and given.slots.tolist() == [0, 1]
+    none = fq.PagedBatch([0], [20], [[1, 0]], 16, 2, device="cpu")
+    assert none.tokens == 0 and none.max_q == 0 and none.slots.numel() == 0
+
+
+@pytest.mark.parametrize("args", [([1], [17], [[0]], 16, 4), ([1], [4], [[4]], 16, 4), ([1], [4], [[-1]], 16, 4), ([-1], [4], [[0]], 16, 4),
+                                  ([1], [-4], [[0]], 16, 4), ([1], [4], [[0]], 24, 4), ([1], [4], [[0]], 16, 0), ([1, 1], [4], [[0]], 16, 4),
+                                  ([1], [4], [[0], [1]], 16, 4), ([], [], [[0]], 16, 4), ([1], [4], [[0]], 256, 1 << 23)], ids=str)
+def test_batch_refuses(args):
+    with pytest.raises(fq.FqError) as e:
+        fq.PagedBatch(*args, device="cpu")
+    assert e.value.code == -2
+
+
+def test_batch_refuses_positions_of_another_length():
+    with pytest.raises(fq.FqError):
+        fq.PagedBatch([2], [4], [[0]], 16, 4, positions=[1], device="cpu")
+
+
+def attn(lib, b, **c):
+    a = dict(q=16, ldq=256, heads=2, kv=2, k=16, v=16, scale=1.0, out=16, lse=None, weights=None, weights_out=None, stride=0,
+             ws=16, ws_bytes=1 << 30)
+    a.update(c)
+    return lib.fq_attn_paged(None if b is None else ctypes.byref(b), a["q"], a["ldq"], a["heads"], a["kv"], a["k"], a["v"], a["scale"], a["out"],
+                             a["lse"], a["weights"], a["weights_out"], a["stride"], a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("code, call, changes", [
+    (-1, {}, None), (-1, {}, {"q_start": None}), (-1, {}, {"seq_len": None}), (-1, {}, {"table": None}), (-1, {"q": None}, {}), (-1, {"k": None}, {}),
+    (-1, {"v": None}, {}), (-1, {"out": None}, {}), (-1, {"weights": 16}, {}), (-2, {"heads": 3}, {}), (-2, {"heads": 0}, {}), (-2, {"kv": 0}, {}),
+    (-2, {"ldq": 255}, {}), (-2, {"ldq": 260}, {}), (-2, {"scale": 0.0}, {}), (-2, {"scale": -1.0}, {}), (-2, {"scale": float("nan")}, {}),
+    (-2, {"scale": float("inf")}, {}), (-2, {"weights_out": 16, "stride": 99}, {}), (-2, {}, {"seqs": 0}), (-2, {}, {"seqs": 65536}),
+    (-2, {}, {"tokens": -1}), (-2, {}, {"max_q": 6}), (-2, {}, {"max_q": 2}), (-2, {}, {"max_len": 129}), (-2, {}, {"max_len": -1}),
+    (-2, {}, {"table_stride": 0}), (-2, {}, {"page": 8}), (-2, {}, {"page": 48}), (-2, {}, {"page": 512}), (-2, {}, {"pages": 0}),
+    (-2, {}, {"pages": 1 << 27, "page": 16}), (-2, {"heads": 1 << 28, "kv": 1}, {"tokens": 3}), (-5, {"q": 8}, {}), (-5, {"k": 24}, {}),
+    (-5, {"v": 24}, {}), (-5, {"out": 8}, {}), (-6, {"ws": None, "weights_out": 16, "stride": 100}, {}),
+    (-6, {"ws_bytes": 8, "weights_out": 16, "stride": 100}, {})], ids=str)
+def test_attention_refuses(code, call, changes):
+    b = None if changes is None else batch(**changes)
+    assert attn(fq._lib, b, **call) == code
+    assert "fq_attn_paged" in fq.fq_last_error()
+
+
+def test_workspace_of_bad_arguments_is_none():
+    lib = fq._lib
+    assert lib.fq_attn_paged_workspace_bytes(None, 2, 2, 0) == 0
+    assert lib.fq_attn_paged_workspace_bytes(ctypes.byref(batch(page=5)), 2, 2, 0) == 0
+    assert lib.fq_attn_paged_workspace_bytes(ctypes.byref(batch()), 3, 2, 0) == 0
+    assert lib.fq_attn_paged_workspace_bytes(ctypes.byref(batch()), 2, 2, 1) >= 5 * 2 * 4
+
+
+def rope(lib, **c):
+    a = dict(q=16, ldq=256, k=16, ldk=256, v=16, ldv=256, tokens=3, heads=2, kv=2, positions=16, slots=16, rope=16, rows=9, qg=None, kg=None,
+             eps=1e-5, out=32, kp=16, vp=16, page=16, pages=4)
+    a.update(c)
+    return lib.fq_qk_norm_rope(*a.values(), None)
+
+
+@pytest.mark.parametrize("code, call", [(-1, {n: None}) for n in ("q", "k", "v", "positions", "slots", "rope", "out", "kp", "vp")] + [
+    (-2, {"tokens": -1}), (-2, {"heads": 3}), (-2, {"heads": 0}), (-2, {"kv": 0}), (-2, {"rows": 0}), (-2, {"eps": -1.0}),
+    (-2, {"eps": float("nan")}), (-2, {"ldq": 255}), (-2, {"ldk": 252}), (-2, {"ldv": 260}), (-2, {"page": 20}), (-2, {"pages": 0}),
+    (-2, {"out": 16, "ldq": 512}), (-5, {"q": 8}), (-5, {"k": 8}), (-5, {"v": 8}), (-5, {"rope": 8}), (-5, {"qg": 8}), (-5, {"kg": 8}),
+    (-5, {"out": 40}), (-5, {"kp": 8}), (-5, {"vp": 8})], ids=str)
+def test_norm_rope_refuses(code, call):
+    assert rope(fq._lib, **call) == code
+    assert "fq_qk_norm_rope" in fq.fq_last_error()
+
+
+def test_norm_rope_of_no_tokens_does_nothing():
+    assert rope(fq._lib, tokens=0) == 0
+
+
+def evict(lib, b, **c):
+    a = dict(k=16, v=16, kv=2, w=16, ws=100, keep=40, recent=8, dst=16, ds=3, dp=9, ko=16, vo=16, kept=16, new=16, wo=None, wos=0)
+    a.update(c)
+    return lib.fq_cache_evict(None if b is None else ctypes.byref(b), *a.values(), None)
+
+
+@pytest.mark.parametrize("code, call, changes", [(-1, {n: None}, {}) for n in ("k", "v", "w", "dst", "ko", "vo", "kept", "new")] + [
+    (-1, {}, None), (-2, {"kv": 0}, {}), (-2, {"ws": 99}, {}), (-2, {"keep": 0}, {}), (-2, {"recent": -1}, {}), (-2, {"recent": 41}, {}),
+    (-2, {"ds": 2}, {}), (-2, {"ds": 0}, {}), (-2, {"dp": 0}, {}), (-2, {"wo": 32, "wos": 39}, {}), (-2, {"wo": 16, "wos": 100}, {}),
+    (-2, {}, {"page": 17}), (-2, {}, {"max_len": 500}), (-5, {"k": 8}, {}), (-5, {"v": 8}, {}), (-5, {"ko": 8}, {}), (-5, {"vo": 8}, {})], ids=str)
+def test_evict_refuses(code, call, changes):
+    assert evict(fq._lib, None if changes is None else batch(**changes), **call) == code
+    assert "fq_cache_evict" in fq.fq_last_error()
+
+
+def test_device_calls_refuse_host_tensors():
+    import torch
+
+    b = fq.PagedBatch([1], [4], [[0]], 16, 1, device="cpu")
+    x, pool = torch.zeros(1, 256, dtype=torch.float16), torch.zeros(1, 2, 16, 128, dtype=torch.float16)
+    for call in (lambda: fq.fq_attn_paged(x, b, pool, pool), lambda: fq.fq_qk_norm_rope(x, x, x, b, x, pool, pool),
+                 lambda: fq.fq_cache_evict(b, x, pool, pool, x, 4, 2)):
+        with pytest.raises(TypeError):
+            call()
+
+
+def test_reference_attention_of_equal_keys_is_the_mean():
+    V = np.arange(2 * 5 * 128, dtype=np.float64).reshape(2, 5, 128)
+    out, lse, sums, mass, _ = paged_ref.attention(np.ones((3, 4 * 128)), np.zeros((2, 5, 128)), V, 3, 0.5)
+    for i, seen in enumerate((3, 4, 5)):
+        assert np.allclose(out[i].reshape(4, 128), np.repeat(V[:, :seen].mean(1), 2, axis=0)) and np.allclose(lse[i], np.log(seen))
+    assert np.allclose(sums.sum(1), 6) and np.allclose(sums[:, 4], 2 / 5) and np.allclose(mass, out)
+    # more tokens than positions: the first ones see nothing
+    out, lse, sums, _, _ = paged_ref.attention(np.ones((3, 256)), np.zeros((2, 1, 128)), V[:, :1], 3, 1.0)
+    assert (out[:2] == 0).all() and np.isneginf(lse[:2]).all() and np.allclose(lse[2], 0) and np.allclose(sums, 1)
+
+
+def test_reference_eviction():
+    w = np.array([3.0, 1.0, 3.0, np.nan, 0.0, 2.0, 9.0])
+    assert paged_ref.evict(w, 4, 2).tolist() == [0, 3, 5, 6]
+    assert paged_ref.evict(w, 5, 2).tolist() == [0, 2, 3, 5, 6]
+    assert paged_ref.evict(w, 9, 2).tolist() == list(range(7))
+    assert paged_ref.evict(w, 3, 3).tolist() == [4, 5, 6]
+    assert paged_ref.evict(w, 2, 0).tolist() == [3, 6]
+    assert paged_ref.evict(w[:0], 2, 0).tolist() == []
