@@ -234,6 +234,252 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     }
 }
 
+// ------------------------------------------------- tiles of 64 and 128 rows
+// Chunks.  Four wavefronts, 32 rows each (KS = 1), or two by two with every key tile of 64 positions halved between them (KS = 2: 64 rows).
+// Keys and values go through double-buffered LDS tiles, keys straight from memory, values through registers (the compiler keeps
+// track of only a few copies into LDS, and waits for all of them at once beyond those).  32x32x16 MFMAs: a lane has 32 scores of one row, so
+// half as many reads of LDS per product as with sixteen rows, and one step across lanes for a row's maximum.
+constexpr int KT = 64; // positions of a tile
+
+constexpr int tile_rows_of(int KS) { return 128 / KS; }
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f16v mfma32x32x16(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ float other_half(float x, float (*f)(float, float))
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a = r[0], b = r[1]; // values of their own: a bit cast of a vector's element reads its first one
+    return f(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+
+template <int KS>
+__global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p)
+{
+    constexpr int TR = tile_rows_of(KS), KB = 2 / KS; // KB: blocks of 32 positions that a wavefront has of a tile
+    // Key tiles: chunk ch (eight dimensions) of row r at ch ^ (r % 16); value tiles: at ch ^ 4 (r % 4), for the transposing reads of eight rows by
+    // four chunks.  Separate arrays, named statically in a loop unrolled by two: the tile being read is then known not to be the one
+    // that copies in flight write.
+    __shared__ h8 Ks0[KT * 16], Ks1[KT * 16];
+    __shared__ h8 Vs0[KT * 16], Vs1[KT * 16];
+
+    // Longest tiles first, dealt from both ends: workgroups b and b + half share a CU when there are two a CU.
+    const int jobs = (int)gridDim.x, half = (jobs + 1) >> 1, bidx = (int)blockIdx.x;
+    const int job = bidx < half ? bidx : jobs - 1 - (bidx - half);
+    const int kvh = job % p.kv_heads, split = blockIdx.y;
+    const RowTile tile = find_tile<TR>(p, p.tiles - 1 - job / p.kv_heads);
+    if (tile.rows < 0)
+        return;
+    const int begin = split * p.chunk, end = min(tile.seen, begin + p.chunk);
+    if (begin >= end && split > 0)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, h = lane >> 5;
+    const int kpart = wave % KS, qpart = wave / KS;
+    const int row0 = tile.row0 + 32 * qpart; // first row of the wavefront
+    const int row = row0 + col, rowc = min(row, tile.rows - 1), token = rowc / p.group, head = kvh * p.group + rowc - token * p.group;
+    const int older = tile.s.len - tile.s.n;                       // positions ahead of the tokens; may be negative
+    const int seen = min(older + token + 1, tile.s.len);           // positions this lane's row sees
+    const int all_seen = older + min(row0, tile.rows - 1) / p.group + 1; // ... that every row of the wavefront sees
+    const int any_seen = older + min(row0 + 31, tile.rows - 1) / p.group + 1;
+
+    h8 qb[8];
+    {
+        const _Float16 *src = p.q + (size_t)(tile.s.first + token) * p.ldq + head * PD + 8 * h;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            qb[s] = *reinterpret_cast<const h8 *>(src + 16 * s);
+    }
+
+    typedef const __attribute__((address_space(4))) int *const_table; // read through the scalar cache; nothing writes it here
+    const const_table table = (const_table)(p.s.table + (size_t)tile.b * p.s.table_stride);
+    const int last_block = max(end - 1, 0) & ~15, tiles = (end - begin + KT - 1) / KT;
+    const int krow = 4 * wave + (lane >> 4); // the lane's row of every block of sixteen that it copies
+    const uint32_t koff = (uint32_t)(krow * 256 + (((lane & 15) ^ krow) << 4)), voff = (uint32_t)(krow * 256 + ((lane & 15) << 4));
+    int pg[4];
+    auto load_pages = [&](int jt) { // blocks behind the last one repeat it
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            pg[i] = table[min(begin + KT * jt + 16 * i, last_block) >> p.s.page_log2];
+    };
+    h8 vreg[4];
+    auto load_tiles = [&](h8 *Kdst, int jt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = min(begin + KT * jt + 16 * i, last_block), page = min(max(pg[i], 0), p.s.pages - 1);
+            const size_t at = (((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * 256;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(reinterpret_cast<const char *>(p.k) + at, 4096), &Kdst[64 * (wave + 4 * i)], 16, koff,
+                                                     0, 0, 0);
+            vreg[i] = __builtin_bit_cast(h8, buf_load_b128(make_rsrc(reinterpret_cast<const char *>(p.v) + at, 4096), voff, 0));
+        }
+        load_pages(jt + 1);
+    };
+    const int vdst = krow * 16 + ((lane & 15) ^ (4 * (lane >> 4)));
+    auto store_values = [&](h8 *Vdst, int jt) {
+        if (begin + KT * jt + KT > end) { // positions that nobody sees may hold anything, and 0 * NaN is NaN
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (begin + KT * jt + 16 * i + krow >= end)
+                    vreg[i] = h8{};
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            Vdst[256 * i + vdst] = vreg[i];
+    };
+
+    f16v acc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        acc[i] = f16v{};
+    float mx = -INFINITY, l = 0.f;
+    // byte offsets of the lane's operands in a tile: its key row, and its part of the transposing reads
+    const int kat = (32 * KB * kpart + col) * 256 + ((h ^ (lane & 15)) << 4);
+    const int vat = (32 * KB * kpart + 4 * h + ((lane & 15) >> 2)) * 256 + (((lane & 15) >> 2) << 6) + ((lane & 16) << 1) + ((lane & 3) << 3);
+
+    if (tiles > 0) {
+        load_pages(0);
+        load_tiles(Ks0, 0);
+        store_values(Vs0, 0);
+    }
+    __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
+    __syncthreads();
+
+    auto tile_step = [&](int jt, auto parity) {
+        constexpr int PAR = decltype(parity)::value;
+        const char *const Kcur = reinterpret_cast<const char *>(PAR ? Ks1 : Ks0), *const Vcur = reinterpret_cast<const char *>(PAR ? Vs1 : Vs0);
+        if (jt + 1 < tiles)
+            load_tiles(PAR ? Ks0 : Ks1, jt + 1);
+        const int first = begin + KT * jt + 32 * KB * kpart; // first position of the wavefront's part
+        if (first < min(any_seen, end)) {
+            f16v st[KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                st[kb] = f16v{};
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    st[kb] = mfma32x32x16(*reinterpret_cast<const h8 *>(Kcur + ((kat ^ (s << 5)) + 8192 * kb)), qb[s], st[kb]);
+            }
+            if (first + 32 * KB > all_seen || first + 32 * KB > end) { // uniform per wavefront
+                const int limit = min(seen, end) - first - 4 * h;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        st[kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) < limit ? st[kb][v] : -INFINITY;
+            }
+            float top = st[0][0];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    top = fmaxf(top, st[kb][v]);
+            top = other_half(top, larger) * p.scale;
+            // The reference that exponentials are taken from follows the maximum once that is 2^8 above it: weights up to 256 are as good in
+            // fp16 as those up to 1, and the outputs are rescaled that much less often.
+            if (__builtin_amdgcn_ballot_w64(top > mx + 8.f) != 0) {
+                const float mnew = fmaxf(mx, top);
+                const float alpha = __builtin_amdgcn_exp2f(mx - (mnew == -INFINITY ? 0.f : mnew));
+                mx = mnew;
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[i] *= alpha;
+            }
+            const float mref = mx == -INFINITY ? 0.f : mx;
+            float sum = 0.f;
+            h8 pb[KB][2];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(st[kb][v], p.scale, -mref));
+                    sum += e;
+                    pb[kb][v >> 3][v & 7] = (_Float16)e;
+                }
+            l += sum;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        const char *at = Vcur + ((vat ^ (db << 6)) + 8192 * kb + 4096 * j);
+                        const h4 lo = lds_column(reinterpret_cast<const _Float16 *>(at)), hi = lds_column(reinterpret_cast<const _Float16 *>(at + 2048));
+                        acc[db] = mfma32x32x16(h8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pb[kb][j], acc[db]);
+                    }
+        }
+        if (jt + 1 < tiles)
+            store_values(PAR ? Vs0 : Vs1, jt + 1); // last read in the previous step, before its barrier
+        __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
+        __syncthreads();
+    };
+    int jt = 0;
+    for (; jt + 1 < tiles; jt += 2) {
+        tile_step(jt, std::integral_constant<int, 0>{});
+        tile_step(jt + 1, std::integral_constant<int, 1>{});
+    }
+    if (jt < tiles)
+        tile_step(jt, std::integral_constant<int, 0>{});
+    l = other_half(l, add);
+
+    if constexpr (KS == 2) { // both halves meet in LDS, in the wavefront of the first
+        f4 *const acc_at = reinterpret_cast<f4 *>(qpart == 0 ? Ks0 : Ks1);
+        float *const row_at = reinterpret_cast<float *>(Vs0) + 128 * qpart;
+        if (kpart == 1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                acc_at[64 * i + lane] = f4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
+            row_at[lane] = mx;
+            row_at[64 + lane] = l;
+        }
+        __syncthreads();
+        if (kpart == 1)
+            return;
+        const float m2 = row_at[lane], l2 = row_at[64 + lane];
+        const float mnew = fmaxf(mx, m2), mref = mnew == -INFINITY ? 0.f : mnew;
+        const float s1 = __builtin_amdgcn_exp2f(mx - mref), s2 = __builtin_amdgcn_exp2f(m2 - mref);
+        mx = mnew;
+        l = l * s1 + l2 * s2;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const f4 o = acc_at[64 * i + lane];
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                acc[i >> 2][4 * (i & 3) + v] = acc[i >> 2][4 * (i & 3) + v] * s1 + o[v] * s2;
+        }
+    }
+    if (row >= tile.rows)
+        return;
+    const bool only = p.splits == 1 || tile.seen <= p.chunk;
+    const size_t at = (size_t)(tile.s.first + token) * p.heads + head;
+    if (only) {
+        const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l); // a row that sees nothing: zeros; NaN stays
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const h4 o = {(_Float16)(acc[i >> 2][4 * (i & 3)] * inv), (_Float16)(acc[i >> 2][4 * (i & 3) + 1] * inv),
+                          (_Float16)(acc[i >> 2][4 * (i & 3) + 2] * inv), (_Float16)(acc[i >> 2][4 * (i & 3) + 3] * inv)};
+            *reinterpret_cast<h4 *>(p.out + at * PD + 8 * i + 4 * h) = o;
+        }
+        if (h == 0 && p.lse)
+            p.lse[at] = (mx + log2f(l)) * LN2; // log2(0) is -inf
+    } else {
+        const size_t part = ((size_t)split * p.s.tokens + tile.s.first + token) * p.heads + head;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            *reinterpret_cast<f4 *>(p.part_o + part * PD + 8 * i + 4 * h) =
+                f4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
+        if (h == 0) {
+            p.part_ml[2 * part] = mx;
+            p.part_ml[2 * part + 1] = l;
+        }
+    }
+}
+
 // Joins the splits of a row: one wavefront each, two dimensions a lane.  Rows of tiles that one split has served are done already.
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedAttnArgs p, int tile_rows)
 {
@@ -332,31 +578,32 @@ __global__ __launch_bounds__(256, 2) void attn_paged_weights_kernel(PagedAttnArg
     }
 }
 
-// Splits of the positions: as many as bring a few workgroups to every CU, none shorter than 256 positions.
+// How a call is divided: tiles of 16 rows (a wavefront's own way through LDS), 64 or 128, and the positions into splits, as many as bring two
+// workgroups to every CU, none shorter than 256 positions.
 struct SplitPlan {
-    int tiles, splits, chunk;
+    int rows, tiles, splits, chunk;
 };
 
 SplitPlan plan_splits(const fq_paged_batch &b, int heads, int kv_heads)
 {
     SplitPlan s;
     const int group = heads / kv_heads;
-    // tiles of all sequences: at most one of each sequence is not full
-    const long long rows = (long long)b.tokens * group, full = rows / FEW + (b.seqs < rows ? b.seqs : rows);
-    const long long most = (long long)b.seqs * (((long long)b.max_q * group + FEW - 1) / FEW);
-    s.tiles = (int)(full < most ? full : most);
+    const long long rows = (long long)b.tokens * group, longest = (long long)b.max_q * group;
+    const auto tiles = [&](int height) { // of all sequences: at most one of each is not full
+        const long long full = rows / height + (b.seqs < rows ? b.seqs : rows), most = b.seqs * ((longest + height - 1) / height);
+        return full < most ? full : most;
+    };
+    s.rows = longest <= FEW ? FEW : (tiles(128) * kv_heads >= 512 ? 128 : 64);
+    s.tiles = (int)tiles(s.rows);
     const long long jobs = (long long)s.tiles * kv_heads;
-    long long splits = jobs > 0 ? 1024 / jobs : 1;
-    const long long longest = (b.max_len + 255) / 256;
-    splits = splits < 1 ? 1 : (splits > longest ? longest : splits);
-    if (splits < 1)
-        splits = 1;
+    long long splits = jobs > 0 ? (s.rows == FEW ? 1024 : 512) / jobs : 1;
+    const long long shortest = (b.max_len + 255) / 256;
+    splits = splits > shortest ? shortest : splits;
+    splits = splits < 1 ? 1 : splits;
     s.chunk = (int)((b.max_len + splits - 1) / splits + 127) / 128 * 128;
-    if (s.chunk < 128)
-        s.chunk = 128;
+    s.chunk = s.chunk < 128 ? 128 : s.chunk;
     s.splits = (b.max_len + s.chunk - 1) / s.chunk;
-    if (s.splits < 1)
-        s.splits = 1;
+    s.splits = s.splits < 1 ? 1 : s.splits;
     return s;
 }
 
@@ -395,12 +642,18 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     a.tiles = s.tiles;
     a.weights_stride = weights_stride;
     if (b.tokens > 0) {
-        hipLaunchKernelGGL(attn_paged_few_kernel, dim3(s.tiles * kv_heads, s.splits), dim3(256), 0, st, a);
+        const dim3 grid(s.tiles * kv_heads, s.splits);
+        if (s.rows == FEW)
+            hipLaunchKernelGGL(attn_paged_few_kernel, grid, dim3(256), 0, st, a);
+        else if (s.rows == 64)
+            hipLaunchKernelGGL(attn_paged_tile_kernel<2>, grid, dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL(attn_paged_tile_kernel<1>, grid, dim3(256), 0, st, a);
         int rc = (int)hipGetLastError();
         if (rc != 0)
             return rc;
         if (s.splits > 1) {
-            hipLaunchKernelGGL(attn_paged_merge_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, FEW);
+            hipLaunchKernelGGL(attn_paged_merge_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
             if ((rc = (int)hipGetLastError()) != 0)
                 return rc;
         }

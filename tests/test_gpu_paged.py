@@ -146,6 +146,12 @@ def test_ragged_batches(fq, torch, heads, kv, page):
     run(fq, torch, rng, [(1, 40), (0, 77), (70, 70), (1, 300), (0, 0), (5, 3), (19, 140), (3, 0), (1, 1), (40, 290), (130, 131)], heads, kv, page)
 
 
+@pytest.mark.parametrize("seqs", [[(129, 129)] * 8 + [(140, 300)] * 8, [(1, 50), (300, 300), (257, 400), (0, 9), (128, 128), (2, 1)] * 5], ids=["even", "odd"])
+def test_tall_tiles(fq, torch, seqs):
+    """Enough rows for the highest tiles."""
+    run(fq, torch, np.random.default_rng(47), seqs, 16, 16, 64)
+
+
 def test_many_sequences(fq, torch):
     """More sequences than a wavefront has lanes; some without tokens."""
     rng = np.random.default_rng(3)
