@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeArgs p)
 
 // ------------------------------------------------------------------- eviction
 // Of a head's len positions the last `recent` stay, and of the others the keep - recent that weigh most (equal weights: the lower
-// position).  Selecting kernel, one workgroup per (sequence, head): the weight that the last one kept has is found eight bits at a
+// position).  Selecting kernel, one workgroup per (sequence, head): the weight that the last one kept has is found eleven bits at a
 // time (radix selection over keys that order like the weights), then one pass in order numbers what stays.
 struct EvictArgs {
     PagedSeqs s;
@@ -84,7 +84,8 @@ struct EvictArgs {
     int kv_heads, weights_stride, weights_out_stride, keep, recent, dst_stride, dst_pages;
 };
 
-constexpr int SEL = 1024;
+constexpr int SEL = 1024, HELD = 16;             // threads; weights a thread keeps in registers: 16384 positions are read once
+constexpr int DIGIT = 11, DIGITS = 1 << DIGIT; // three digits of a key, the last of ten bits
 
 // Larger weight, larger key; -0 and 0 alike; NaN above everything, as it says nothing against its position.
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -95,11 +96,25 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Sum over the lanes up to this one: inside rows of sixteen lanes, then row ends handed on.
+__device__ __forceinline__ int lanes_upto(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false); // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false); // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false); // row_bcast:31 into rows 2 and 3
+    return v;
+}
+
 __global__ __launch_bounds__(SEL) void evict_select_kernel(EvictArgs p)
 {
-    __shared__ int hist[256];
-    __shared__ int found[2];
-    __shared__ int wave_gt[SEL / 64], wave_eq[SEL / 64];
+    constexpr int WAVES = SEL / 64;
+    __shared__ int hist[DIGITS];
+    __shared__ __align__(16) int wave_sum[WAVES];
+    __shared__ int found[3];
+    __shared__ uint32_t counts[HELD * WAVES]; // of a trip and wavefront: keys above the last one kept, equal ones in the upper half
     const int head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int len = min(max(p.s.seq_len[b], 0), p.s.max_len);
     const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
@@ -108,69 +123,125 @@ __global__ __launch_bounds__(SEL) void evict_select_kernel(EvictArgs p)
     float *wo = p.weights_out ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
     if (head == 0 && tid == 0)
         p.new_len[b] = m;
+    float held[HELD];
+    uint32_t key[HELD];
+    auto load = [&](int t0) { // trips behind the last position are left out here and below (uniform)
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (t0 + SEL * i < len)
+                held[i] = w[min(t0 + SEL * i + tid, len - 1)];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (t0 + SEL * i < len)
+                key[i] = weight_key(held[i]);
+    };
+    const bool once = len <= HELD * SEL; // uniform: the weights are read once
+    if (once)
+        load(0);
+    const bool all = need >= old, none = need <= 0;
     uint32_t prefix = 0;
     int left = need; // how many of the keys that match the prefix so far are kept
-    if (need > 0 && need < old) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256)
-                hist[tid] = 0;
+    if (!all && !none) {
+        for (int shift = 32 - DIGIT; shift > -DIGIT; shift -= DIGIT) { // 21, 10, and the last ten bits
+            const int low = max(shift, 0), bits = DIGIT + min(shift, 0);
+            for (int d = tid; d < DIGITS; d += SEL)
+                hist[d] = 0;
             __syncthreads();
-            const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-            for (int t = tid; t < old; t += SEL) {
-                const uint32_t key = weight_key(w[t]);
-                if ((key & mask) == prefix)
-                    atomicAdd(&hist[(key >> shift) & 255], 1);
+            const uint32_t mask = low + bits == 32 ? 0u : 0xffffffffu << (low + bits);
+            for (int t0 = 0; t0 < old; t0 += HELD * SEL) {
+                if (!once)
+                    load(t0);
+#pragma unroll
+                for (int i = 0; i < HELD; ++i)
+                    if (t0 + SEL * i < old) {
+                        if (t0 + SEL * i + tid < old && (key[i] & mask) == prefix)
+                            atomicAdd(&hist[(key[i] >> low) & ((1u << bits) - 1)], 1);
+                    }
             }
             __syncthreads();
-            if (tid < 256) {
-                int above = 0;
-                for (int d = tid + 1; d < 256; ++d)
-                    above += hist[d];
-                if (above < left && left <= above + hist[tid]) { // one thread
-                    found[0] = tid;
-                    found[1] = left - above;
-                }
+            // thread: two digits, from the highest down; keys of higher digits than these by a scan of the workgroup
+            const int d0 = DIGITS - 1 - 2 * tid, h0 = hist[d0], h1 = hist[d0 - 1];
+            const int upto = lanes_upto(h0 + h1);
+            if (lane == 63)
+                wave_sum[wave] = upto;
+            __syncthreads();
+            int above = upto - h0 - h1;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i)
+                above += i < wave ? wave_sum[i] : 0;
+            if (above < left && left <= above + h0) { // one thread and digit
+                found[0] = d0;
+                found[1] = left - above;
+                found[2] = h0;
+            } else if (above + h0 < left && left <= above + h0 + h1) {
+                found[0] = d0 - 1;
+                found[1] = left - above - h0;
+                found[2] = h1;
             }
             __syncthreads();
-            prefix |= (uint32_t)found[0] << shift;
+            prefix |= (uint32_t)found[0] << low;
             left = found[1];
-            __syncthreads();
+            if (left == found[2]) { // all of them: what is at least this prefix stays (and not everything does, so the prefix is not 0)
+                prefix -= 1;
+                left = 0;
+                break;
+            }
         }
     }
     // in order: a key above the last one kept stays, equal ones while they last
-    const bool all = need >= old, none = need <= 0;
     int gt_before = 0, eq_before = 0;
-    for (int t0 = 0; t0 < len; t0 += SEL) {
-        const int t = t0 + tid;
-        const float weight = t < len ? w[t] : 0.f;
-        const uint32_t key = weight_key(weight);
-        const bool gt = t < len && (t >= old || all || (!none && key > prefix));
-        const bool eq = t < old && !all && !none && key == prefix;
-        const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
-        if (lane == 0) {
-            wave_gt[wave] = (int)__popcll(gts);
-            wave_eq[wave] = (int)__popcll(eqs);
+    for (int t0 = 0; t0 < len; t0 += HELD * SEL) {
+        if (!once)
+            load(t0);
+        unsigned long long gts[HELD], eqs[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const int t = t0 + SEL * i + tid;
+            gts[i] = eqs[i] = 0;
+            if (t0 + SEL * i < len) {
+                gts[i] = __builtin_amdgcn_ballot_w64(t < len && (t >= old || all || (!none && key[i] > prefix)));
+                eqs[i] = __builtin_amdgcn_ballot_w64(t < old && !all && !none && key[i] == prefix);
+            }
+            if (lane == 0)
+                counts[WAVES * i + wave] = (uint32_t)__popcll(gts[i]) | (uint32_t)__popcll(eqs[i]) << 16;
         }
         __syncthreads();
-        int g = gt_before, e = eq_before;
-        for (int i = 0; i < SEL / 64; ++i) {
-            if (i == wave) {
-                const unsigned long long lower = (1ull << lane) - 1;
-                const int ge = g + (int)__popcll(gts & lower), ee = e + (int)__popcll(eqs & lower);
-                if (gt || (eq && ee < left)) {
-                    const int at = ge + min(ee, left);
-                    if (at < m) {
-                        kept[at] = t;
-                        if (wo)
-                            wo[at] = weight;
-                    }
-                }
+        if (tid < 64) { // sums ahead of every entry: four a lane, over the trips' wavefronts in order
+            static_assert(HELD * WAVES == 256 && HELD * SEL < 65536, "four entries a lane, sixteen bits a sum");
+            uint32_t c[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = counts[4 * lane + i];
+                sum += c[i];
             }
-            g += wave_gt[i];
-            e += wave_eq[i];
+            uint32_t ahead = (uint32_t)lanes_upto((int)sum) - sum;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                counts[4 * lane + i] = ahead;
+                ahead += c[i];
+            }
+            if (lane == 63)
+                found[0] = (int)ahead;
         }
-        gt_before = g;
-        eq_before = e;
+        __syncthreads();
+        const unsigned long long lower = (1ull << lane) - 1;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            if (t0 + SEL * i >= len)
+                continue;
+            const uint32_t ahead = counts[WAVES * i + wave];
+            const int gt = gt_before + (int)(ahead & 0xffffu) + (int)__popcll(gts[i] & lower);
+            const int eq = eq_before + (int)(ahead >> 16) + (int)__popcll(eqs[i] & lower);
+            const bool is_gt = gts[i] >> lane & 1, is_eq = eqs[i] >> lane & 1;
+            const int at = gt + min(eq, left);
+            if ((is_gt || (is_eq && eq < left)) && at < m) {
+                kept[at] = t0 + SEL * i + tid;
+                if (wo)
+                    wo[at] = held[i];
+            }
+        }
+        gt_before += found[0] & 0xffff;
+        eq_before += (int)((uint32_t)found[0] >> 16);
         __syncthreads();
     }
     for (int t = m + tid; t < p.keep; t += SEL)
