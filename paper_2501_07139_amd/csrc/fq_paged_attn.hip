@@ -24,8 +24,9 @@ struct PagedAttnArgs {
     float *part_o, *part_ml;  // [splits][tokens][heads][128], [..][2]: unnormalised output; maximum (in powers of 2) and sum
     const float *weights;     // [seqs][kv_heads][weights_stride], or NULL: zeros
     float *weights_out;
+    float *scores;            // [tokens][heads][scores_stride]: scaled scores of sequences of few rows
     float scale;              // times log2(e): scores are powers of 2
-    int ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride;
+    int scores_stride, ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride;
 };
 
 // A tile of rows of one sequence and key/value head.
@@ -68,6 +69,7 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile)
     return r;
 }
 
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 
 // Four halves of one column from four consecutive rows: lane j of sixteen names the 8 bytes of row j / 4, columns 4 (j % 4)... of a
@@ -77,34 +79,39 @@ __device__ __forceinline__ h4 lds_column(const _Float16 *at)
     return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v *)(at)));
 }
 
-// ------------------------------------------------- up to sixteen rows a tile
-// Four wavefronts, 32 positions of every 128 each: keys straight into registers as MFMA operands, values through a part of LDS of the
-// wavefront's own (no barrier in the loop), and one merge of the four at the end.  Bound by the read of the cache.
+// ------------------------------------------------- up to sixteen rows a sequence
+// Single tokens: one tile a sequence and head.  Four wavefronts, 32 positions of every 128 each: keys straight into registers as MFMA
+// operands, values through a part of LDS of the wavefront's own (no barrier in the loop), and one merge of the four at the end.  Bound by the read
+// of the cache.  With SCORES the scaled scores of every row are left for the column sums, which need the sum over all splits first.
 constexpr int FEW = 16;
 
+typedef const __attribute__((address_space(4))) int *const_ints; // read through the scalar cache; nothing writes them in these kernels
+
+template <bool SCORES>
 __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
 {
     // values of a step: 32 rows of 16 chunks of eight, chunk ch of row r at ch ^ 2 (r % 8), so that the transposing read of sixteen rows by
     // two chunks meets every bank twice; afterwards the wavefronts' outputs
     __shared__ h8 Vs[4][32 * 16];
     __shared__ float ms[4][FEW], ls[4][FEW];
-    const int kvh = blockIdx.x % p.kv_heads, split = blockIdx.y;
-    const RowTile tile = find_tile<FEW>(p, blockIdx.x / p.kv_heads);
-    if (tile.rows < 0)
-        return;
-    const int begin = split * p.chunk, end = min(tile.seen, begin + p.chunk);
-    if (begin >= end && split > 0)
-        return;
+    const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.x / p.kv_heads, split = blockIdx.y, begin = split * p.chunk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // The pages of 64 blocks of sixteen positions, a lane each, asked for together with the lengths: one wait less ahead of the cache.
+    const int *table = p.s.table + (size_t)b * p.s.table_stride;
+    const auto block_pages = [&](int t) { return table[min(((t >> 4) + lane) >> (p.s.page_log2 - 4), p.s.table_stride - 1)]; };
+    int pages = block_pages(begin);
+    const int q0 = ((const_ints)p.s.q_start)[b], q1 = ((const_ints)p.s.q_start)[b + 1], len = min(max(((const_ints)p.s.seq_len)[b], 0), p.s.max_len);
+    const int first = min(max(q0, 0), p.s.tokens), n = min(max(q1, first), p.s.tokens) - first, rows = min(n * p.group, FEW);
+    const int end = min(len, begin + p.chunk);
+    if (rows == 0 || (begin >= end && split > 0))
+        return;
     const int col = lane & 15, g = lane >> 4;
-    const int row = tile.row0 + col, token = min(row, tile.rows - 1) / p.group;
-    const int head = kvh * p.group + min(row, tile.rows - 1) - token * p.group;
-    const int seen = min(tile.s.len - tile.s.n + token + 1, tile.s.len); // positions this lane's row sees; may be negative
-    const int all_seen = max(tile.s.len - tile.s.n + tile.row0 / p.group + 1, 0); // ... that every row of the tile sees
+    const int token = min(col, rows - 1) / p.group, head = kvh * p.group + min(col, rows - 1) - token * p.group;
+    const int seen = len - n + token + 1, all_seen = len - n + 1; // positions this lane's row sees; ... that every row sees; may be negative
 
     h8 qb[4];
     {
-        const _Float16 *src = p.q + (size_t)(tile.s.first + token) * p.ldq + head * PD + 8 * g;
+        const _Float16 *src = p.q + (size_t)(first + token) * p.ldq + head * PD + 8 * g;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
             qb[s] = *reinterpret_cast<const h8 *>(src + 32 * s);
@@ -119,68 +126,87 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     // the lane's part of the transposing reads: rows 4g + col / 4 of a block of sixteen, columns 4 (col % 4)
     const int vrow = 4 * g + (col >> 2);
     const int vbase = vrow * 256 + ((vrow & 7) << 5) + ((col & 3) << 3);
+    float *scores = nullptr;
+    if constexpr (SCORES)
+        scores = p.scores + ((size_t)(first + token) * p.heads + head) * p.scores_stride + 4 * g;
     for (int t0 = begin + 32 * wave; t0 < end; t0 += 128) {
+        const int block = (t0 - begin) >> 4; // of the split
+        if ((block & 63) < 8 && block >= 64) // the wavefront's first step among the next 64 blocks
+            pages = block_pages(begin + 16 * (block & ~63));
         h8 kk[2][4], vv[2][4];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const size_t at = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, tile.b, t0 + 16 * b) * PD;
+        for (int i = 0; i < 2; ++i) {
+            const int page = min(max(__builtin_amdgcn_readlane(pages, (block + i) & 63), 0), p.s.pages - 1);
+            const size_t at = ((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)((t0 + 16 * i) & ((1 << p.s.page_log2) - 1))) * PD;
+            const _Float16 *k = p.k + at, *v = p.v + at;
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                kk[b][s] = *reinterpret_cast<const h8 *>(p.k + at + col * PD + 32 * s + 8 * g);
+                kk[i][s] = *reinterpret_cast<const h8 *>(k + (col * PD + 32 * s + 8 * g));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                vv[b][i] = *reinterpret_cast<const h8 *>(p.v + at + (4 * i + g) * PD + 8 * col);
-                if (t0 + 16 * b + 4 * i + g >= end) // rows that nobody sees may hold anything, and 0 * NaN is NaN
-                    vv[b][i] = h8{};
-            }
+            for (int s = 0; s < 4; ++s)
+                vv[i][s] = *reinterpret_cast<const h8 *>(v + ((4 * s + g) * PD + 8 * col));
         }
         f4 st[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            st[b] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 2; ++i) {
+            st[i] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                st[b] = mfma16x16x32(kk[b][s], qb[s], st[b]);
+                st[i] = mfma16x16x32(kk[i][s], qb[s], st[i]);
+            st[i] *= p.scale;
         }
-        const bool whole = t0 + 32 <= all_seen; // uniform
-        float top = -INFINITY;
+        if (t0 + 32 > min(all_seen, end)) { // uniform; rows that nobody sees may hold anything, and 0 * NaN is NaN
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float x = st[b][v] * p.scale;
-                st[b][v] = whole || t0 + 16 * b + 4 * g + v < seen ? x : -INFINITY;
-                top = fmaxf(top, st[b][v]);
+                for (int v = 0; v < 4; ++v) {
+                    st[i][v] = t0 + 16 * i + 4 * g + v < min(seen, end) ? st[i][v] : -INFINITY;
+                    if (t0 + 16 * i + 4 * v + g >= end)
+                        vv[i][v] = h8{};
+                }
+        }
+        if constexpr (SCORES) {
+            if (col < rows) {
+                *reinterpret_cast<f4 *>(scores + t0) = st[0];
+                *reinterpret_cast<f4 *>(scores + t0 + 16) = st[1];
             }
+        }
+        float top = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float mnew = fmaxf(mx, top), mref = mnew == -INFINITY ? 0.f : mnew;
-        const float alpha = __builtin_amdgcn_exp2f(mx - mref);
-        mx = mnew;
+        if (__builtin_amdgcn_ballot_w64(mnew != mx) != 0) { // some row's maximum moved
+            const float alpha = __builtin_amdgcn_exp2f(mx - mref);
+            mx = mnew;
+            l *= alpha;
+#pragma unroll
+            for (int db = 0; db < 8; ++db)
+                acc[db] *= alpha;
+        }
         h8 pb;
         float sum = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const float e = __builtin_amdgcn_exp2f(st[b][v] - mref);
+                const float e = __builtin_amdgcn_exp2f(st[i][v] - mref);
                 sum += e;
-                pb[4 * b + v] = (_Float16)e;
+                pb[4 * i + v] = (_Float16)e;
             }
-        l = l * alpha + sum;
+        l += sum;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 16 * b + 4 * i + g;
-                V[r * 16 + (col ^ (2 * (r & 7)))] = vv[b][i];
+            for (int s = 0; s < 4; ++s) {
+                const int r = 16 * i + 4 * s + g;
+                V[r * 16 + (col ^ (2 * (r & 7)))] = vv[i][s];
             }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
             const char *at = reinterpret_cast<const char *>(V) + (vbase ^ (db << 5));
             const h4 lo = lds_column(reinterpret_cast<const _Float16 *>(at)), hi = lds_column(reinterpret_cast<const _Float16 *>(at + 4096));
-            acc[db] = mfma16x16x32(h8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pb, acc[db] * alpha);
+            acc[db] = mfma16x16x32(h8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pb, acc[db]);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -196,6 +222,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         ls[wave][col] = l;
     }
     __syncthreads();
+    if (col >= rows)
+        return;
     // thread: row col, dimensions 16 db + 4 g of two db's
     const float m = fmaxf(fmaxf(ms[0][col], ms[1][col]), fmaxf(ms[2][col], ms[3][col])), mref = m == -INFINITY ? 0.f : m;
     float w[4], sum = 0.f;
@@ -204,11 +232,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         w[i] = __builtin_amdgcn_exp2f(ms[i][col] - mref);
         sum += w[i] * ls[i][col];
     }
-    if (row >= tile.rows)
-        return;
-    const bool only = p.splits == 1 || tile.seen <= p.chunk;
-    const size_t at = (size_t)(tile.s.first + token) * p.heads + head;
-    const size_t part = ((size_t)split * p.s.tokens + tile.s.first + token) * p.heads + head;
+    const bool only = len <= p.chunk; // no other split has any of it
+    const size_t at = (size_t)(first + token) * p.heads + head, part = (size_t)split * p.s.tokens * p.heads + at;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int db = 2 * wave + i;
@@ -296,8 +321,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
             qb[s] = *reinterpret_cast<const h8 *>(src + 16 * s);
     }
 
-    typedef const __attribute__((address_space(4))) int *const_table; // read through the scalar cache; nothing writes it here
-    const const_table table = (const_table)(p.s.table + (size_t)tile.b * p.s.table_stride);
+    const const_ints table = (const_ints)(p.s.table + (size_t)tile.b * p.s.table_stride);
     const int last_block = max(end - 1, 0) & ~15, tiles = (end - begin + KT - 1) / KT;
     const int krow = 4 * wave + (lane >> 4); // the lane's row of every block of sixteen that it copies
     const uint32_t koff = (uint32_t)(krow * 256 + (((lane & 15) ^ krow) << 4)), voff = (uint32_t)(krow * 256 + ((lane & 15) << 4));
@@ -480,11 +504,15 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     }
 }
 
-// Joins the splits of a row: one wavefront each, two dimensions a lane.  Rows of tiles that one split has served are done already.
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedAttnArgs p, int tile_rows)
+// Joins the splits of a row.  WAVES wavefronts each, which deal the splits among them; a wavefront takes 64 of its own at a time: a lane has one's
+// maximum and sum, then two dimensions of the outputs, eight loads at a time (those are what a row waits for: a token over 100003 positions, 196
+// splits of 32 rows, 9.5 us with four wavefronts).  Rows of tiles that one split has served are done already.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_kernel(PagedAttnArgs p, int tile_rows)
 {
-    const int lane = threadIdx.x & 63;
-    const int item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); // token * heads + head
+    __shared__ float sums[WAVES][PD + 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int item = WAVES > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave, part = WAVES > 1 ? wave : 0; // token * heads + head
     if (item >= p.s.tokens * p.heads)
         return;
     const int m = item / p.heads, head = item - m * p.heads;
@@ -498,16 +526,64 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedAttnArgs p, 
         return;
     const int live = (max(s.len - s.n + token + 1, 0) + p.chunk - 1) / p.chunk;
     const size_t stride = (size_t)p.s.tokens * p.heads;
-    const float *ml = p.part_ml + 2 * (size_t)item, *o = p.part_o + (size_t)item * PD + 2 * lane;
+    const f2 *ml = reinterpret_cast<const f2 *>(p.part_ml) + item, *o = reinterpret_cast<const f2 *>(p.part_o) + (size_t)item * (PD / 2) + lane;
     float mx = -INFINITY, l = 0.f, a0 = 0.f, a1 = 0.f;
-    for (int i = 0; i < live; ++i) {
-        const float m2 = ml[2 * i * stride], l2 = ml[2 * i * stride + 1];
-        const float mnew = fmaxf(mx, m2), mref = mnew == -INFINITY ? 0.f : mnew;
-        const float s1 = __builtin_amdgcn_exp2f(mx - mref), s2 = __builtin_amdgcn_exp2f(m2 - mref);
-        l = l * s1 + l2 * s2;
-        a0 = a0 * s1 + o[i * stride * PD] * s2;
-        a1 = a1 * s1 + o[i * stride * PD + 1] * s2;
+    const int mine_all = (live - part + WAVES - 1) / WAVES; // splits part, part + WAVES, ...
+    const auto at = [&](int i) { return (size_t)(part + WAVES * min(i, mine_all - 1)) * stride; };
+    for (int i0 = 0; i0 < mine_all; i0 += 64) {
+        const f2 mine = ml[at(i0 + lane)];
+        float top = i0 + lane < mine_all ? mine[0] : -INFINITY;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1)
+            top = fmaxf(top, __shfl_xor(top, d, 64));
+        const float mnew = fmaxf(mx, top), mref = mnew == -INFINITY ? 0.f : mnew;
+        const float w = i0 + lane < mine_all ? __builtin_amdgcn_exp2f(mine[0] - mref) : 0.f, alpha = __builtin_amdgcn_exp2f(mx - mref);
+        float sum = i0 + lane < mine_all ? w * mine[1] : 0.f;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1)
+            sum += __shfl_xor(sum, d, 64);
         mx = mnew;
+        l = l * alpha + sum;
+        a0 *= alpha;
+        a1 *= alpha;
+        const int count = min(64, mine_all - i0);
+        for (int i = 0; i < count; i += 8) {
+            f2 v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) // those past the last one repeat it, with a weight of zero
+                v[e] = o[at(i0 + i + e) * (PD / 2)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float we = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i + e));
+                if (i + e < count) {
+                    a0 = fmaf(we, v[e][0], a0);
+                    a1 = fmaf(we, v[e][1], a1);
+                }
+            }
+        }
+    }
+    if constexpr (WAVES > 1) {
+        sums[wave][2 * lane] = a0;
+        sums[wave][2 * lane + 1] = a1;
+        if (lane == 0) {
+            sums[wave][PD] = mx;
+            sums[wave][PD + 1] = l;
+        }
+        __syncthreads();
+        if (wave != 0)
+            return;
+        mx = sums[0][PD];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i)
+            mx = fmaxf(mx, sums[i][PD]);
+        l = a0 = a1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float w = __builtin_amdgcn_exp2f(sums[i][PD] - (mx == -INFINITY ? 0.f : mx));
+            l = fmaf(w, sums[i][PD + 1], l);
+            a0 = fmaf(w, sums[i][2 * lane], a0);
+            a1 = fmaf(w, sums[i][2 * lane + 1], a1);
+        }
     }
     const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
     *reinterpret_cast<h2 *>(p.out + (size_t)item * PD + 2 * lane) = h2{(_Float16)(a0 * inv), (_Float16)(a1 * inv)};
@@ -578,15 +654,53 @@ __global__ __launch_bounds__(256, 2) void attn_paged_weights_kernel(PagedAttnArg
     }
 }
 
-// How a call is divided: tiles of 16 rows (a wavefront's own way through LDS), 64 or 128, and the positions into splits, as many as bring two
-// workgroups to every CU, none shorter than 256 positions.
-struct SplitPlan {
+// The same where every sequence has at most sixteen rows: their scores are there already, and nothing is read twice but those.
+__global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnArgs p)
+{
+    constexpr int PER = 4; // positions a thread
+    const int kvh = blockIdx.x, b = blockIdx.z;
+    const SeqRange s = seq_range(p.s, b);
+    const int rows = min(s.n * p.group, FEW), t0 = blockIdx.y * (256 * PER) + threadIdx.x;
+    float sum[PER] = {};
+    for (int r = 0; r < rows; ++r) {
+        const size_t item = (size_t)(s.first + r / p.group) * p.heads + kvh * p.group + r % p.group;
+        const float lse = p.lse[item] * LOG2E;
+        if (lse == -INFINITY) // a row that sees nothing
+            continue;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (t0 + 256 * i < s.len)
+                sum[i] += __builtin_amdgcn_exp2f(p.scores[item * p.scores_stride + t0 + 256 * i] - lse);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int t = t0 + 256 * i;
+        if (t < s.len) {
+            const size_t at = ((size_t)b * p.kv_heads + kvh) * p.weights_stride + t;
+            p.weights_out[at] = (p.weights && t < s.len - s.n ? p.weights[at] : 0.f) + sum[i];
+        }
+    }
+}
+
+// How a call is divided: one tile of up to sixteen rows a sequence, or tiles of 64 or 128, and the positions into splits.
+//
+// Single tokens: a step of 128 positions takes a workgroup 1.15 us, of which most is the wait for memory, until about 100 workgroups together
+// reach the rate of HBM; joining splits takes 3 us more, the launch.  So one split where that is no longer than a short one and the join (384
+// positions, or 1024 where sequences and heads fill the chip), else splits as short as keep the workgroups at about 384, but no longer than 512 positions, as
+// sequences differ in length.  Measured (us at splits of 128 / 256 / 512 / 1024 positions): 32 heads, 1000 positions 8.6 / 9.9 / 12.7 / 14.2, 4000
+// 20 / 17.7 / 16.9 / 20.7; 8 heads, 8000 positions 15.8 / 12.8 / 14 / 19; 64 sequences of 8 heads, 700 positions 35 / 35 / 35 / 29 (one split); 64 of 17
+// to 4096 (with the join) 41.7 / 38.2 / 38.7 / 42.1.
+//
+// Chunks: as many splits as bring two workgroups to every CU, none shorter than 256 positions.
+struct AttnPlan {
     int rows, tiles, splits, chunk;
+    size_t part_o, part_ml, lse, scores, end; // offsets in the workspace, in floats
+    int scores_stride;
 };
 
-SplitPlan plan_splits(const fq_paged_batch &b, int heads, int kv_heads)
+AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weights)
 {
-    SplitPlan s;
+    AttnPlan s;
     const int group = heads / kv_heads;
     const long long rows = (long long)b.tokens * group, longest = (long long)b.max_q * group;
     const auto tiles = [&](int height) { // of all sequences: at most one of each is not full
@@ -594,16 +708,29 @@ SplitPlan plan_splits(const fq_paged_batch &b, int heads, int kv_heads)
         return full < most ? full : most;
     };
     s.rows = longest <= FEW ? FEW : (tiles(128) * kv_heads >= 512 ? 128 : 64);
-    s.tiles = (int)tiles(s.rows);
+    s.tiles = s.rows == FEW ? b.seqs : (int)tiles(s.rows);
     const long long jobs = (long long)s.tiles * kv_heads;
-    long long splits = jobs > 0 ? (s.rows == FEW ? 1024 : 512) / jobs : 1;
-    const long long shortest = (b.max_len + 255) / 256;
-    splits = splits > shortest ? shortest : splits;
-    splits = splits < 1 ? 1 : splits;
-    s.chunk = (int)((b.max_len + splits - 1) / splits + 127) / 128 * 128;
+    const auto pieces = [&](int chunk) { return jobs * ((b.max_len + chunk - 1) / chunk); };
+    if (s.rows == FEW) {
+        const bool one = b.max_len <= 384 || (b.max_len <= 1024 && jobs >= 128);
+        s.chunk = one ? (b.max_len + 127) / 128 * 128 : pieces(128) <= 384 ? 128 : pieces(256) <= 384 ? 256 : 512;
+    } else {
+        long long splits = jobs > 0 ? 512 / jobs : 1;
+        const long long shortest = (b.max_len + 255) / 256;
+        splits = splits > shortest ? shortest : splits;
+        splits = splits < 1 ? 1 : splits;
+        s.chunk = (int)((b.max_len + splits - 1) / splits + 127) / 128 * 128;
+    }
     s.chunk = s.chunk < 128 ? 128 : s.chunk;
     s.splits = (b.max_len + s.chunk - 1) / s.chunk;
     s.splits = s.splits < 1 ? 1 : s.splits;
+    const size_t items = (size_t)b.tokens * heads, parts = s.splits > 1 ? (size_t)s.splits * items : 0;
+    s.scores_stride = (b.max_len + 31) / 32 * 32;
+    s.scores = 0; // the parts of a multiple of four floats first
+    s.part_o = s.scores + (weights && s.rows == FEW ? items * s.scores_stride : 0);
+    s.part_ml = s.part_o + parts * PD;
+    s.lse = s.part_ml + parts * 2;
+    s.end = s.lse + (weights ? items : 0);
     return s;
 }
 
@@ -611,25 +738,25 @@ SplitPlan plan_splits(const fq_paged_batch &b, int heads, int kv_heads)
 
 size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights)
 {
-    const SplitPlan s = plan_splits(b, heads, kv_heads);
-    const size_t items = (size_t)b.tokens * heads;
-    return (s.splits > 1 ? (size_t)s.splits * items * (PD + 2) * sizeof(float) : 0) + (weights ? items * sizeof(float) : 0);
+    return plan_attn(b, heads, kv_heads, weights).end * sizeof(float);
 }
 
 int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int heads, int kv_heads, const void *k, const void *v, float scale,
                          void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st)
 {
-    const SplitPlan s = plan_splits(b, heads, kv_heads);
-    const size_t items = (size_t)b.tokens * heads;
+    const AttnPlan s = plan_attn(b, heads, kv_heads, weights_out != nullptr);
+    float *ws = static_cast<float *>(workspace);
     PagedAttnArgs a;
     a.s = paged_seqs(b);
     a.q = static_cast<const _Float16 *>(q);
     a.k = static_cast<const _Float16 *>(k);
     a.v = static_cast<const _Float16 *>(v);
     a.out = static_cast<_Float16 *>(out);
-    a.part_o = static_cast<float *>(workspace);
-    a.part_ml = a.part_o + (s.splits > 1 ? (size_t)s.splits * items * PD : 0);
-    a.lse = lse || !weights_out ? lse : a.part_ml + (s.splits > 1 ? (size_t)s.splits * items * 2 : 0);
+    a.part_o = ws + s.part_o;
+    a.part_ml = ws + s.part_ml;
+    a.lse = lse || !weights_out ? lse : ws + s.lse;
+    a.scores = ws + s.scores;
+    a.scores_stride = s.scores_stride;
     a.weights = weights;
     a.weights_out = weights_out;
     a.scale = scale * LOG2E;
@@ -643,8 +770,10 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     a.weights_stride = weights_stride;
     if (b.tokens > 0) {
         const dim3 grid(s.tiles * kv_heads, s.splits);
-        if (s.rows == FEW)
-            hipLaunchKernelGGL(attn_paged_few_kernel, grid, dim3(256), 0, st, a);
+        if (s.rows == FEW && weights_out)
+            hipLaunchKernelGGL(attn_paged_few_kernel<true>, grid, dim3(256), 0, st, a);
+        else if (s.rows == FEW)
+            hipLaunchKernelGGL(attn_paged_few_kernel<false>, grid, dim3(256), 0, st, a);
         else if (s.rows == 64)
             hipLaunchKernelGGL(attn_paged_tile_kernel<2>, grid, dim3(256), 0, st, a);
         else
@@ -653,12 +782,22 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
         if (rc != 0)
             return rc;
         if (s.splits > 1) {
-            hipLaunchKernelGGL(attn_paged_merge_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
+            const size_t items = (size_t)b.tokens * heads;
+            if (s.splits > 64) // more than a wavefront takes at once
+                hipLaunchKernelGGL(attn_paged_merge_kernel<16>, dim3((unsigned)items), dim3(1024), 0, st, a, s.rows);
+            else if (s.splits > 8) // more than one of its turns
+                hipLaunchKernelGGL(attn_paged_merge_kernel<4>, dim3((unsigned)items), dim3(256), 0, st, a, s.rows);
+            else
+                hipLaunchKernelGGL(attn_paged_merge_kernel<1>, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
             if ((rc = (int)hipGetLastError()) != 0)
                 return rc;
         }
     }
-    if (weights_out && b.max_len > 0)
-        hipLaunchKernelGGL(attn_paged_weights_kernel, dim3(kv_heads, (b.max_len + 63) / 64, b.seqs), dim3(256), 0, st, a);
+    if (weights_out && b.max_len > 0) {
+        if (s.rows == FEW)
+            hipLaunchKernelGGL(attn_paged_few_weights_kernel, dim3(kv_heads, (b.max_len + 1023) / 1024, b.seqs), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL(attn_paged_weights_kernel, dim3(kv_heads, (b.max_len + 63) / 64, b.seqs), dim3(256), 0, st, a);
+    }
     return (int)hipGetLastError();
 }
