@@ -124,7 +124,8 @@ def _load_bind():
         warnings.warn(f"{_PKG}/_bind is not built for this Python and torch ({e}): small calls take 1.7 us longer; "
                       "`python paper_2501_07139_amd/build.py` builds it", RuntimeWarning, stacklevel=2)
         return None
-    names = ("fq_qlinear_tile", "fq_qlinear_mixed", "fq_dense_f16", "fq_head_nll", "fq_token_nll", "fq_logit_l2")
+    names = ("fq_qlinear_tile", "fq_qlinear_mixed", "fq_dense_f16", "fq_head_nll", "fq_token_nll", "fq_logit_l2", "fq_qk_norm_rope",
+             "fq_attn_paged", "fq_cache_evict")
     _bind.bind(*(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
     return _bind
 
@@ -733,12 +734,19 @@ def _fresh(shape, dtype, device, stream):
 def fq_qk_norm_rope(q, k, v, batch: PagedBatch, rope, k_pages, v_pages, q_gain=None, k_gain=None, eps: float = 1e-5, out=None,
                     stream=None):
     """q, k, v fp16 [tokens, 128 heads] (rows may be columns of one product) -> rotated q; k and v go into the batch's slots."""
+    if _bind is not None and out is not None:
+        rc = _bind.qk_norm_rope(q, k, v, batch, rope, k_pages, v_pages, q_gain, k_gain, eps, out, stream)
+        if rc is not None:
+            _check(rc)
+            return out
     n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_qk_norm_rope")
     width = q.shape[-1]
     ld = [_rows(t, w, n) for t, w, n in ((q, width, "q"), (k, 128 * n_kv, "k"), (v, 128 * n_kv, "v"))]
     rope = _dev(rope, torch.float32, "rope")
     if width % 128 or any(t.shape[0] != batch.tokens for t in (q, k, v)):
         raise ValueError(f"fq_qk_norm_rope: q, k, v [{batch.tokens}, 128 heads]")
+    if any(_dev(t, torch.int32, n).numel() != batch.tokens for t, n in ((batch.positions, "positions"), (batch.slots, "slots"))):
+        raise ValueError(f"fq_qk_norm_rope: positions and slots [{batch.tokens}]")
     if rope.dim() != 3 or tuple(rope.shape[1:]) != (64, 2):
         raise ValueError("fq_qk_norm_rope: rope must be [positions, 64, 2]")
     for gain in (q_gain, k_gain):
@@ -766,6 +774,12 @@ def fq_attn_paged(q, batch: PagedBatch, k_pages, v_pages, scale: Optional[float]
 
     lse fp32 [tokens, heads] and weights_out fp32 [sequences, kv heads, >= positions of the longest] are written if given;
     weights (of that shape, may be weights_out) are added to what the positions receive."""
+    scale = 128 ** -0.5 if scale is None else scale
+    if _bind is not None and out is not None:
+        rc = _bind.attn_paged(q, batch, k_pages, v_pages, scale, out, lse, weights, weights_out, workspace, stream)
+        if rc is not None:
+            _check(rc)
+            return out
     n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_attn_paged")
     width = q.shape[-1]
     ldq = _rows(q, width, "q")
@@ -789,9 +803,9 @@ def fq_attn_paged(q, batch: PagedBatch, k_pages, v_pages, scale: Optional[float]
         nbytes = fq_attn_paged_workspace_bytes(batch, heads, n_kv, weights_out is not None)
         workspace = _fresh((nbytes,), torch.uint8, q.device, stream) if nbytes else None
     _same_device("fq_attn_paged", batch.device, q, k_pages, v_pages, out, lse, weights, weights_out, workspace)
-    _check(_lib.fq_attn_paged(batch.struct, _dp(q), ldq, heads, n_kv, _dp(k_pages), _dp(v_pages), 128 ** -0.5 if scale is None else scale,
-                              _dp(out), _dp(lse), _dp(weights), _dp(weights_out), wstride, _dp(workspace),
-                              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.fq_attn_paged(batch.struct, _dp(q), ldq, heads, n_kv, _dp(k_pages), _dp(v_pages), scale, _dp(out), _dp(lse), _dp(weights),
+                              _dp(weights_out), wstride, _dp(workspace), nbytes, _stream(stream)))
     return out
 
 
@@ -806,10 +820,15 @@ def fq_cache_evict(batch: PagedBatch, weights, k_pages, v_pages, dst_table, keep
     """Cut every sequence to `keep` positions a head, into the pages of dst_table (int32 [sequences, pages], device) of k_out, v_out (the
     same pools if not given).  Returns (kept int32 [sequences, kv heads, keep], new_len int32 [sequences]); weights_out fp32
     [sequences, kv heads, >= keep] takes the weights of what stays."""
-    n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_cache_evict")
     if (k_out is None) != (v_out is None):
         raise ValueError("fq_cache_evict: k_out and v_out go together")
     k_out, v_out = (k_pages, v_pages) if k_out is None else (k_out, v_out)
+    if _bind is not None and kept is not None and new_len is not None:
+        rc = _bind.cache_evict(batch, weights, k_pages, v_pages, dst_table, keep, recent, k_out, v_out, kept, new_len, weights_out, stream)
+        if rc is not None:
+            _check(rc)
+            return kept, new_len
+    n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_cache_evict")
     if _pools(batch, k_out, v_out, -1, "fq_cache_evict") != n_kv:
         raise ValueError("fq_cache_evict: k_out must have the heads of k_pages")
     _weights(weights, batch, n_kv, "weights")

@@ -495,3 +495,35 @@ def test_refusals(fq, torch):
         with pytest.raises(fq.FqError) as e:
             bad()
         assert e.value.code == code
+
+
+def test_both_ways_of_a_call(fq, torch, monkeypatch):
+    """Through the extension module and through ctypes: the same bits; the module takes the calls that allocate nothing."""
+    rng = np.random.default_rng(53)
+    seqs, heads, kv, page = [(1, 700), (1, 33)], 8, 2, 16
+    table, pages, k, v, q = case(rng, seqs, heads, kv, page)
+    b = fq.PagedBatch([1, 1], [700, 33], table, page, pages)
+    rope, dst = fq.rope_table(700), torch.arange(14, dtype=torch.int32, device="cuda").view(2, 7)
+    taken = []
+    for name in ("qk_norm_rope", "attn_paged", "cache_evict"):
+        def watch(*a, real=getattr(fq._bind, name), name=name):
+            rc = real(*a)
+            taken.append((name, rc))
+            return rc
+        monkeypatch.setattr(fq._bind, name, watch)
+    results = []
+    for module in (fq._bind, None):
+        monkeypatch.setattr(fq, "_bind", module)
+        x, y, z, dk, dv = (dev(torch, a) for a in (q, q[:, :256].copy(), q[:, 256:512].copy(), np.nan_to_num(k), np.nan_to_num(v)))
+        gain = dev(torch, rng.normal(size=128).astype(np.float16) if not results else results[0][0].cpu().numpy())
+        fq.fq_qk_norm_rope(x, y, z, b, rope, dk, dv, q_gain=gain, out=x)
+        out, lse, w = torch.empty_like(x), torch.empty(2, heads, device="cuda"), torch.zeros(2, kv, 700, device="cuda")
+        ws = torch.empty(fq.fq_attn_paged_workspace_bytes(b, heads, kv, True), dtype=torch.uint8, device="cuda")
+        fq.fq_attn_paged(x, b, dk, dv, out=out, lse=lse, weights=w, weights_out=w, workspace=ws)
+        ko, vo = (torch.zeros(14, kv, page, 128, dtype=torch.float16, device="cuda") for _ in range(2))
+        kept, new_len, wo = torch.zeros(2, kv, 100, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, kv, 100, device="cuda")
+        fq.fq_cache_evict(b, w, dk, dv, dst, 100, 10, ko, vo, kept, new_len, wo)
+        results.append([gain, x, dk, dv, out, lse, w, ko, vo, kept, new_len, wo])
+    assert taken == [("qk_norm_rope", 0), ("attn_paged", 0), ("cache_evict", 0)]
+    for g, h in zip(*results):
+        assert torch.equal(g, h)
