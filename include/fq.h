@@ -455,7 +455,7 @@ typedef struct {
     int seqs;               /* 1..65535 */
     int tokens;             /* rows of the call's arrays */
     int max_q;              /* most tokens of one sequence */
-    int max_len;            /* most positions of one sequence, at most table_stride * page */
+    int max_len;            /* most positions of one sequence, at most table_stride * page and 2^24 */
     int table_stride;
     int page;               /* positions of a page */
     int pages;              /* pages of the pools */

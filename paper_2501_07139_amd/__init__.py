@@ -668,7 +668,7 @@ class PagedBatch:
             raise FqError(-2, f"PagedBatch: {pages} pages of {page} positions (pages of {PAGE_SIZES}, 2^31 - 1 positions at most)")
         if not 1 <= seqs <= 65535 or len(seq_lens) != seqs or table.ndim != 2 or table.shape[0] != seqs or table.shape[1] < 1:
             raise FqError(-2, f"PagedBatch: {seqs} q_lens, {len(seq_lens)} seq_lens, table {table.shape}")
-        if q_lens.min() < 0 or seq_lens.min() < 0 or seq_lens.max() > min(table.shape[1] * page, 1 << 30) or q_lens.sum() >= 1 << 29:
+        if q_lens.min() < 0 or seq_lens.min() < 0 or seq_lens.max() > min(table.shape[1] * page, 1 << 24) or q_lens.sum() >= 1 << 29:
             raise FqError(-2, "PagedBatch: lengths must be at least 0 and fit the table")
         used = np.arange(table.shape[1])[None, :] * page < seq_lens[:, None]
         if ((table < 0) | (table >= pages))[used].any():

@@ -797,8 +797,8 @@ int check_batch(const char *fn, const fq_paged_batch *b, int n_kv_heads)
         return rc;
     if (b->seqs <= 0 || b->seqs > 65535 || b->tokens < 0 || b->max_q < 0 || b->max_q > b->tokens || (long long)b->max_q * b->seqs < b->tokens)
         return fq_fail(FQ_ERR_SHAPE, "%s: seqs=%d tokens=%d max_q=%d (need max_q <= tokens <= seqs * max_q)", fn, b->seqs, b->tokens, b->max_q);
-    if (b->table_stride <= 0 || b->max_len < 0 || b->max_len > (1 << 30) || b->max_len > (long long)b->table_stride * b->page)
-        return fq_fail(FQ_ERR_SHAPE, "%s: max_len=%d table_stride=%d (need max_len <= table_stride * page, at most 2^30)", fn, b->max_len,
+    if (b->table_stride <= 0 || b->max_len < 0 || b->max_len > (1 << 24) || b->max_len > (long long)b->table_stride * b->page)
+        return fq_fail(FQ_ERR_SHAPE, "%s: max_len=%d table_stride=%d (need max_len <= table_stride * page, at most 2^24)", fn, b->max_len,
                        b->table_stride);
     return FQ_OK;
 }

@@ -24,9 +24,9 @@ struct PagedAttnArgs {
     float *part_o, *part_ml;  // [splits][tokens][heads][128], [..][2]: unnormalised output; maximum (in powers of 2) and sum
     const float *weights;     // [seqs][kv_heads][weights_stride], or NULL: zeros
     float *weights_out;
-    float *scores;            // [tokens][heads][scores_stride]: scaled scores of sequences of few rows
+    float *scores;            // [tokens][heads][scores_stride]: scaled scores of sequences of few rows; [parts][seqs][kv_heads][..]: parts of column sums
     float scale;              // times log2(e): scores are powers of 2
-    int scores_stride, ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride;
+    int scores_stride, parts, part_rows, ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride;
 };
 
 // A tile of rows of one sequence and key/value head.
@@ -592,75 +592,182 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_ker
 }
 
 // --------------------------------------------------------------- column sums
-// w[t] of 64 positions: their keys stay in registers, the rows that see them stream by, sixteen a step and wavefront, and with lse known
-// a weight is one exponential.  One workgroup owns its positions: no atomics, the same sums every time.
+// w[t] of 256 positions from a part of the rows that see them, 64 positions a wavefront, whose keys stay in registers.  The rows come by 64 a
+// step through double-buffered LDS, straight from memory; with lse known a weight is one exponential.  Rows are the first operand here, so that a
+// lane has sixteen weights of ONE position and adds them up in place; what differs by row (lse, positions seen) is laid beside the rows.  One
+// workgroup owns its sums and the parts are added in order: no atomics, the same sums every time.
+constexpr int WK = 256, WR = 64; // positions of a workgroup, rows of a step
+
+// Rows of part `part` that see positions from t0 on: [lo, hi).
+__device__ __forceinline__ void part_rows(const PagedAttnArgs &p, const SeqRange &s, int t0, int part, int *lo, int *hi)
+{
+    *lo = max(max(t0 - (s.len - s.n), 0) * p.group, part * p.part_rows);
+    *hi = min(s.n * p.group, part * p.part_rows + p.part_rows);
+}
+
 __global__ __launch_bounds__(256, 2) void attn_paged_weights_kernel(PagedAttnArgs p)
 {
-    __shared__ float part[4][64];
-    const int kvh = blockIdx.x, t0 = blockIdx.y * 64, b = blockIdx.z;
+    __shared__ h8 Q0[WR * 16], Q1[WR * 16]; // chunk ch of row r at ch ^ (r % 16)
+    __shared__ __align__(16) float row_lse[2][WR];
+    __shared__ __align__(16) int row_seen[2][WR];
+    const int kvh = blockIdx.x % p.kv_heads, job = blockIdx.x / p.kv_heads, part = job % p.parts, t0 = job / p.parts * WK, b = blockIdx.y;
     const SeqRange s = seq_range(p.s, b);
     if (t0 >= s.len)
         return;
+    int lo, hi;
+    part_rows(p, s, t0, part, &lo, &hi);
+    if (lo >= hi && p.parts > 1)
+        return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15, g = lane >> 4;
-    h8 kk[4][4];
+    const int col = lane & 31, h = lane >> 5, older = s.len - s.n, mine = t0 + 64 * wave; // first position of the wavefront
+    h8 kk[2][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const size_t at = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, b, t0 + 16 * i) * PD;
+    for (int i = 0; i < 2; ++i) {
+        const size_t at = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, b, min(mine + 32 * i + col, s.len - 1)) * PD;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            kk[i][k] = *reinterpret_cast<const h8 *>(p.k + at + col * PD + 32 * k + 8 * g);
+        for (int k = 0; k < 8; ++k)
+            kk[i][k] = *reinterpret_cast<const h8 *>(p.k + at + 16 * k + 8 * h);
     }
-    float sum[4][4] = {};
-    const int rows = s.n * p.group, first = max(t0 - (s.len - s.n), 0) * p.group; // rows ahead see none of the positions
-    for (int r0 = first + 16 * wave; r0 < rows; r0 += 64) {
-        const int row = r0 + col, token = min(row, rows - 1) / p.group, head = kvh * p.group + min(row, rows - 1) - token * p.group;
-        const _Float16 *src = p.q + (size_t)(s.first + token) * p.ldq + head * PD + 8 * g;
-        h8 qb[4];
+    // A wavefront copies rows 16 wave + 4 i + lane / 16, i < 4, of a step; token and head of the group of each, kept up from step to step.  Rows
+    // behind the last one repeat it and count for nothing.
+    constexpr int NC = WR / 16;      // copies
+    int token[NC + 1], head[NC + 1]; // of each, and of the row whose lse the thread looks up
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            qb[k] = *reinterpret_cast<const h8 *>(src + 32 * k);
-        const float lse = p.lse[(size_t)(s.first + token) * p.heads + head] * LOG2E;
-        const int seen = row < rows ? min(s.len - s.n + token + 1, s.len) : 0;
+    for (int i = 0; i <= NC; ++i) {
+        const int ahead = i < NC ? 4 * (NC * wave + i) + (lane >> 4) : tid & (WR - 1);
+        token[i] = (lo + ahead) / p.group;
+        head[i] = lo + ahead - token[i] * p.group;
+    }
+    const int step_tokens = WR / p.group, step_heads = WR % p.group;
+    float lse_n; // used where the step ends, so that nothing waits for it
+    int seen_n;
+    bool real_n;
+    auto load = [&](h8 *dst) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f4 st = f4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < NC; ++i) {
+            const bool real = token[i] < s.n;
+            const int row = 4 * ((NC * wave + i) & 3) + (lane >> 4); // modulo sixteen
+            const _Float16 *src = p.q + (size_t)(s.first + (real ? token[i] : s.n - 1)) * p.ldq + (kvh * p.group + (real ? head[i] : 0)) * PD;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + 8 * ((lane & 15) ^ row)),
+                                             (__attribute__((address_space(3))) void *)(dst + 64 * (NC * wave + i)), 16, 0, 0);
+        }
+        real_n = token[NC] < s.n && token[NC] * p.group + head[NC] < hi;
+        lse_n = p.lse[(size_t)(s.first + (real_n ? token[NC] : 0)) * p.heads + kvh * p.group + (real_n ? head[NC] : 0)];
+        seen_n = older + token[NC] + 1;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                st = mfma16x16x32(kk[i][k], qb[k], st);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float e = __builtin_amdgcn_exp2f(st[v] * p.scale - lse);
-                sum[i][v] += t0 + 16 * i + 4 * g + v < seen ? e : 0.f;
+        for (int i = 0; i <= NC; ++i) {
+            token[i] += step_tokens;
+            head[i] += step_heads;
+            if (head[i] >= p.group) {
+                head[i] -= p.group;
+                ++token[i];
             }
         }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1)
-                sum[i][v] += __shfl_xor(sum[i][v], o, 64);
-            if (col == 0)
-                part[wave][16 * i + 4 * g + v] = sum[i][v];
+    };
+    auto store_rows = [&](int to) {
+        if (tid < WR) {
+            row_lse[to][tid] = real_n && lse_n != -INFINITY ? lse_n * LOG2E : INFINITY;
+            row_seen[to][tid] = seen_n;
         }
-    __syncthreads();
-    const int t = t0 + tid;
-    if (tid < 64 && t < s.len) {
-        const size_t at = ((size_t)b * p.kv_heads + kvh) * p.weights_stride + t;
-        const float before = p.weights && t < s.len - s.n ? p.weights[at] : 0.f;
-        p.weights_out[at] = before + ((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]));
+    };
+    float sum[2] = {0.f, 0.f};
+    if (lo < hi) {
+        load(Q0);
+        store_rows(0);
     }
+    __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
+    __syncthreads();
+    const int qat = col * 256 + ((h ^ (col & 15)) << 4);
+    auto step = [&](int r0, auto parity) {
+        constexpr int PAR = decltype(parity)::value;
+        const char *const Q = reinterpret_cast<const char *>(PAR ? Q1 : Q0);
+        const bool more = r0 + WR < hi;
+        if (more)
+            load(PAR ? Q0 : Q1);
+        if (older + (min(r0 + WR, hi) - 1) / p.group >= mine) { // some row sees some of the wavefront's positions (uniform)
+            const bool whole = older + r0 / p.group + 1 >= mine + 64;
+#pragma unroll
+            for (int rb = 0; rb < WR / 32; ++rb) {
+                f16v st[2] = {f16v{}, f16v{}};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const h8 qa = *reinterpret_cast<const h8 *>(Q + ((qat ^ (k << 5)) + 8192 * rb));
+                    st[0] = mfma32x32x16(qa, kk[0][k], st[0]);
+                    st[1] = mfma32x32x16(qa, kk[1][k], st[1]);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int4 seen = *reinterpret_cast<const int4 *>(&row_seen[PAR][32 * rb + 8 * u + 4 * h]);
+                        const int limit[4] = {seen.x, seen.y, seen.z, seen.w};
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v)
+                                st[i][4 * u + v] = mine + 32 * i + col < limit[v] ? st[i][4 * u + v] : -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const f4 lse = *reinterpret_cast<const f4 *>(&row_lse[PAR][32 * rb + 8 * u + 4 * h]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            sum[i] += __builtin_amdgcn_exp2f(fmaf(st[i][4 * u + v], p.scale, -lse[v]));
+                }
+            }
+        }
+        if (more)
+            store_rows(PAR ^ 1);
+        __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
+        __syncthreads();
+    };
+    for (int r0 = lo; r0 < hi; r0 += 2 * WR) {
+        step(r0, std::integral_constant<int, 0>{});
+        if (r0 + WR < hi)
+            step(r0 + WR, std::integral_constant<int, 1>{});
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float both = other_half(sum[i], add);
+        const int t = mine + 32 * i + col;
+        if (h != 0 || t >= s.len)
+            continue;
+        if (p.parts > 1) {
+            p.scores[(((size_t)part * p.s.seqs + b) * p.kv_heads + kvh) * p.scores_stride + t] = both;
+        } else {
+            const size_t at = ((size_t)b * p.kv_heads + kvh) * p.weights_stride + t;
+            p.weights_out[at] = (p.weights && t < older ? p.weights[at] : 0.f) + both;
+        }
+    }
+}
+
+// Adds the parts up, in order.
+__global__ __launch_bounds__(256) void attn_paged_weights_join_kernel(PagedAttnArgs p)
+{
+    const int kvh = blockIdx.x % p.kv_heads, t = blockIdx.x / p.kv_heads * 256 + threadIdx.x, b = blockIdx.y;
+    const SeqRange s = seq_range(p.s, b);
+    if (t >= s.len)
+        return;
+    const size_t at = ((size_t)b * p.kv_heads + kvh) * p.weights_stride + t;
+    float sum = p.weights && t < s.len - s.n ? p.weights[at] : 0.f;
+    for (int part = 0; part < p.parts; ++part) {
+        int lo, hi;
+        part_rows(p, s, t / WK * WK, part, &lo, &hi);
+        if (lo < hi)
+            sum += p.scores[(((size_t)part * p.s.seqs + b) * p.kv_heads + kvh) * p.scores_stride + t];
+    }
+    p.weights_out[at] = sum;
 }
 
 // The same where every sequence has at most sixteen rows: their scores are there already, and nothing is read twice but those.
 __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnArgs p)
 {
     constexpr int PER = 4; // positions a thread
-    const int kvh = blockIdx.x, b = blockIdx.z;
+    const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.y;
     const SeqRange s = seq_range(p.s, b);
-    const int rows = min(s.n * p.group, FEW), t0 = blockIdx.y * (256 * PER) + threadIdx.x;
+    const int rows = min(s.n * p.group, FEW), t0 = blockIdx.x / p.kv_heads * (256 * PER) + threadIdx.x;
     float sum[PER] = {};
     for (int r = 0; r < rows; ++r) {
         const size_t item = (size_t)(s.first + r / p.group) * p.heads + kvh * p.group + r % p.group;
@@ -695,7 +802,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 struct AttnPlan {
     int rows, tiles, splits, chunk;
     size_t part_o, part_ml, lse, scores, end; // offsets in the workspace, in floats
-    int scores_stride;
+    int scores_stride, parts, part_rows; // of the column sums: parts of the rows, rows of one
 };
 
 AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weights)
@@ -726,8 +833,12 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
     s.splits = s.splits < 1 ? 1 : s.splits;
     const size_t items = (size_t)b.tokens * heads, parts = s.splits > 1 ? (size_t)s.splits * items : 0;
     s.scores_stride = (b.max_len + 31) / 32 * 32;
-    s.scores = 0; // the parts of a multiple of four floats first
-    s.part_o = s.scores + (weights && s.rows == FEW ? items * s.scores_stride : 0);
+    // parts of the rows for the column sums: 512 rows, or what makes eight parts
+    s.part_rows = longest > 8 * 512 ? (int)((longest + 8 * WR - 1) / (8 * WR) * WR) : 512;
+    s.parts = (int)((longest + s.part_rows - 1) / s.part_rows);
+    s.parts = s.parts < 1 ? 1 : s.parts;
+    s.scores = 0; // what is a multiple of four floats first
+    s.part_o = s.scores + (!weights ? 0 : s.rows == FEW ? items * s.scores_stride : s.parts > 1 ? (size_t)s.parts * b.seqs * kv_heads * s.scores_stride : 0);
     s.part_ml = s.part_o + parts * PD;
     s.lse = s.part_ml + parts * 2;
     s.end = s.lse + (weights ? items : 0);
@@ -757,6 +868,8 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     a.lse = lse || !weights_out ? lse : ws + s.lse;
     a.scores = ws + s.scores;
     a.scores_stride = s.scores_stride;
+    a.parts = s.parts;
+    a.part_rows = s.part_rows;
     a.weights = weights;
     a.weights_out = weights_out;
     a.scale = scale * LOG2E;
@@ -794,10 +907,16 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
         }
     }
     if (weights_out && b.max_len > 0) {
-        if (s.rows == FEW)
-            hipLaunchKernelGGL(attn_paged_few_weights_kernel, dim3(kv_heads, (b.max_len + 1023) / 1024, b.seqs), dim3(256), 0, st, a);
-        else
-            hipLaunchKernelGGL(attn_paged_weights_kernel, dim3(kv_heads, (b.max_len + 63) / 64, b.seqs), dim3(256), 0, st, a);
+        const auto grid = [&](int positions, int parts) { return dim3((unsigned)((b.max_len + positions - 1) / positions * parts * kv_heads), b.seqs); };
+        if (s.rows == FEW) {
+            hipLaunchKernelGGL(attn_paged_few_weights_kernel, grid(1024, 1), dim3(256), 0, st, a);
+        } else {
+            hipLaunchKernelGGL(attn_paged_weights_kernel, grid(WK, s.parts), dim3(256), 0, st, a);
+            int rc = (int)hipGetLastError();
+            if (rc != 0 || s.parts == 1)
+                return rc;
+            hipLaunchKernelGGL(attn_paged_weights_join_kernel, grid(256, 1), dim3(256), 0, st, a);
+        }
     }
     return (int)hipGetLastError();
 }

@@ -152,6 +152,12 @@ def test_tall_tiles(fq, torch, seqs):
     run(fq, torch, np.random.default_rng(47), seqs, 16, 16, 64)
 
 
+@pytest.mark.parametrize("heads, kv, n, cached", [(24, 1, 129, 700), (64, 1, 70, 3), (20, 2, 90, 300)])
+def test_column_sums_of_many_rows(fq, torch, heads, kv, n, cached):
+    """Rows that are dealt to several parts, some of which see none of the later positions."""
+    run(fq, torch, np.random.default_rng(59), [(n, n + cached), (2, 40), (0, 300), (n // 2, n)], heads, kv, 64)
+
+
 def test_many_sequences(fq, torch):
     """More sequences than a wavefront has lanes; some without tokens."""
     rng = np.random.default_rng(3)

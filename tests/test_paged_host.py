@@ -61,7 +61,7 @@ def attn(lib, b, **c):
     (-1, {"v": None}, {}), (-1, {"out": None}, {}), (-1, {"weights": 16}, {}), (-2, {"heads": 3}, {}), (-2, {"heads": 0}, {}), (-2, {"kv": 0}, {}),
     (-2, {"ldq": 255}, {}), (-2, {"ldq": 260}, {}), (-2, {"scale": 0.0}, {}), (-2, {"scale": -1.0}, {}), (-2, {"scale": float("nan")}, {}),
     (-2, {"scale": float("inf")}, {}), (-2, {"weights_out": 16, "stride": 99}, {}), (-2, {}, {"seqs": 0}), (-2, {}, {"seqs": 65536}),
-    (-2, {}, {"tokens": -1}), (-2, {}, {"max_q": 6}), (-2, {}, {"max_q": 2}), (-2, {}, {"max_len": 129}), (-2, {}, {"max_len": -1}),
+    (-2, {}, {"tokens": -1}), (-2, {}, {"max_q": 6}), (-2, {}, {"max_q": 2}), (-2, {}, {"max_len": 129}), (-2, {}, {"max_len": -1}), (-2, {}, {"max_len": (1 << 24) + 1, "table_stride": 1 << 21}),
     (-2, {}, {"table_stride": 0}), (-2, {}, {"page": 8}), (-2, {}, {"page": 48}), (-2, {}, {"page": 512}), (-2, {}, {"pages": 0}),
     (-2, {}, {"pages": 1 << 27, "page": 16}), (-2, {"heads": 1 << 28, "kv": 1}, {"tokens": 3}), (-5, {"q": 8}, {}), (-5, {"k": 24}, {}),
     (-5, {"v": 24}, {}), (-5, {"out": 8}, {}), (-6, {"ws": None, "weights_out": 16, "stride": 100}, {}),
