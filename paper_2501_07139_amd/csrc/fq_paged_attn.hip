@@ -263,7 +263,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
 // Chunks.  Four wavefronts, 32 rows each (KS = 1), or two by two with every key tile of 64 positions halved between them (KS = 2: 64 rows).
 // Keys and values go through double-buffered LDS tiles, keys straight from memory, values through registers (the compiler keeps
 // track of only a few copies into LDS, and waits for all of them at once beyond those).  32x32x16 MFMAs: a lane has 32 scores of one row, so
-// half as many reads of LDS per product as with sixteen rows, and one step across lanes for a row's maximum.
+// half as many reads of LDS per product as with sixteen rows, and one step across lanes for a row's maximum.  Where a tile lies in one page (WHOLE:
+// pages of 64 positions and more) its address is formed once, not for each block of sixteen: a quarter of a step's instructions.
 constexpr int KT = 64; // positions of a tile
 
 constexpr int tile_rows_of(int KS) { return 128 / KS; }
@@ -283,10 +284,11 @@ __device__ __forceinline__ float other_half(float x, float (*f)(float, float))
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 
-template <int KS>
+template <int KS, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p)
 {
     constexpr int TR = tile_rows_of(KS), KB = 2 / KS; // KB: blocks of 32 positions that a wavefront has of a tile
+    constexpr int PARTS = WHOLE ? 1 : 4;              // runs of rows in a page that a key tile is made of: itself, or blocks of sixteen
     // Key tiles: chunk ch (eight dimensions) of row r at ch ^ (r % 16); value tiles: at ch ^ 4 (r % 4), for the transposing reads of eight rows by
     // four chunks.  Separate arrays, named statically in a loop unrolled by two: the tile being read is then known not to be the one
     // that copies in flight write.
@@ -322,24 +324,29 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     }
 
     const const_ints table = (const_ints)(p.s.table + (size_t)tile.b * p.s.table_stride);
-    const int last_block = max(end - 1, 0) & ~15, tiles = (end - begin + KT - 1) / KT;
+    const int tiles = (end - begin + KT - 1) / KT, last_run = max(end - 1, 0) & ~(KT / PARTS - 1);
     const int krow = 4 * wave + (lane >> 4); // the lane's row of every block of sixteen that it copies
     const uint32_t koff = (uint32_t)(krow * 256 + (((lane & 15) ^ krow) << 4)), voff = (uint32_t)(krow * 256 + ((lane & 15) << 4));
-    int pg[4];
-    auto load_pages = [&](int jt) { // blocks behind the last one repeat it
+    int pg[PARTS];
+    auto load_pages = [&](int jt) { // runs behind the last one repeat it
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            pg[i] = table[min(begin + KT * jt + 16 * i, last_block) >> p.s.page_log2];
+        for (int i = 0; i < PARTS; ++i)
+            pg[i] = table[min(begin + KT * jt + 16 * i, last_run) >> p.s.page_log2];
     };
     h8 vreg[4];
     auto load_tiles = [&](h8 *Kdst, int jt) {
+        fq_rsrc kr, vr;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = min(begin + KT * jt + 16 * i, last_block), page = min(max(pg[i], 0), p.s.pages - 1);
-            const size_t at = (((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * 256;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(reinterpret_cast<const char *>(p.k) + at, 4096), &Kdst[64 * (wave + 4 * i)], 16, koff,
-                                                     0, 0, 0);
-            vreg[i] = __builtin_bit_cast(h8, buf_load_b128(make_rsrc(reinterpret_cast<const char *>(p.v) + at, 4096), voff, 0));
+            if (i < PARTS) {
+                const int t = min(begin + KT * jt + 16 * i, last_run), page = min(max(pg[i], 0), p.s.pages - 1);
+                const size_t at = (((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * 256;
+                kr = make_rsrc(reinterpret_cast<const char *>(p.k) + at, KT / PARTS * 256);
+                vr = make_rsrc(reinterpret_cast<const char *>(p.v) + at, KT / PARTS * 256);
+            }
+            const uint32_t block = WHOLE ? 4096 * i : 0;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, &Kdst[64 * (wave + 4 * i)], 16, koff, block, 0, 0);
+            vreg[i] = __builtin_bit_cast(h8, buf_load_b128(vr, voff, block));
         }
         load_pages(jt + 1);
     };
@@ -887,10 +894,14 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
             hipLaunchKernelGGL(attn_paged_few_kernel<true>, grid, dim3(256), 0, st, a);
         else if (s.rows == FEW)
             hipLaunchKernelGGL(attn_paged_few_kernel<false>, grid, dim3(256), 0, st, a);
+        else if (s.rows == 64 && b.page >= KT)
+            hipLaunchKernelGGL((attn_paged_tile_kernel<2, true>), grid, dim3(256), 0, st, a);
         else if (s.rows == 64)
-            hipLaunchKernelGGL(attn_paged_tile_kernel<2>, grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((attn_paged_tile_kernel<2, false>), grid, dim3(256), 0, st, a);
+        else if (b.page >= KT)
+            hipLaunchKernelGGL((attn_paged_tile_kernel<1, true>), grid, dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL(attn_paged_tile_kernel<1>, grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL((attn_paged_tile_kernel<1, false>), grid, dim3(256), 0, st, a);
         int rc = (int)hipGetLastError();
         if (rc != 0)
             return rc;
