@@ -334,34 +334,21 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
             pg[i] = table[min(begin + KT * jt + 16 * i, last_run) >> p.s.page_log2];
     };
     h8 vreg[4];
-    auto load_tiles = [&](h8 *Kdst, int jt) {
-        fq_rsrc kr, vr;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < PARTS) {
-                const int t = min(begin + KT * jt + 16 * i, last_run), page = min(max(pg[i], 0), p.s.pages - 1);
-                const size_t at = (((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * 256;
-                kr = make_rsrc(reinterpret_cast<const char *>(p.k) + at, KT / PARTS * 256);
-                vr = make_rsrc(reinterpret_cast<const char *>(p.v) + at, KT / PARTS * 256);
-            }
-            const uint32_t block = WHOLE ? 4096 * i : 0;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, &Kdst[64 * (wave + 4 * i)], 16, koff, block, 0, 0);
-            vreg[i] = __builtin_bit_cast(h8, buf_load_b128(vr, voff, block));
+    fq_rsrc kr, vr;
+    auto load_block = [&](h8 *Kdst, int jt, int i) { // block i of both tiles; behind the last tile that one again
+        if (i < PARTS) {
+            const int t = min(begin + KT * jt + 16 * i, last_run), page = min(max(pg[i], 0), p.s.pages - 1);
+            const size_t at = (((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * 256;
+            kr = make_rsrc(reinterpret_cast<const char *>(p.k) + at, KT / PARTS * 256);
+            // values of positions that nobody sees may be anything, and 0 * NaN is NaN: the descriptor ends ahead of them, what is behind reads 0
+            vr = make_rsrc(reinterpret_cast<const char *>(p.v) + at, (uint32_t)min(end - t, KT / PARTS) * 256u);
         }
-        load_pages(jt + 1);
+        const uint32_t block = WHOLE ? 4096 * i : 0;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, &Kdst[64 * (wave + 4 * i)], 16, koff, block, 0, 0);
+        vreg[i] = __builtin_bit_cast(h8, buf_load_b128(vr, voff, block));
     };
     const int vdst = krow * 16 + ((lane & 15) ^ (4 * (lane >> 4)));
-    auto store_values = [&](h8 *Vdst, int jt) {
-        if (begin + KT * jt + KT > end) { // positions that nobody sees may hold anything, and 0 * NaN is NaN
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (begin + KT * jt + 16 * i + krow >= end)
-                    vreg[i] = h8{};
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            Vdst[256 * i + vdst] = vreg[i];
-    };
+    auto store_block = [&](h8 *Vdst, int i) { Vdst[256 * i + vdst] = vreg[i]; };
 
     f16v acc[4];
 #pragma unroll
@@ -374,8 +361,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
 
     if (tiles > 0) {
         load_pages(0);
-        load_tiles(Ks0, 0);
-        store_values(Vs0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            load_block(Ks0, 0, i);
+        load_pages(1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store_block(Vs0, i);
     }
     __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
     __syncthreads();
@@ -383,17 +375,23 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     auto tile_step = [&](int jt, auto parity) {
         constexpr int PAR = decltype(parity)::value;
         const char *const Kcur = reinterpret_cast<const char *>(PAR ? Ks1 : Ks0), *const Vcur = reinterpret_cast<const char *>(PAR ? Vs1 : Vs0);
-        if (jt + 1 < tiles)
-            load_tiles(PAR ? Ks0 : Ks1, jt + 1);
+        h8 *const Knext = PAR ? Ks0 : Ks1, *const Vnext = PAR ? Vs0 : Vs1;
         const int first = begin + KT * jt + 32 * KB * kpart; // first position of the wavefront's part
         if (first < min(any_seen, end)) {
+            // the next tile's copies go out between the products: issued in a row they wait for each other
             f16v st[KB];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
+            for (int kb = 0; kb < KB; ++kb)
                 st[kb] = f16v{};
 #pragma unroll
-                for (int s = 0; s < 8; ++s)
+            for (int s = 0; s < 8; ++s) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
                     st[kb] = mfma32x32x16(*reinterpret_cast<const h8 *>(Kcur + ((kat ^ (s << 5)) + 8192 * kb)), qb[s], st[kb]);
+                if (s & 1) {
+                    load_block(Knext, jt + 1, s >> 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             if (first + 32 * KB > all_seen || first + 32 * KB > end) { // uniform per wavefront
                 const int limit = min(seen, end) - first - 4 * h;
@@ -436,16 +434,26 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < 2; ++j) {
 #pragma unroll
                     for (int db = 0; db < 4; ++db) {
                         const char *at = Vcur + ((vat ^ (db << 6)) + 8192 * kb + 4096 * j);
                         const h4 lo = lds_column(reinterpret_cast<const _Float16 *>(at)), hi = lds_column(reinterpret_cast<const _Float16 *>(at + 2048));
                         acc[db] = mfma32x32x16(h8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pb[kb][j], acc[db]);
                     }
+#pragma unroll
+                    for (int i = (2 * kb + j) * 2 / KB; i < (2 * kb + j + 1) * 2 / KB; ++i)
+                        store_block(Vnext, i); // last read in the previous step, before its barrier
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                load_block(Knext, jt + 1, i);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_block(Vnext, i);
         }
-        if (jt + 1 < tiles)
-            store_values(PAR ? Vs0 : Vs1, jt + 1); // last read in the previous step, before its barrier
+        load_pages(jt + 2);
         __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
         __syncthreads();
     };
