@@ -491,6 +491,11 @@ size_t fq_attn_paged_workspace_bytes(const fq_paged_batch *batch, int n_heads, i
 int fq_attn_paged(const fq_paged_batch *batch, const void *q, int ldq, int n_heads, int n_kv_heads, const void *k_pages,
                   const void *v_pages, float scale, void *out, float *lse, const float *weights, float *weights_out,
                   int weights_stride, void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * How fq_attn_paged divides a call (host only; for tests and tools).  route_out (host, 3 ints): rows of a tile, a row being a token and a
+ * query head of one key/value head (16: single tokens, 64 or 128), splits of the positions, positions of a split.
+ */
+int fq_attn_paged_route(const fq_paged_batch *batch, int n_heads, int n_kv_heads, int *route_out);
 
 /*
  * Cut every sequence of the batch to `keep` positions, for each key/value head on its own: its last `recent` positions stay,

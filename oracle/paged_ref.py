@@ -35,28 +35,28 @@ def norm_rope(x, positions, table, gain=None, eps=1e-5):
 
 def attention(q, keys, values, n, scale):
     """One sequence: q [n, 128 heads], keys and values [kv_heads, S, 128].  Returns (out, lse [n, heads], column sums
-    [kv_heads, S], sum of p |V| as out, largest scale * sum |q| |K| of a visible pair)."""
+    [kv_heads, S], sum of p |V| as out, largest scale * sum |q| |K| of a pair)."""
     keys, values = _f64(keys), _f64(values)
     kv, S, _ = keys.shape
     heads = q.shape[1] // D
     q = _f64(q).reshape(n, heads, D)
     out, mass, lse = np.zeros_like(q), np.zeros_like(q), np.full((n, heads), -np.inf)
     sums, size = np.zeros((kv, S)), 0.0
-    for i in range(n):
-        seen = S - n + i + 1
-        if seen <= 0:
-            continue
-        for h in range(heads):
-            g = h // (heads // kv)
-            s = scale * (keys[g, :seen] @ q[i, h])
-            top = s.max()
-            e = np.exp(s - top)
-            lse[i, h] = top + np.log(e.sum())
-            p = e / e.sum()
-            out[i, h] = p @ values[g, :seen]
-            mass[i, h] = p @ np.abs(values[g, :seen])
-            sums[g, :seen] += p
-            size = max(size, scale * (np.abs(keys[g, :seen]) @ np.abs(q[i, h])).max())
+    first = max(n - S, 0)  # tokens ahead of it see nothing
+    if S == 0 or first >= n:
+        return out.reshape(n, heads * D), lse, sums, mass.reshape(n, heads * D), size
+    hidden = np.arange(S)[None, :] > S - n + np.arange(first, n)[:, None]
+    for h in range(heads):
+        g = h // (heads // kv)
+        s = np.where(hidden, -np.inf, scale * (q[first:, h] @ keys[g].T))
+        top = s.max(1, keepdims=True)
+        e = np.exp(s - top)
+        norm = e.sum(1, keepdims=True)
+        lse[first:, h] = (top + np.log(norm))[:, 0]
+        p = e / norm
+        out[first:, h], mass[first:, h] = p @ values[g], p @ np.abs(values[g])
+        sums[g] += p.sum(0)
+        size = max(size, scale * (np.abs(q[first:, h]) @ np.abs(keys[g]).T).max())
     return out.reshape(n, heads * D), lse, sums, mass.reshape(n, heads * D), size
 
 

@@ -100,6 +100,7 @@ def _load() -> ctypes.CDLL:
         "fq_prefill_forward": (ci, [ctypes.POINTER(fq_layer), ci, vp, vp, ci, vp, vp, vp, ci, vp, vp, sz, vp]),
         "fq_qk_norm_rope": (ci, [vp, ci, vp, ci, vp, ci, ci, ci, ci, vp, vp, vp, ci, vp, vp, ctypes.c_float, vp, vp, vp, ci, ci, vp]),
         "fq_attn_paged_workspace_bytes": (sz, [ctypes.POINTER(fq_paged_batch), ci, ci, ci]),
+        "fq_attn_paged_route": (ci, [ctypes.POINTER(fq_paged_batch), ci, ci, vp]),
         "fq_attn_paged": (ci, [ctypes.POINTER(fq_paged_batch), vp, ci, ci, ci, vp, vp, ctypes.c_float, vp, vp, vp, vp, ci, vp, sz, vp]),
         "fq_cache_evict": (ci, [ctypes.POINTER(fq_paged_batch), vp, vp, ci, vp, ci, ci, ci, vp, ci, ci, vp, vp, vp, vp, vp, ci, vp]),
     }
@@ -139,7 +140,8 @@ EXPORTS = ("fq_last_error", "fq_version", "fq_quantize_rtn", "fq_packed_bytes", 
            "fq_init", "fq_dense_f16_tile", "fq_rope_table", "fq_stack_forward_noalloc", "fq_set_decode_mode",
            "fq_decode_give_up_ticks", "fq_async_error", "fq_clear_async_error", "fq_decode_partition", "fq_decode_persistent",
            "fq_decode_persistent_launches", "fq_qlinear_route", "fq_qlinear_tall_tile", "fq_dense_route",
-           "fq_qk_norm_rope", "fq_attn_paged_workspace_bytes", "fq_attn_paged", "fq_cache_evict")
+           "fq_qk_norm_rope", "fq_attn_paged_workspace_bytes", "fq_attn_paged", "fq_attn_paged_route",
+           "fq_cache_evict")
 
 
 # The calls below that small ones are made of go through _bind where nothing is to be allocated; it answers None to whatever it does
@@ -766,6 +768,13 @@ def fq_qk_norm_rope(q, k, v, batch: PagedBatch, rope, k_pages, v_pages, q_gain=N
 
 def fq_attn_paged_workspace_bytes(batch: PagedBatch, n_heads: int, n_kv_heads: int, with_weights: bool = False) -> int:
     return _lib.fq_attn_paged_workspace_bytes(batch.struct, n_heads, n_kv_heads, int(with_weights))
+
+
+def fq_attn_paged_route(batch: PagedBatch, n_heads: int, n_kv_heads: int):
+    """(rows of a tile, splits of the positions, positions of a split) as fq_attn_paged divides a call."""
+    out = np.zeros(3, dtype=np.int32)
+    _check(_lib.fq_attn_paged_route(batch.struct, n_heads, n_kv_heads, _hp(out)))
+    return tuple(int(v) for v in out)
 
 
 def fq_attn_paged(q, batch: PagedBatch, k_pages, v_pages, scale: Optional[float] = None, out=None, lse=None, weights=None,

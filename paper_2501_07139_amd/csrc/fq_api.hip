@@ -842,6 +842,19 @@ extern "C" size_t fq_attn_paged_workspace_bytes(const fq_paged_batch *batch, int
     return align_up(fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, with_weights != 0));
 }
 
+extern "C" int fq_attn_paged_route(const fq_paged_batch *batch, int n_heads, int n_kv_heads, int *route_out)
+{
+    const char *fn = "fq_attn_paged_route";
+    if (!route_out)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL output", fn);
+    if (int rc = check_batch(fn, batch, n_kv_heads))
+        return rc;
+    if (int rc = check_heads(fn, batch->tokens, n_heads, n_kv_heads))
+        return rc;
+    fq_attn_paged_plan(*batch, n_heads, n_kv_heads, &route_out[0], &route_out[1], &route_out[2]);
+    return FQ_OK;
+}
+
 extern "C" int fq_attn_paged(const fq_paged_batch *batch, const void *q, int ldq, int n_heads, int n_kv_heads, const void *k_pages,
                              const void *v_pages, float scale, void *out, float *lse, const float *weights, float *weights_out,
                              int weights_stride, void *workspace, size_t workspace_bytes, void *stream)

@@ -108,6 +108,7 @@ int fq_launch_attn_prefill(const void *q, const void *k, const void *v, int T, v
 int fq_launch_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, int tokens, int heads, int kv_heads,
                            const int32_t *positions, const int32_t *slots, const float *rope, int rope_rows, const void *q_gain,
                            const void *k_gain, float eps, void *q_out, void *k_pages, void *v_pages, int page_log2, int pages, fq_stream st);
+void fq_attn_paged_plan(const fq_paged_batch &b, int heads, int kv_heads, int *rows, int *splits, int *chunk);
 size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights);
 int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int heads, int kv_heads, const void *k, const void *v, float scale,
                          void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st);

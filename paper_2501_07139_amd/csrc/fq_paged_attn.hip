@@ -813,7 +813,13 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 // 20 / 17.7 / 16.9 / 20.7; 8 heads, 8000 positions 15.8 / 12.8 / 14 / 19; 64 sequences of 8 heads, 700 positions 35 / 35 / 35 / 29 (one split); 64 of 17
 // to 4096 (with the join) 41.7 / 38.2 / 38.7 / 42.1.
 //
-// Chunks: as many splits as bring two workgroups to every CU, none shorter than 256 positions.
+// Chunks: what an estimate (us) of these finds shortest, for tiles of 64 and 128 rows: 6 for the launch, the first loads and the end; a step of 64
+// positions takes a workgroup 0.69 (128 rows: 1.0) by itself, and 256 CUs together do one in 0.9 (1.36) each, as the card lowers its clock
+// under that load; joining splits takes 4 and two passes over the parts at 4 TB/s.  Over 37 sizes of 5 to 3000 tokens and 256
+// to 16000 positions its choice takes 1.8 % longer than the best of both heights and six lengths, at most 8 % (17 % where several sequences are all as
+// long as the longest).  Some, as measured: 16 tokens, 8 key/value
+// heads of 4 queries, 16000 positions 171 in one split, 23.5 / 21.2 / 24.8 in splits of 1024 / 512 / 256; 2048 tokens of 32 heads 50 in tiles of 128 rows, 66
+// in tiles of 64; 1000 tokens 24.5 and 21.2.
 struct AttnPlan {
     int rows, tiles, splits, chunk;
     size_t part_o, part_ml, lse, scores, end; // offsets in the workspace, in floats
@@ -829,24 +835,35 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
         const long long full = rows / height + (b.seqs < rows ? b.seqs : rows), most = b.seqs * ((longest + height - 1) / height);
         return full < most ? full : most;
     };
-    s.rows = longest <= FEW ? FEW : (tiles(128) * kv_heads >= 512 ? 128 : 64);
-    s.tiles = s.rows == FEW ? b.seqs : (int)tiles(s.rows);
-    const long long jobs = (long long)s.tiles * kv_heads;
-    const auto pieces = [&](int chunk) { return jobs * ((b.max_len + chunk - 1) / chunk); };
-    if (s.rows == FEW) {
+    const size_t items = (size_t)b.tokens * heads;
+    if (longest <= FEW) {
+        s.rows = FEW;
+        s.tiles = b.seqs;
+        const long long jobs = (long long)b.seqs * kv_heads;
+        const auto pieces = [&](int chunk) { return jobs * ((b.max_len + chunk - 1) / chunk); };
         const bool one = b.max_len <= 384 || (b.max_len <= 1024 && jobs >= 128);
         s.chunk = one ? (b.max_len + 127) / 128 * 128 : pieces(128) <= 384 ? 128 : pieces(256) <= 384 ? 256 : 512;
     } else {
-        long long splits = jobs > 0 ? 512 / jobs : 1;
-        const long long shortest = (b.max_len + 255) / 256;
-        splits = splits > shortest ? shortest : splits;
-        splits = splits < 1 ? 1 : splits;
-        s.chunk = (int)((b.max_len + splits - 1) / splits + 127) / 128 * 128;
+        double best = 0;
+        // steps of a tile, all splits together; several sequences are taken to be half as long as the longest
+        const double mean = (b.max_len > b.max_q ? b.max_len - 0.5 * b.max_q : 0.5 * b.max_len) / KT * (b.seqs > 1 ? 0.5 : 1.0) + 0.5;
+        for (int rows = 64; rows <= 128; rows *= 2)
+            for (int splits = 1; splits == 1 || b.max_len / splits > 128; splits *= 2) { // none shorter than 256 positions
+                const int chunk = ((b.max_len + splits - 1) / splits + 127) / 128 * 128;
+                const double alone = (double)chunk / KT * (rows == 64 ? 0.69 : 1.0), together = tiles(rows) * kv_heads * mean / 256 * (rows == 64 ? 0.9 : 1.36);
+                const double us = 6 + (alone > together ? alone : together) + (splits > 1 ? 4 + items * splits * 1040e-6 / 4 : 0);
+                if (best == 0 || us < best) {
+                    best = us;
+                    s.rows = rows;
+                    s.chunk = chunk;
+                }
+            }
+        s.tiles = (int)tiles(s.rows);
     }
     s.chunk = s.chunk < 128 ? 128 : s.chunk;
     s.splits = (b.max_len + s.chunk - 1) / s.chunk;
     s.splits = s.splits < 1 ? 1 : s.splits;
-    const size_t items = (size_t)b.tokens * heads, parts = s.splits > 1 ? (size_t)s.splits * items : 0;
+    const size_t parts = s.splits > 1 ? (size_t)s.splits * items : 0;
     s.scores_stride = (b.max_len + 31) / 32 * 32;
     // parts of the rows for the column sums: 512 rows, or what makes eight parts
     s.part_rows = longest > 8 * 512 ? (int)((longest + 8 * WR - 1) / (8 * WR) * WR) : 512;
@@ -861,6 +878,14 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
 }
 
 } // namespace
+
+void fq_attn_paged_plan(const fq_paged_batch &b, int heads, int kv_heads, int *rows, int *splits, int *chunk)
+{
+    const AttnPlan s = plan_attn(b, heads, kv_heads, false);
+    *rows = s.rows;
+    *splits = s.splits;
+    *chunk = s.chunk;
+}
 
 size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights)
 {

@@ -146,10 +146,16 @@ def test_ragged_batches(fq, torch, heads, kv, page):
     run(fq, torch, rng, [(1, 40), (0, 77), (70, 70), (1, 300), (0, 0), (5, 3), (19, 140), (3, 0), (1, 1), (40, 290), (130, 131)], heads, kv, page)
 
 
-@pytest.mark.parametrize("seqs", [[(129, 129)] * 8 + [(140, 300)] * 8, [(1, 50), (300, 300), (257, 400), (0, 9), (128, 128), (2, 1)] * 5], ids=["even", "odd"])
-def test_tall_tiles(fq, torch, seqs):
-    """Enough rows for the highest tiles."""
-    run(fq, torch, np.random.default_rng(47), seqs, 16, 16, 64)
+@pytest.mark.parametrize("page", [32, 128])
+@pytest.mark.parametrize("seqs, heads, kv, route", [
+    ([(2048, 2048)], 32, 16, (128, 1)), ([(1700, 1701), (3, 900)], 32, 32, (64, 1)), ([(256, 4000)], 32, 8, (128, 4)),
+    ([(100, 2000)], 32, 16, (64, 4)), ([(300, 1000)], 40, 8, (64, 1))], ids=str)
+def test_every_division(fq, torch, seqs, heads, kv, route, page):
+    """Both heights of the tiles, with and without splits, tiles in one page and of several."""
+    table, pages = deal(np.random.default_rng(0), [S for _, S in seqs], page)
+    b = fq.PagedBatch([n for n, _ in seqs], [S for _, S in seqs], table, page, pages)
+    assert fq.fq_attn_paged_route(b, heads, kv)[:2] == route
+    run(fq, torch, np.random.default_rng(47), seqs, heads, kv, page)
 
 
 @pytest.mark.parametrize("heads, kv, n, cached", [(24, 1, 129, 700), (64, 1, 70, 3), (20, 2, 90, 300)])

@@ -80,6 +80,24 @@ def test_workspace_of_bad_arguments_is_none():
     assert lib.fq_attn_paged_workspace_bytes(ctypes.byref(batch()), 2, 2, 1) >= 5 * 2 * 4
 
 
+def test_division_of_calls():
+    """One split where that is no longer, splits that cover the positions, 128-row tiles for the largest calls only."""
+    one = lambda q, S, seqs=1: fq.PagedBatch([q] * seqs, [S] * seqs, np.zeros((seqs, S // 16 + 1), dtype=np.int64), 16, 4, device="cpu")
+    assert fq.fq_attn_paged_route(one(1, 300), 32, 32) == (16, 1, 384)
+    assert fq.fq_attn_paged_route(one(1, 1000, 64), 32, 8)[:2] == (16, 1)
+    assert fq.fq_attn_paged_route(one(1, 1000), 32, 8) == (16, 8, 128)
+    assert fq.fq_attn_paged_route(one(1, 100000), 32, 8) == (16, 196, 512)
+    assert fq.fq_attn_paged_route(one(16, 16000), 32, 8)[0] == 64 and fq.fq_attn_paged_route(one(2048, 2048), 32, 32)[:2] == (128, 1)
+    rng = np.random.default_rng(0)
+    for _ in range(3000):
+        kv, group, n, S = (int(2 ** rng.uniform(0, t)) for t in (5, 5, 12, 17))
+        rows, splits, chunk = fq.fq_attn_paged_route(one(n, S), kv * group, kv)
+        assert (rows == 16) == (n * group <= 16) and chunk % 128 == 0 and (splits - 1) * chunk < S <= splits * chunk, (kv, group, n, S)
+    lib, out = fq._lib, np.zeros(3, dtype=np.int32)
+    assert lib.fq_attn_paged_route(ctypes.byref(batch()), 2, 2, None) == -1
+    assert lib.fq_attn_paged_route(ctypes.byref(batch(page=5)), 2, 2, out.ctypes.data_as(ctypes.c_void_p)) == -2
+
+
 def rope(lib, **c):
     a = dict(q=16, ldq=256, k=16, ldk=256, v=16, ldv=256, tokens=3, heads=2, kv=2, positions=16, slots=16, rope=16, rows=9, qg=None, kg=None,
              eps=1e-5, out=32, kp=16, vp=16, page=16, pages=4)
