@@ -72,6 +72,34 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile)
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 
+__device__ __forceinline__ bool is_finite(_Float16 x) { return (__builtin_bit_cast(unsigned short, x) & 0x7c00) != 0x7c00; }
+
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// The largest magnitudes of both halves of the dwords, as bits: 0x7c00 and above are not finite.
+__device__ __forceinline__ us2 largest_bits(h8 x, us2 so_far)
+{
+    const u4v u = __builtin_bit_cast(u4v, x) & 0x7fff7fffu;
+    const uint32_t d[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        so_far = __builtin_elementwise_max(so_far, __builtin_bit_cast(us2, d[i]));
+    return so_far;
+}
+
+__device__ __forceinline__ bool finite_bits(us2 m) { return m.x < 0x7c00 && m.y < 0x7c00; }
+
+__device__ __forceinline__ bool all_finite(h8 x) { return finite_bits(largest_bits(x, us2{0, 0})); }
+
+__device__ __forceinline__ h8 finite_only(h8 x)
+{
+    h8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        y[e] = is_finite(x[e]) ? x[e] : (_Float16)0.f;
+    return y;
+}
+
 // Four halves of one column from four consecutive rows: lane j of sixteen names the 8 bytes of row j / 4, columns 4 (j % 4)... of a
 // 4 x 16 block and gets column j of it.
 __device__ __forceinline__ h4 lds_column(const _Float16 *at)
@@ -155,6 +183,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
                 st[i] = mfma16x16x32(kk[i][s], qb[s], st[i]);
             st[i] *= p.scale;
         }
+        uint32_t not_finite = 0; // rows of the step, bit 16 i + 4 s + g, with values that not every row sees and that are not finite
         if (t0 + 32 > min(all_seen, end)) { // uniform; rows that nobody sees may hold anything, and 0 * NaN is NaN
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -163,6 +192,15 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
                     st[i][v] = t0 + 16 * i + 4 * g + v < min(seen, end) ? st[i][v] : -INFINITY;
                     if (t0 + 16 * i + 4 * v + g >= end)
                         vv[i][v] = h8{};
+                    if (all_seen < end) { // a chunk's own positions: out of the product, and added for the rows that see them (below)
+                        const unsigned long long bad = __builtin_amdgcn_ballot_w64(!all_finite(vv[i][v]));
+                        if (bad) {
+                            vv[i][v] = finite_only(vv[i][v]);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                not_finite |= (bad >> (16 * r) & 0xffffu) ? 1u << (16 * i + 4 * v + r) : 0u;
+                        }
+                    }
                 }
         }
         if constexpr (SCORES) {
@@ -209,6 +247,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
             acc[db] = mfma16x16x32(h8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pb, acc[db]);
         }
         __builtin_amdgcn_wave_barrier();
+        for (; not_finite; not_finite &= not_finite - 1) {
+            const int t = t0 + __builtin_ctz(not_finite);
+            if (t >= seen)
+                continue;
+            const _Float16 *v = p.v + pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, b, t) * PD + 4 * g;
+#pragma unroll
+            for (int db = 0; db < 8; ++db) {
+                const h4 x = *reinterpret_cast<const h4 *>(v + 16 * db);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[db][e] += is_finite(x[e]) ? 0.f : (float)x[e];
+            }
+        }
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
@@ -294,6 +345,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     // that copies in flight write.
     __shared__ h8 Ks0[KT * 16], Ks1[KT * 16];
     __shared__ h8 Vs0[KT * 16], Vs1[KT * 16];
+    __shared__ __align__(8) unsigned short not_finite[2][4]; // of a value tile that not every row sees all of: rows with such a value, per wavefront that copied them
 
     // Longest tiles first, dealt from both ends: workgroups b and b + half share a CU when there are two a CU.
     const int jobs = (int)gridDim.x, half = (jobs + 1) >> 1, bidx = (int)blockIdx.x;
@@ -349,6 +401,30 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     };
     const int vdst = krow * 16 + ((lane & 15) ^ (4 * (lane >> 4)));
     auto store_block = [&](h8 *Vdst, int i) { Vdst[256 * i + vdst] = vreg[i]; };
+    // A weight of zero takes nothing from a position, but the matrix product has 0 * inf = NaN.  In tiles that reach behind the first row's last
+    // position, values that are not finite are therefore zeros in LDS, and rows that see them get them added (below).
+    const int every = older + tile.row0 / p.group + 1; // positions that every row of the tile sees
+    auto clear_not_finite = [&](h8 *Vdst, int jt, unsigned short *flags) {
+        if (begin + KT * jt + KT <= every)
+            return;
+        uint32_t found = 0; // bit 4 i + r: row 16 i + 4 wave + r
+        us2 most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            most = largest_bits(vreg[i], most);
+        if (__builtin_amdgcn_ballot_w64(!finite_bits(most))) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned long long bad = __builtin_amdgcn_ballot_w64(!all_finite(vreg[i]));
+                Vdst[256 * i + vdst] = finite_only(vreg[i]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    found |= (bad >> (16 * r) & 0xffffu) ? 1u << (4 * i + r) : 0u;
+            }
+        }
+        if (lane == 0)
+            flags[wave] = (unsigned short)found;
+    };
 
     f16v acc[4];
 #pragma unroll
@@ -368,16 +444,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             store_block(Vs0, i);
+        clear_not_finite(Vs0, 0, not_finite[0]);
     }
     __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
     __syncthreads();
 
-    auto tile_step = [&](int jt, auto parity) {
+    // PLAIN: this tile and the next are seen by all rows.
+    auto tile_step = [&](int jt, auto parity, auto plain) {
         constexpr int PAR = decltype(parity)::value;
+        constexpr bool PLAIN = decltype(plain)::value;
         const char *const Kcur = reinterpret_cast<const char *>(PAR ? Ks1 : Ks0), *const Vcur = reinterpret_cast<const char *>(PAR ? Vs1 : Vs0);
         h8 *const Knext = PAR ? Ks0 : Ks1, *const Vnext = PAR ? Vs0 : Vs1;
         const int first = begin + KT * jt + 32 * KB * kpart; // first position of the wavefront's part
-        if (first < min(any_seen, end)) {
+        if (PLAIN || first < min(any_seen, end)) {
             // the next tile's copies go out between the products: issued in a row they wait for each other
             f16v st[KB];
 #pragma unroll
@@ -393,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (first + 32 * KB > all_seen || first + 32 * KB > end) { // uniform per wavefront
+            if (!PLAIN && (first + 32 * KB > all_seen || first + 32 * KB > end)) { // uniform per wavefront
                 const int limit = min(seen, end) - first - 4 * h;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
@@ -445,6 +524,25 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
                     for (int i = (2 * kb + j) * 2 / KB; i < (2 * kb + j + 1) * 2 / KB; ++i)
                         store_block(Vnext, i); // last read in the previous step, before its barrier
                 }
+            if (!PLAIN && begin + KT * jt + KT > every) {
+                const u2v flags = *reinterpret_cast<const u2v *>(not_finite[PAR]); // bit 16 wave + 4 i + r
+                unsigned long long bits = (unsigned long long)__builtin_amdgcn_readfirstlane(flags.y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(flags.x);
+#pragma unroll 1
+                for (; bits; bits &= bits - 1) {
+                    const int b = __builtin_ctzll(bits);
+                    const int r = 16 * ((b & 15) >> 2) + 4 * (b >> 4) + (b & 3), t = begin + KT * jt + r;
+                    if (r / (32 * KB) != kpart || t >= seen)
+                        continue;
+                    const _Float16 *v = p.v + pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, tile.b, t) * PD + 4 * h;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const h4 x = *reinterpret_cast<const h4 *>(v + 8 * i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[i >> 2][4 * (i & 3) + e] += is_finite(x[e]) ? 0.f : (float)x[e];
+                    }
+                }
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -453,17 +551,23 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
             for (int i = 0; i < 4; ++i)
                 store_block(Vnext, i);
         }
+        if constexpr (!PLAIN)
+            clear_not_finite(Vnext, jt + 1, not_finite[PAR ^ 1]);
         load_pages(jt + 2);
         __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0);
         __syncthreads();
     };
+    const int seen_by_all = min((min(every, end) - begin) / KT, tiles); // tiles
     int jt = 0;
-    for (; jt + 1 < tiles; jt += 2) {
-        tile_step(jt, std::integral_constant<int, 0>{});
-        tile_step(jt + 1, std::integral_constant<int, 1>{});
+    for (; jt + 2 < seen_by_all; jt += 2) {
+        tile_step(jt, std::integral_constant<int, 0>{}, std::true_type{});
+        tile_step(jt + 1, std::integral_constant<int, 1>{}, std::true_type{});
     }
-    if (jt < tiles)
-        tile_step(jt, std::integral_constant<int, 0>{});
+    for (; jt < tiles; jt += 2) {
+        tile_step(jt, std::integral_constant<int, 0>{}, std::false_type{});
+        if (jt + 1 < tiles)
+            tile_step(jt + 1, std::integral_constant<int, 1>{}, std::false_type{});
+    }
     l = other_half(l, add);
 
     if constexpr (KS == 2) { // both halves meet in LDS, in the wavefront of the first

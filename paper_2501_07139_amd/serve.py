@@ -1,0 +1,184 @@
+"""Serving several sequences at once out of one pool of cache pages (FlexQuant, arXiv 2501.07139, Sections "Introduction" and
+"Elastic Serving": a hosted model answers requests while the memory that it may take varies).
+
+The weights' part of that memory is what ``elastic.ElasticModel`` moves along the ensemble; the cache's part is what is kept
+here.  Every block has its keys and values in pages of a pool, a sequence holds as many pages as it has positions, a step takes
+any mixture of prompts, chunks of prompts and single tokens, and a sequence that has outgrown its share is cut back to the
+positions that its tokens have looked at most, and its last ones.  The bit vector may change from step to step.
+
+All arithmetic is the library's; this module keeps account of pages and lengths.
+"""
+from __future__ import annotations
+
+from typing import Dict, List, Optional
+
+import numpy as np
+import torch
+
+from . import (FqError, PagedBatch, Stack, fq_attn_paged, fq_cache_evict, fq_glue, fq_qk_norm_rope, fq_qlinear, rope_table)
+
+
+class PagePool:
+    """Numbers of the pages that no sequence holds; the same page of every block's pools belongs together."""
+
+    def __init__(self, pages: int, page: int):
+        self.page, self.pages = page, pages
+        self._free = list(range(pages - 1, -1, -1))
+
+    @property
+    def free(self) -> int:
+        return len(self._free)
+
+    def need(self, positions: int) -> int:
+        return -(-positions // self.page)
+
+    def take(self, count: int) -> List[int]:
+        if count > len(self._free):
+            raise MemoryError(f"{count} pages needed, {len(self._free)} free of {self.pages}")
+        taken = [self._free.pop() for _ in range(count)]
+        return taken
+
+    def give(self, pages: List[int]) -> None:
+        self._free.extend(reversed(pages))
+
+
+class _Sequence:
+    def __init__(self):
+        self.pages: List[int] = []
+        self.length = 0    # positions in the cache
+        self.position = 0  # of the next token: runs ahead of the length once positions have been dropped
+
+
+class PagedServer:
+    """Blocks of a hosted model over a paged cache.
+
+    stack: its shapes decide heads and key/value heads (rows of q and k over 128).  slots: sequences at once.  gains: per block
+    (q_gain, k_gain), fp16 [128] on the device, for models that normalise their heads.  With `keep`, a sequence that is longer than
+    `limit` after a step is cut to `keep` positions a head, the last `recent` among them.
+    """
+
+    def __init__(self, stack: Stack, slots: int, pages: int, page: int = 64, max_positions: int = 4096, gains=None,
+                 keep: Optional[int] = None, recent: int = 0, limit: Optional[int] = None, device="cuda"):
+        q, k = (next(iter(stack.layers[0][j].values())) for j in (0, 1))
+        if q.N % 128 or k.N % 128 or (q.N // 128) % (k.N // 128):
+            raise ValueError("q and k must have 128 rows a head, the query heads a multiple of the key/value heads")
+        if gains is not None and len(gains) != stack.L:
+            raise ValueError("a pair of gains for every block")
+        if keep is not None and not 0 <= recent <= keep <= (limit if limit is not None else keep):
+            raise ValueError("need 0 <= recent <= keep <= limit")
+        self.heads, self.kv_heads, self.L = q.N // 128, k.N // 128, stack.L
+        self.pool = PagePool(pages, page)
+        self.max_positions, self.device = max_positions, torch.device(device)
+        self.keep, self.recent, self.limit = keep, recent, keep if limit is None else limit
+        self.gains = gains
+        shape = (self.L, pages, self.kv_heads, page, 128)
+        self.k, self.v = (torch.zeros(shape, dtype=torch.float16, device=self.device) for _ in range(2))
+        self.rope = rope_table(max_positions, device=self.device)
+        self.slots = slots
+        self.seqs: Dict[int, _Sequence] = {}
+        self.weights = None
+        if keep is not None:  # what every position has received of the softmax, per block
+            self.weights = torch.zeros((self.L, slots, self.kv_heads, max_positions), dtype=torch.float32, device=self.device)
+
+    # ------------------------------------------------------------------ sequences
+    def open(self) -> int:
+        """A slot for a new sequence."""
+        for i in range(self.slots):
+            if i not in self.seqs:
+                self.seqs[i] = _Sequence()
+                return i
+        raise MemoryError(f"all {self.slots} slots are taken")
+
+    def close(self, slot: int) -> None:
+        self.pool.give(self.seqs.pop(slot).pages)
+
+    def length(self, slot: int) -> int:
+        return self.seqs[slot].length
+
+    def cache_bytes(self) -> int:
+        """Bytes of the pages that sequences hold, all blocks together."""
+        return (self.pool.pages - self.pool.free) * self.pool.page * self.kv_heads * 128 * 2 * 2 * self.L
+
+    def _table(self, rows: Dict[int, List[int]]) -> np.ndarray:
+        table = np.full((self.slots, max([1] + [len(p) for p in rows.values()])), -1, dtype=np.int64)
+        for i, pages in rows.items():
+            table[i, :len(pages)] = pages
+        return table
+
+    # ----------------------------------------------------------------------- steps
+    def step(self, stack: Stack, bitvec, tokens: Dict[int, torch.Tensor]) -> Dict[int, torch.Tensor]:
+        """tokens: for some slots the hidden states of their next tokens, fp16 [n, hidden] (one token, or a chunk of a prompt).
+        Returns the last block's output for each.  Nothing is changed if the pages do not suffice."""
+        order = sorted(tokens)
+        if not order:
+            return {}
+        rows = {i: tokens[i].shape[0] for i in order}
+        for i in order:
+            s = self.seqs[i]
+            if rows[i] == 0:
+                raise ValueError(f"slot {i}: no tokens")
+            if s.position + rows[i] > self.max_positions:
+                raise FqError(-2, f"slot {i}: position {s.position + rows[i]} of {self.max_positions}")
+        more = {i: self.pool.need(self.seqs[i].length + rows[i]) - len(self.seqs[i].pages) for i in order}
+        if sum(more.values()) > self.pool.free:
+            raise MemoryError(f"{sum(more.values())} pages needed, {self.pool.free} free of {self.pool.pages}")
+        for i in order:
+            self.seqs[i].pages += self.pool.take(more[i])
+            self.seqs[i].length += rows[i]
+        positions = [np.arange(self.seqs[i].position, self.seqs[i].position + rows[i]) for i in order]
+        batch = PagedBatch([rows.get(i, 0) for i in range(self.slots)],
+                           [self.seqs[i].length if i in self.seqs else 0 for i in range(self.slots)],
+                           self._table({i: s.pages for i, s in self.seqs.items()}), self.pool.page, self.pool.pages,
+                           positions=np.concatenate(positions), device=self.device)
+        x = torch.cat([tokens[i] for i in order])
+        bitvec = np.asarray(bitvec, dtype=np.uint8).reshape(self.L, 7)
+        for l in range(self.L):
+            w = [stack.layers[l][j][int(bitvec[l, j])] for j in range(7)]
+            q_gain, k_gain = self.gains[l] if self.gains is not None else (None, None)
+            acc = None if self.weights is None else self.weights[l]
+            u = fq_glue(0, x)
+            q, k, v = (fq_qlinear(u, w[j]) for j in range(3))
+            q = fq_qk_norm_rope(q, k, v, batch, self.rope, self.k[l], self.v[l], q_gain, k_gain, out=q)
+            a = fq_attn_paged(q, batch, self.k[l], self.v[l], weights=acc, weights_out=acc)
+            x1 = fq_glue(2, x, fq_qlinear(a, w[3]))
+            u = fq_glue(0, x1)
+            m = fq_glue(5, fq_qlinear(u, w[4]), fq_qlinear(u, w[5]))
+            x = fq_glue(2, x1, fq_qlinear(m, w[6]))
+        for i in order:
+            self.seqs[i].position += rows[i]
+        if self.keep is not None:
+            self.cut([i for i in self.seqs if self.seqs[i].length > self.limit])
+        return dict(zip(order, torch.split(x, [rows[i] for i in order])))
+
+    def cut(self, slots: List[int]) -> List[int]:
+        """Cut these sequences to `keep` positions a head, into pages of their own; their old pages are free afterwards.  All at once
+        if the free pages hold the new rows of all, else one after the other.  Returns the slots for which there was no room:
+        they stay as they are, and the next step tries again."""
+        need = {i: self.pool.need(min(self.keep, self.seqs[i].length)) for i in slots}
+        if sum(need.values()) <= self.pool.free:
+            self._cut(slots)
+            return []
+        left = []
+        for i in slots:
+            if need[i] <= self.pool.free:
+                self._cut([i])
+            else:
+                left.append(i)
+        return left
+
+    def _cut(self, slots: List[int]) -> None:
+        if not slots:
+            return
+        batch = PagedBatch([0] * len(slots), [self.seqs[i].length for i in slots], self._table({n: self.seqs[i].pages for n, i in enumerate(slots)})
+                           [:len(slots)], self.pool.page, self.pool.pages, device=self.device)
+        new = [self.pool.take(self.pool.need(min(self.keep, self.seqs[i].length))) for i in slots]
+        dst = torch.from_numpy(self._table(dict(enumerate(new)))[:len(slots)].astype(np.int32)).to(self.device)
+        index = torch.tensor(slots, device=self.device)
+        for l in range(self.L):
+            kept = torch.zeros((len(slots), self.kv_heads, self.max_positions), dtype=torch.float32, device=self.device)
+            fq_cache_evict(batch, self.weights[l].index_select(0, index), self.k[l], self.v[l], dst, self.keep, self.recent, weights_out=kept)
+            self.weights[l].index_copy_(0, index, kept)
+        for i, pages in zip(slots, new):
+            s = self.seqs[i]
+            self.pool.give(s.pages)
+            s.pages, s.length = pages, min(self.keep, s.length)

@@ -307,6 +307,29 @@ def test_what_is_not_finite_stays_where_it_is_seen(fq, torch):
         assert np.isfinite(out[0][~sees]).all() and np.isfinite(out[1]).all()
 
 
+@pytest.mark.parametrize("heads, kv, n, S", [(4, 2, 1, 60), (4, 2, 5, 60), (2, 2, 16, 16), (4, 2, 20, 60), (8, 2, 150, 400), (4, 4, 200, 201), (2, 1, 70, 5000), (32, 16, 2048, 2048)])
+def test_values_that_are_not_finite(fq, torch, heads, kv, n, S):
+    """An infinite or NaN value reaches its dimension of the rows that see its position; rows ahead of it, whose weight is none, stay
+    as they are, and so do the other dimensions."""
+    rng = np.random.default_rng(61)
+    table, pages, k, v, q = case(rng, [(n, S)], heads, kv, 16)
+    b = fq.PagedBatch([n], [S], table, 16, pages)
+    clean = fq.fq_attn_paged(dev(torch, q), b, dev(torch, k), dev(torch, v)).cpu().numpy().reshape(n, heads, 128)
+    old = S - n
+    marks = [(t, h, d, x) for t, h, d, x in ((S - 1, 0, 3, np.inf), (old, 0, 4, -np.inf), (old + n // 2, kv - 1, 127, np.nan), (old // 2, 0, 64, np.inf),
+                                             (old + n // 3, kv - 1, 126, np.inf), (old + n // 2, kv - 1, 126, -np.inf))]
+    want = clean.copy()
+    for (t, h, d), x in {m[:3]: m[3] for m in marks}.items():  # of two at one place, as for one token, the last
+        v[table[0, t // 16], h, t % 16, d] = x
+        rows, group = np.arange(n) + old >= t, heads // kv
+        for g in range(h * group, (h + 1) * group):
+            want[rows, g, d] += np.float16(x)
+    got = fq.fq_attn_paged(dev(torch, q), b, dev(torch, k), dev(torch, v)).cpu().numpy().reshape(n, heads, 128)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want))
+    fine = np.isfinite(want)
+    assert np.array_equal(got[fine], clean[fine]) and np.array_equal(np.sign(got[np.isinf(want)]), np.sign(want[np.isinf(want)]))
+
+
 # ----------------------------------------------------------- norm, rotation, write
 @pytest.mark.parametrize("norm", [False, True])
 @pytest.mark.parametrize("heads, kv, page", [(1, 1, 16), (32, 32, 64), (40, 8, 32), (7, 1, 256)])
