@@ -122,7 +122,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     // two chunks meets every bank twice; afterwards the wavefronts' outputs
     __shared__ h8 Vs[4][32 * 16];
     __shared__ float ms[4][FEW], ls[4][FEW];
-    const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.x / p.kv_heads, split = blockIdx.y, begin = split * p.chunk;
+    const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.x / p.kv_heads;
+    // The last splits first: of sequences that differ in length only the longest have them, and the workgroups with nothing to do are over
+    // before the bulk (64 sequences of 17 to 4096 positions, caches cold: 51.4 -> 49.1 us).
+    const int split = (int)gridDim.y - 1 - (int)blockIdx.y, begin = split * p.chunk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // The pages of 64 blocks of sixteen positions, a lane each, asked for together with the lengths: one wait less ahead of the cache.
     const int *table = p.s.table + (size_t)b * p.s.table_stride;
@@ -347,9 +350,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     __shared__ h8 Vs0[KT * 16], Vs1[KT * 16];
     __shared__ __align__(8) unsigned short not_finite[2][4]; // of a value tile that not every row sees all of: rows with such a value, per wavefront that copied them
 
-    // Longest tiles first, dealt from both ends: workgroups b and b + half share a CU when there are two a CU.
+    // Longest tiles first; where all workgroups are resident together, two a CU, dealt from both ends: b and b + half share a CU.
     const int jobs = (int)gridDim.x, half = (jobs + 1) >> 1, bidx = (int)blockIdx.x;
-    const int job = bidx < half ? bidx : jobs - 1 - (bidx - half);
+    const int job = bidx < half || jobs * (int)gridDim.y > 512 ? bidx : jobs - 1 - (bidx - half);
     const int kvh = job % p.kv_heads, split = blockIdx.y;
     const RowTile tile = find_tile<TR>(p, p.tiles - 1 - job / p.kv_heads);
     if (tile.rows < 0)
