@@ -733,19 +733,28 @@ __global__ __launch_bounds__(256, 2) void attn_paged_weights_kernel(PagedAttnArg
     __shared__ __align__(16) float row_lse[2][WR];
     __shared__ __align__(16) int row_seen[2][WR];
     const int kvh = blockIdx.x % p.kv_heads, job = blockIdx.x / p.kv_heads, part = job % p.parts, t0 = job / p.parts * WK, b = blockIdx.y;
-    const SeqRange s = seq_range(p.s, b);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, h = lane >> 5, mine = t0 + 64 * wave; // first position of the wavefront
+    int page[2]; // of the lane's positions; asked for together with the lengths
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        page[i] = p.s.table[(size_t)b * p.s.table_stride + min((mine + 32 * i + col) >> p.s.page_log2, p.s.table_stride - 1)];
+    SeqRange s;
+    s.first = min(max(((const_ints)p.s.q_start)[b], 0), p.s.tokens);
+    s.n = min(max(((const_ints)p.s.q_start)[b + 1], s.first), p.s.tokens) - s.first;
+    s.len = min(max(((const_ints)p.s.seq_len)[b], 0), p.s.max_len);
     if (t0 >= s.len)
         return;
     int lo, hi;
     part_rows(p, s, t0, part, &lo, &hi);
     if (lo >= hi && p.parts > 1)
         return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 31, h = lane >> 5, older = s.len - s.n, mine = t0 + 64 * wave; // first position of the wavefront
-    h8 kk[2][8];
+    const int older = s.len - s.n;
+    h8 kk[2][8]; // positions behind the last one count for nothing: what their page holds is read where it has one, page 0 or the last where not
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const size_t at = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, b, min(mine + 32 * i + col, s.len - 1)) * PD;
+        const int t = mine + 32 * i + col, pg = min(max(page[i], 0), p.s.pages - 1);
+        const size_t at = ((((size_t)pg * p.kv_heads + kvh) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1))) * PD;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             kk[i][k] = *reinterpret_cast<const h8 *>(p.k + at + 16 * k + 8 * h);

@@ -423,9 +423,10 @@ def weights_like(rng, shape, kind):
 @pytest.mark.parametrize("kind", ["spread", "ties", "equal", "odd"])
 @pytest.mark.parametrize("page", [16, 64, 256])
 @pytest.mark.parametrize("keep, recent", [(1, 0), (1, 1), (16, 5), (100, 0), (100, 100), (333, 64), (1500, 7)])
-def test_evict(fq, torch, keep, recent, page, kind):
+@pytest.mark.parametrize("lengths", [[1, 0, 40, 100, 101, 1023, 1025, 2200], [1, 0, 63, 64, 65, 101, 334, 1000, 1024]], ids=["long", "short"])
+def test_evict(fq, torch, lengths, keep, recent, page, kind):
     rng = np.random.default_rng(keep + page)
-    kv, lengths = 3, [1, 0, 40, 100, 101, 1023, 1025, 2200]
+    kv = 3
     table, pages = deal(rng, lengths, page)
     k, v = pools(rng, pages, kv, page, table, lengths)
     k, v = np.nan_to_num(k), np.nan_to_num(v)
