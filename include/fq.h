@@ -446,7 +446,8 @@ int fq_prefill_forward(const fq_layer *layers, int L, const uint8_t *bitvec, con
  * states bounds for them.  What the arrays say beyond those bounds is cut to them, and a page number outside the pool is
  * taken for the nearest one inside: results are then wrong, but no access leaves the buffers.  Entries of the table behind
  * a sequence's last page are not used.  max_q and max_len decide how a call is divided (and with the sizes what workspace
- * it needs): state what the arrays hold, or what they will hold at most.
+ * it needs): state what the arrays hold, or what they will hold at most.  tokens * n_heads must be below 2^26, seqs * n_kv_heads
+ * below 2^23, and with column sums max_len * n_kv_heads below 2^28.
  */
 typedef struct {
     const int32_t *q_start; /* device [seqs + 1]: first token of every sequence; the last entry is tokens */
@@ -479,8 +480,9 @@ int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *
  * Attention of the batch's tokens over their sequences' pages, which hold the tokens' own keys and values already: token
  * i of the n of a sequence of S positions sees the positions t <= S - n + i, and per query head
  *   out = sum_t p[t] V[t],  p = softmax_t(scale * q . K[t]);  lse = log sum_t exp(scale * q . K[t])  (NULL: not wanted).
- * A row that sees nothing (n > S) is 0 with lse -inf.  q fp16, row m at m * ldq elements (a multiple of 8); out fp16
- * [tokens][n_heads * 128]; lse fp32 [tokens][n_heads].
+ * A row that sees nothing (n > S) is 0 with lse -inf; keys and values that are not finite reach the rows that see their
+ * position and no others.  q fp16, row m at m * ldq elements (a multiple of 8); out fp16 [tokens][n_heads * 128], not
+ * over q; lse fp32 [tokens][n_heads].
  * With weights_out (fp32 [seqs][n_kv_heads][weights_stride], else NULL), what every position has received is added up:
  *   weights_out[b][h][t] = (t < S - n ? weights[b][h][t] : 0) + sum of p[t] over the tokens and the query heads of h,
  * t < S; weights may be weights_out, or NULL for zeros.  Sums are taken in a fixed order.

@@ -783,9 +783,9 @@ int check_pool(const char *fn, int page, int pages, int n_kv_heads)
 
 int check_heads(const char *fn, int tokens, int n_heads, int n_kv_heads)
 {
-    if (n_kv_heads <= 0 || n_heads <= 0 || n_heads % n_kv_heads != 0 || (long long)tokens * n_heads > INT32_MAX / 4)
+    if (n_kv_heads <= 0 || n_heads <= 0 || n_heads % n_kv_heads != 0 || (long long)tokens * n_heads >= 1 << 26)
         return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d n_heads=%d n_kv_heads=%d (n_heads a multiple of n_kv_heads, tokens * n_heads "
-                       "below 2^29)", fn, tokens, n_heads, n_kv_heads);
+                       "below 2^26)", fn, tokens, n_heads, n_kv_heads);
     return FQ_OK;
 }
 
@@ -797,10 +797,18 @@ int check_batch(const char *fn, const fq_paged_batch *b, int n_kv_heads)
         return rc;
     if (b->seqs <= 0 || b->seqs > 65535 || b->tokens < 0 || b->max_q < 0 || b->max_q > b->tokens || (long long)b->max_q * b->seqs < b->tokens)
         return fq_fail(FQ_ERR_SHAPE, "%s: seqs=%d tokens=%d max_q=%d (need max_q <= tokens <= seqs * max_q)", fn, b->seqs, b->tokens, b->max_q);
+    if ((long long)b->seqs * n_kv_heads >= 1 << 23)
+        return fq_fail(FQ_ERR_SHAPE, "%s: seqs=%d n_kv_heads=%d (their product must be below 2^23)", fn, b->seqs, n_kv_heads);
     if (b->table_stride <= 0 || b->max_len < 0 || b->max_len > (1 << 24) || b->max_len > (long long)b->table_stride * b->page)
         return fq_fail(FQ_ERR_SHAPE, "%s: max_len=%d table_stride=%d (need max_len <= table_stride * page, at most 2^24)", fn, b->max_len,
                        b->table_stride);
     return FQ_OK;
+}
+
+bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
 }
 
 bool stride_ok(int ld, int width) { return ld >= width && ld % 8 == 0; }
@@ -822,11 +830,12 @@ extern "C" int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, c
         return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d n_heads=%d rope_rows=%d eps=%g", fn, tokens, n_heads, rope_rows, eps);
     if (!stride_ok(ldq, n_heads * 128) || !stride_ok(ldk, n_kv_heads * 128) || !stride_ok(ldv, n_kv_heads * 128))
         return fq_fail(FQ_ERR_SHAPE, "%s: ldq=%d ldk=%d ldv=%d (at least the row, multiples of 8)", fn, ldq, ldk, ldv);
-    if (q_out == q && ldq != n_heads * 128)
-        return fq_fail(FQ_ERR_SHAPE, "%s: q_out is q, whose rows are not contiguous", fn);
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(rope) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(q_out) ||
         !aligned16(k_pages) || !aligned16(v_pages))
         return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    const size_t row = (size_t)n_heads * 128 * 2;
+    if (tokens > 0 && !(q_out == q && (ldq == n_heads * 128 || tokens == 1)) && overlap(q, (size_t)(tokens - 1) * ldq * 2 + row, q_out, tokens * row))
+        return fq_fail(FQ_ERR_SHAPE, "%s: q_out overlaps q other than row by row", fn);
     if (tokens == 0)
         return FQ_OK;
     return check_hip(fq_launch_qk_norm_rope(q, ldq, k, ldk, v, ldv, tokens, n_heads, n_kv_heads, positions, slots, rope, rope_rows, q_gain, k_gain,
@@ -872,13 +881,17 @@ extern "C" int fq_attn_paged(const fq_paged_batch *batch, const void *q, int ldq
         return fq_fail(FQ_ERR_SHAPE, "%s: scale=%g (must be positive and finite)", fn, scale);
     if (weights && !weights_out)
         return fq_fail(FQ_ERR_NULL, "%s: weights without weights_out", fn);
-    if (weights_out && weights_stride < batch->max_len)
-        return fq_fail(FQ_ERR_SHAPE, "%s: weights_stride=%d below max_len=%d", fn, weights_stride, batch->max_len);
+    if (weights_out && (weights_stride < batch->max_len || (long long)batch->max_len * n_kv_heads >= 1 << 28))
+        return fq_fail(FQ_ERR_SHAPE, "%s: weights_stride=%d max_len=%d n_kv_heads=%d (need weights_stride >= max_len, max_len * n_kv_heads "
+                       "below 2^28)", fn, weights_stride, batch->max_len, n_kv_heads);
     const size_t need = fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, weights_out != nullptr);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fq_fail(FQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace))
         return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    const size_t row = (size_t)n_heads * 128 * 2;
+    if (batch->tokens > 0 && overlap(q, (size_t)(batch->tokens - 1) * ldq * 2 + row, out, batch->tokens * row))
+        return fq_fail(FQ_ERR_SHAPE, "%s: out overlaps q, which every part of the call reads", fn);
     return check_hip(fq_launch_attn_paged(*batch, q, ldq, n_heads, n_kv_heads, k_pages, v_pages, scale, out, lse, weights, weights_out,
                                           weights_stride, workspace, static_cast<fq_stream>(stream)), "fq_attn_paged launch");
 }

@@ -1056,9 +1056,10 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
             return rc;
         if (s.splits > 1) {
             const size_t items = (size_t)b.tokens * heads;
-            if (s.splits > 64) // more than a wavefront takes at once
+            // more than a wavefront takes at once; more than one of its turns (a grid has less than 2^32 threads)
+            if (s.splits > 64 && items < 1 << 22)
                 hipLaunchKernelGGL(attn_paged_merge_kernel<16>, dim3((unsigned)items), dim3(1024), 0, st, a, s.rows);
-            else if (s.splits > 8) // more than one of its turns
+            else if (s.splits > 8 && items < 1 << 24)
                 hipLaunchKernelGGL(attn_paged_merge_kernel<4>, dim3((unsigned)items), dim3(256), 0, st, a, s.rows);
             else
                 hipLaunchKernelGGL(attn_paged_merge_kernel<1>, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);

@@ -174,6 +174,9 @@ def test_rows_that_see_nothing_and_calls_without_tokens(fq, torch):
     rng = np.random.default_rng(5)
     run(fq, torch, rng, [(4, 0), (20, 3), (2, 1)], 8, 2, 16)
     run(fq, torch, rng, [(0, 33), (0, 0), (0, 200)], 8, 2, 16)
+    run(fq, torch, rng, [(3, 0), (1, 0)], 8, 2, 16)
+    run(fq, torch, rng, [(30, 0)], 8, 2, 16)
+    run(fq, torch, rng, [(0, 0)], 8, 2, 16)
 
 
 @pytest.mark.parametrize("scale, std", [(1.0, 1.0), (0.01, 3.0), (128 ** -0.5, 6.0)])
@@ -323,7 +326,8 @@ def test_values_that_are_not_finite(fq, torch, heads, kv, n, S):
         v[table[0, t // 16], h, t % 16, d] = x
         rows, group = np.arange(n) + old >= t, heads // kv
         for g in range(h * group, (h + 1) * group):
-            want[rows, g, d] += np.float16(x)
+            with np.errstate(invalid="ignore"):
+                want[rows, g, d] += np.float16(x)
     got = fq.fq_attn_paged(dev(torch, q), b, dev(torch, k), dev(torch, v)).cpu().numpy().reshape(n, heads, 128)
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want))
     fine = np.isfinite(want)
@@ -526,7 +530,7 @@ def test_refusals(fq, torch):
         with pytest.raises(ValueError):
             bad()
     for code, bad in ((-2, lambda: fq.fq_cache_evict(b, w, pool, pool, dst, 0, 0)), (-2, lambda: fq.fq_cache_evict(b, w, pool, pool, dst, 8, 9)),
-                      (-2, lambda: fq.fq_cache_evict(b, w, pool, pool, dst, 18, 2)), (-2, lambda: fq.fq_attn_paged(x, b, pool, pool, scale=0.0)),
+                      (-2, lambda: fq.fq_cache_evict(b, w, pool, pool, dst, 18, 2)), (-2, lambda: fq.fq_attn_paged(x, b, pool, pool, out=x)), (-2, lambda: fq.fq_attn_paged(x, b, pool, pool, scale=0.0)),
                       (-2, lambda: fq.fq_cache_evict(b, w, pool, pool, dst, 8, 2, weights_out=w))):
         with pytest.raises(fq.FqError) as e:
             bad()

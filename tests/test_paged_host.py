@@ -49,7 +49,7 @@ def test_batch_refuses_positions_of_another_length():
 
 
 def attn(lib, b, **c):
-    a = dict(q=16, ldq=256, heads=2, kv=2, k=16, v=16, scale=1.0, out=16, lse=None, weights=None, weights_out=None, stride=0,
+    a = dict(q=16, ldq=256, heads=2, kv=2, k=16, v=16, scale=1.0, out=1 << 20, lse=None, weights=None, weights_out=None, stride=0,
              ws=16, ws_bytes=1 << 30)
     a.update(c)
     return lib.fq_attn_paged(None if b is None else ctypes.byref(b), a["q"], a["ldq"], a["heads"], a["kv"], a["k"], a["v"], a["scale"], a["out"],
@@ -63,7 +63,10 @@ def attn(lib, b, **c):
     (-2, {"scale": float("inf")}, {}), (-2, {"weights_out": 16, "stride": 99}, {}), (-2, {}, {"seqs": 0}), (-2, {}, {"seqs": 65536}),
     (-2, {}, {"tokens": -1}), (-2, {}, {"max_q": 6}), (-2, {}, {"max_q": 2}), (-2, {}, {"max_len": 129}), (-2, {}, {"max_len": -1}), (-2, {}, {"max_len": (1 << 24) + 1, "table_stride": 1 << 21}),
     (-2, {}, {"table_stride": 0}), (-2, {}, {"page": 8}), (-2, {}, {"page": 48}), (-2, {}, {"page": 512}), (-2, {}, {"pages": 0}),
-    (-2, {}, {"pages": 1 << 27, "page": 16}), (-2, {"heads": 1 << 28, "kv": 1}, {"tokens": 3}), (-5, {"q": 8}, {}), (-5, {"k": 24}, {}),
+    (-2, {}, {"pages": 1 << 27, "page": 16}), (-2, {"heads": 1 << 25, "kv": 1}, {"tokens": 3}), (-2, {"kv": 1024, "heads": 1024}, {"seqs": 8192}),
+    (-2, {"kv": 64, "heads": 64, "ldq": 8192, "out": 1 << 30, "weights_out": 16, "stride": 1 << 22}, {"max_len": 1 << 22, "table_stride": 1 << 18}),
+    (-2, {"q": 4096, "out": 4096}, {}), (-2, {"q": 4096, "out": 4096 + 5 * 512 - 16}, {}), (-2, {"q": 4096, "out": 4096 - 5 * 512 + 16}, {}),
+    (-2, {"q": 4096, "ldq": 1024, "out": 4096 + 8192}, {}), (-5, {"q": 8}, {}), (-5, {"k": 24}, {}),
     (-5, {"v": 24}, {}), (-5, {"out": 8}, {}), (-6, {"ws": None, "weights_out": 16, "stride": 100}, {}),
     (-6, {"ws_bytes": 8, "weights_out": 16, "stride": 100}, {})], ids=str)
 def test_attention_refuses(code, call, changes):
@@ -100,7 +103,7 @@ def test_division_of_calls():
 
 def rope(lib, **c):
     a = dict(q=16, ldq=256, k=16, ldk=256, v=16, ldv=256, tokens=3, heads=2, kv=2, positions=16, slots=16, rope=16, rows=9, qg=None, kg=None,
-             eps=1e-5, out=32, kp=16, vp=16, page=16, pages=4)
+             eps=1e-5, out=1 << 20, kp=16, vp=16, page=16, pages=4)
     a.update(c)
     return lib.fq_qk_norm_rope(*a.values(), None)
 
@@ -108,7 +111,7 @@ def rope(lib, **c):
 @pytest.mark.parametrize("code, call", [(-1, {n: None}) for n in ("q", "k", "v", "positions", "slots", "rope", "out", "kp", "vp")] + [
     (-2, {"tokens": -1}), (-2, {"heads": 3}), (-2, {"heads": 0}), (-2, {"kv": 0}), (-2, {"rows": 0}), (-2, {"eps": -1.0}),
     (-2, {"eps": float("nan")}), (-2, {"ldq": 255}), (-2, {"ldk": 252}), (-2, {"ldv": 260}), (-2, {"page": 20}), (-2, {"pages": 0}),
-    (-2, {"out": 16, "ldq": 512}), (-5, {"q": 8}), (-5, {"k": 8}), (-5, {"v": 8}), (-5, {"rope": 8}), (-5, {"qg": 8}), (-5, {"kg": 8}),
+    (-2, {"out": 16, "ldq": 512}), (-2, {"out": 32}), (-2, {"q": 4096, "out": 4096 + 512}), (-2, {"q": 4096, "out": 4096 - 512}), (-5, {"q": 8}), (-5, {"k": 8}), (-5, {"v": 8}), (-5, {"rope": 8}), (-5, {"qg": 8}), (-5, {"kg": 8}),
     (-5, {"out": 40}), (-5, {"kp": 8}), (-5, {"vp": 8})], ids=str)
 def test_norm_rope_refuses(code, call):
     assert rope(fq._lib, **call) == code
