@@ -892,17 +892,69 @@ __global__ __launch_bounds__(256) void attn_paged_weights_join_kernel(PagedAttnA
     p.weights_out[at] = sum;
 }
 
-// The same where every sequence has at most sixteen rows: their scores are there already, and nothing is read twice but those.
+// The same where every sequence has at most sixteen rows: their scores are there already, and nothing is read twice but those.  With JOIN the
+// call has 2 to 8 splits, and their parts are joined here as well (in the order of the kernel above), a launch less: every workgroup forms the rows' lse from the splits' maxima
+// and sums, and the first of a sequence and head joins the outputs (24 sequences of 100 to 2048 positions, 40 heads: 11.6 -> 9.0 us).
+template <bool JOIN>
 __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnArgs p)
 {
     constexpr int PER = 4; // positions a thread
-    const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.y;
+    __shared__ float row_lse[FEW];
+    const int kvh = blockIdx.x % p.kv_heads, block = blockIdx.x / p.kv_heads, b = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const SeqRange s = seq_range(p.s, b);
-    const int rows = min(s.n * p.group, FEW), t0 = blockIdx.x / p.kv_heads * (256 * PER) + threadIdx.x;
+    const int rows = min(s.n * p.group, FEW), t0 = block * (256 * PER) + tid;
+    if (block * 256 * PER >= s.len && block > 0)
+        return;
+    const auto item_of = [&](int r) { return (size_t)(s.first + r / p.group) * p.heads + kvh * p.group + r % p.group; };
+    if (JOIN && s.len > p.chunk) {
+        const size_t stride = (size_t)p.s.tokens * p.heads;
+        for (int r = wave; r < rows; r += 4) {
+            const size_t item = item_of(r);
+            const int live = (max(s.len - s.n + r / p.group + 1, 0) + p.chunk - 1) / p.chunk;
+            const f2 ml = reinterpret_cast<const f2 *>(p.part_ml)[item + min(lane, max(live - 1, 0)) * stride];
+            float mx = lane < live ? ml[0] : -INFINITY;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1)
+                mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+            const float w = lane < live ? __builtin_amdgcn_exp2f(ml[0] - (mx == -INFINITY ? 0.f : mx)) : 0.f;
+            float l = lane < live ? w * ml[1] : 0.f;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1)
+                l += __shfl_xor(l, d, 64);
+            const float lse = mx + log2f(l);
+            if (lane == 0)
+                row_lse[r] = lse;
+            if (block > 0)
+                continue;
+            const f2 *o = reinterpret_cast<const f2 *>(p.part_o) + item * (PD / 2) + lane;
+            float a0 = 0.f, a1 = 0.f;
+            for (int i = 0; i < live; i += 8) {
+                f2 v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) // those past the last one repeat it
+                    v[e] = o[min(i + e, live - 1) * stride * (PD / 2)];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (i + e < live) { // uniform
+                        const float we = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i + e));
+                        a0 = fmaf(we, v[e][0], a0);
+                        a1 = fmaf(we, v[e][1], a1);
+                    }
+            }
+            const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+            *reinterpret_cast<h2 *>(p.out + item * PD + 2 * lane) = h2{(_Float16)(a0 * inv), (_Float16)(a1 * inv)};
+            if (lane == 0)
+                p.lse[item] = lse * LN2;
+        }
+    } else if (tid < rows) {
+        row_lse[tid] = p.lse[item_of(tid)] * LOG2E;
+    }
+    __syncthreads();
     float sum[PER] = {};
     for (int r = 0; r < rows; ++r) {
-        const size_t item = (size_t)(s.first + r / p.group) * p.heads + kvh * p.group + r % p.group;
-        const float lse = p.lse[item] * LOG2E;
+        const size_t item = item_of(r);
+        const float lse = row_lse[r];
         if (lse == -INFINITY) // a row that sees nothing
             continue;
 #pragma unroll
@@ -1037,6 +1089,7 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     a.chunk = s.chunk;
     a.tiles = s.tiles;
     a.weights_stride = weights_stride;
+    const bool joined = weights_out && s.rows == FEW && s.splits > 1 && s.splits <= 8; // with the column sums
     if (b.tokens > 0) {
         const dim3 grid(s.tiles * kv_heads, s.splits);
         if (s.rows == FEW && weights_out)
@@ -1054,7 +1107,7 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
         int rc = (int)hipGetLastError();
         if (rc != 0)
             return rc;
-        if (s.splits > 1) {
+        if (s.splits > 1 && !joined) {
             const size_t items = (size_t)b.tokens * heads;
             // more than a wavefront takes at once; more than one of its turns (a grid has less than 2^32 threads)
             if (s.splits > 64 && items < 1 << 22)
@@ -1069,8 +1122,10 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     }
     if (weights_out && b.max_len > 0) {
         const auto grid = [&](int positions, int parts) { return dim3((unsigned)((b.max_len + positions - 1) / positions * parts * kv_heads), b.seqs); };
-        if (s.rows == FEW) {
-            hipLaunchKernelGGL(attn_paged_few_weights_kernel, grid(1024, 1), dim3(256), 0, st, a);
+        if (joined) {
+            hipLaunchKernelGGL(attn_paged_few_weights_kernel<true>, grid(1024, 1), dim3(256), 0, st, a);
+        } else if (s.rows == FEW) {
+            hipLaunchKernelGGL(attn_paged_few_weights_kernel<false>, grid(1024, 1), dim3(256), 0, st, a);
         } else {
             hipLaunchKernelGGL(attn_paged_weights_kernel, grid(WK, s.parts), dim3(256), 0, st, a);
             int rc = (int)hipGetLastError();
