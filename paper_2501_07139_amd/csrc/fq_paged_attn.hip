@@ -160,6 +160,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     float *scores = nullptr;
     if constexpr (SCORES)
         scores = p.scores + ((size_t)(first + token) * p.heads + head) * p.scores_stride + 4 * g;
+    // Read once, and past the caches' usual order of eviction: a token over 100003 positions 83.8 -> 75.6 us, with column sums of 24 sequences 70 -> 63.
     for (int t0 = begin + 32 * wave; t0 < end; t0 += 128) {
         const int block = (t0 - begin) >> 4; // of the split
         if ((block & 63) < 8 && block >= 64) // the wavefront's first step among the next 64 blocks
@@ -172,10 +173,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
             const _Float16 *k = p.k + at, *v = p.v + at;
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                kk[i][s] = *reinterpret_cast<const h8 *>(k + (col * PD + 32 * s + 8 * g));
+                kk[i][s] = __builtin_nontemporal_load(reinterpret_cast<const h8 *>(k + (col * PD + 32 * s + 8 * g)));
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                vv[i][s] = *reinterpret_cast<const h8 *>(v + ((4 * s + g) * PD + 8 * col));
+                vv[i][s] = __builtin_nontemporal_load(reinterpret_cast<const h8 *>(v + ((4 * s + g) * PD + 8 * col)));
         }
         f4 st[2];
 #pragma unroll
