@@ -26,7 +26,7 @@ struct PagedAttnArgs {
     float *weights_out;
     float *scores;            // [tokens][heads][scores_stride]: scaled scores of sequences of few rows; [parts][seqs][kv_heads][..]: parts of column sums
     float scale;              // times log2(e): scores are powers of 2
-    int scores_stride, parts, part_rows, ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride;
+    int scores_stride, parts, part_rows, ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride, packed;
 };
 
 // A tile of rows of one sequence and key/value head.
@@ -115,6 +115,35 @@ constexpr int FEW = 16;
 
 typedef const __attribute__((address_space(4))) int *const_ints; // read through the scalar cache; nothing writes them in these kernels
 
+// Sequence and split of workgroup `job` of a large grid whose sequences have several splits: those that there are come first, so that the
+// workgroups with nothing to do (sequences shorter than the longest) follow them (64 sequences of 17 to 4096 positions, caches cold: 48.0 -> 44.8 us).
+__device__ __forceinline__ bool find_split(const PagedAttnArgs &p, int job, int *b, int *split)
+{
+    const int lane = threadIdx.x & 63;
+    for (int i = 0, base = 0; i < p.s.seqs; i += 64) {
+        int count = 0;
+        if (i + lane < p.s.seqs) {
+            const SeqRange s = seq_range(p.s, i + lane);
+            count = s.n > 0 ? max((s.len + p.chunk - 1) / p.chunk, 1) : 0;
+        }
+        int upto = count;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o, 64);
+            upto += lane >= o ? v : 0;
+        }
+        const unsigned long long behind = __builtin_amdgcn_ballot_w64(base + upto > job);
+        if (behind) {
+            const int at = __builtin_ctzll(behind);
+            *b = i + at;
+            *split = job - base - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(count, at));
+            return true;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
 template <bool SCORES>
 __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
 {
@@ -122,10 +151,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     // two chunks meets every bank twice; afterwards the wavefronts' outputs
     __shared__ h8 Vs[4][32 * 16];
     __shared__ float ms[4][FEW], ls[4][FEW];
-    const int kvh = blockIdx.x % p.kv_heads, b = blockIdx.x / p.kv_heads;
-    // The last splits first: of sequences that differ in length only the longest have them, and the workgroups with nothing to do are over
-    // before the bulk (64 sequences of 17 to 4096 positions, caches cold: 51.4 -> 49.1 us).
-    const int split = (int)gridDim.y - 1 - (int)blockIdx.y, begin = split * p.chunk;
+    const int kvh = blockIdx.x % p.kv_heads;
+    int b = blockIdx.x / p.kv_heads, split = blockIdx.y;
+    if (p.packed && !find_split(p, b, &b, &split))
+        return;
+    const int begin = split * p.chunk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // The pages of 64 blocks of sixteen positions, a lane each, asked for together with the lengths: one wait less ahead of the cache.
     const int *table = p.s.table + (size_t)b * p.s.table_stride;
@@ -1092,7 +1122,9 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     a.weights_stride = weights_stride;
     const bool joined = weights_out && s.rows == FEW && s.splits > 1 && s.splits <= 8; // with the column sums
     if (b.tokens > 0) {
-        const dim3 grid(s.tiles * kv_heads, s.splits);
+        const long long jobs = (long long)s.tiles * kv_heads;
+        a.packed = s.rows == FEW && b.seqs > 1 && s.splits > 1 && jobs * s.splits > 768 && jobs * s.splits < 1 << 24; // more than are resident together
+        const dim3 grid((unsigned)(jobs * (a.packed ? s.splits : 1)), a.packed ? 1 : s.splits);
         if (s.rows == FEW && weights_out)
             hipLaunchKernelGGL(attn_paged_few_kernel<true>, grid, dim3(256), 0, st, a);
         else if (s.rows == FEW)
