@@ -508,8 +508,8 @@ int fq_attn_paged_route(const fq_paged_batch *batch, int n_heads, int n_kv_heads
  * seq_len, table, pages of the batch: where to copy from (its tokens do not matter).  weights fp32
  * [seqs][n_kv_heads][weights_stride].  dst_table int32 [seqs][dst_stride], pages of k_out and v_out (dst_pages of them;
  * they may be k_pages and v_pages, the pages other ones than are read).  kept int32 [seqs][n_kv_heads][keep], written:
- * the positions that stay, then -1.  new_len int32 [seqs], written.  weights_out fp32
- * [seqs][n_kv_heads][weights_out_stride], written: the weights of what stays; NULL: not wanted; not `weights` itself.
+ * the positions that stay, then -1.  new_len int32 [seqs], written, not over seq_len.  weights_out fp32
+ * [seqs][n_kv_heads][weights_out_stride], written: the weights of what stays; NULL: not wanted; not over `weights`.
  */
 int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void *v_pages, int n_kv_heads,
                    const float *weights, int weights_stride, int keep, int recent, const int32_t *dst_table,

@@ -905,8 +905,6 @@ extern "C" int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, 
         return rc;
     if (!k_pages || !v_pages || !weights || !dst_table || !k_out || !v_out || !kept || !new_len)
         return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
-    if (weights_out == weights)
-        return fq_fail(FQ_ERR_SHAPE, "%s: weights_out must not be weights", fn);
     if (keep <= 0 || keep > (1 << 30) || recent < 0 || recent > keep)
         return fq_fail(FQ_ERR_SHAPE, "%s: keep=%d recent=%d (need 0 <= recent <= keep, 0 < keep)", fn, keep, recent);
     if (int rc = check_pool(fn, batch->page, dst_pages, n_kv_heads))
@@ -918,6 +916,12 @@ extern "C" int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, 
                        weights_out_stride, dst_stride, batch->max_len, most);
     if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_out) || !aligned16(v_out))
         return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    const size_t rows = (size_t)batch->seqs * n_kv_heads - 1;
+    if (weights_out && (weights_out == weights || overlap(weights, (rows * weights_stride + batch->max_len) * 4, weights_out,
+                                                          (rows * weights_out_stride + most) * 4)))
+        return fq_fail(FQ_ERR_SHAPE, "%s: weights_out must not be weights", fn);
+    if (overlap(batch->seq_len, (size_t)batch->seqs * 4, new_len, (size_t)batch->seqs * 4))
+        return fq_fail(FQ_ERR_SHAPE, "%s: new_len must not be seq_len", fn);
     return check_hip(fq_launch_cache_evict(*batch, k_pages, v_pages, n_kv_heads, weights, weights_stride, keep, recent, dst_table, dst_stride,
                                            dst_pages, k_out, v_out, kept, new_len, weights_out, weights_out_stride,
                                            static_cast<fq_stream>(stream)), "fq_cache_evict launch");

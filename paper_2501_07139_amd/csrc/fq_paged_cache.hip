@@ -81,7 +81,7 @@ struct EvictArgs {
     const int *dst_table;
     int *kept, *new_len;
     float *weights_out;
-    int kv_heads, weights_stride, weights_out_stride, keep, recent, dst_stride, dst_pages;
+    int kv_heads, weights_stride, weights_out_stride, keep, recent, dst_stride, dst_pages, share;
 };
 
 constexpr int SEL = 1024, HELD = 16;             // threads; weights a thread keeps in registers: 16384 positions are read once
@@ -248,89 +248,6 @@ __global__ __launch_bounds__(SEL) void evict_select_kernel(EvictArgs p)
         kept[t] = -1;
 }
 
-// The same for up to 1024 positions with one wavefront, which needs no barriers and no reads of others' counts: digits of eight bits, 16 keys a lane.
-// Bound by latency (the length, then the weights, then about 250 clocks a digit): one sequence of 611 positions and 32 heads 9.8 -> 5.0 us.
-constexpr int SMALL = 16; // keys a lane
-
-__global__ __launch_bounds__(64) void evict_select_small_kernel(EvictArgs p)
-{
-    __shared__ __align__(16) int hist[256];
-    const int head = blockIdx.x, b = blockIdx.y, lane = threadIdx.x;
-    const int len = min(min(max(p.s.seq_len[b], 0), p.s.max_len), 64 * SMALL);
-    const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
-    const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
-    int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
-    float *wo = p.weights_out ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
-    if (head == 0 && lane == 0)
-        p.new_len[b] = m;
-    float held[SMALL];
-    uint32_t key[SMALL];
-#pragma unroll
-    for (int i = 0; i < SMALL; ++i)
-        if (64 * i < len) // uniform, here and below
-            held[i] = w[min(64 * i + lane, len - 1)];
-#pragma unroll
-    for (int i = 0; i < SMALL; ++i)
-        if (64 * i < len)
-            key[i] = weight_key(held[i]);
-    const bool all = need >= old, none = need <= 0;
-    uint32_t prefix = 0;
-    int left = need;
-    if (!all && !none) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            *reinterpret_cast<int4 *>(&hist[4 * lane]) = int4{0, 0, 0, 0};
-            __builtin_amdgcn_wave_barrier();
-            const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-#pragma unroll
-            for (int i = 0; i < SMALL; ++i)
-                if (64 * i < old) {
-                    if (64 * i + lane < old && (key[i] & mask) == prefix)
-                        atomicAdd(&hist[(key[i] >> shift) & 255], 1);
-                }
-            __builtin_amdgcn_wave_barrier();
-            const int4 h = *reinterpret_cast<const int4 *>(&hist[252 - 4 * lane]); // four digits a lane, from the highest down
-            const int count[4] = {h.w, h.z, h.y, h.x};
-            int above = lanes_upto(h.x + h.y + h.z + h.w) - (h.x + h.y + h.z + h.w), digit = -1, rest = 0, size = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (above < left && left <= above + count[i]) { // one lane and digit
-                    digit = 255 - 4 * lane - i;
-                    rest = left - above;
-                    size = count[i];
-                }
-                above += count[i];
-            }
-            const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));
-            prefix |= (uint32_t)__builtin_amdgcn_readlane(digit, at) << shift;
-            left = __builtin_amdgcn_readlane(rest, at);
-            if (left == __builtin_amdgcn_readlane(size, at)) { // all of them: what is at least this prefix stays
-                prefix -= 1;
-                left = 0;
-                break;
-            }
-        }
-    }
-    const unsigned long long lower = (1ull << lane) - 1;
-    int gt_before = 0, eq_before = 0;
-#pragma unroll
-    for (int i = 0; i < SMALL; ++i)
-        if (64 * i < len) {
-            const int t = 64 * i + lane;
-            const bool gt = t < len && (t >= old || all || (!none && key[i] > prefix)), eq = t < old && !all && !none && key[i] == prefix;
-            const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
-            const int e = eq_before + (int)__popcll(eqs & lower), at = gt_before + (int)__popcll(gts & lower) + min(e, left);
-            if ((gt || (eq && e < left)) && at < m) {
-                kept[at] = t;
-                if (wo)
-                    wo[at] = held[i];
-            }
-            gt_before += (int)__popcll(gts);
-            eq_before += (int)__popcll(eqs);
-        }
-    for (int t = m + lane; t < p.keep; t += 64)
-        kept[t] = -1;
-}
-
 // Copies the rows that stay, in order, sixteen lanes a row of keys and its row of values.
 __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs p)
 {
@@ -345,6 +262,122 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs p)
     const h8 k = *reinterpret_cast<const h8 *>(p.k + from), v = *reinterpret_cast<const h8 *>(p.v + from);
     *reinterpret_cast<h8 *>(p.k_out + to) = k;
     *reinterpret_cast<h8 *>(p.v_out + to) = v;
+}
+
+// Selection for up to 1024 positions by one wavefront: no barriers, digits of eight bits, 16 keys a lane.  Bound by latency (the length, then the
+// weights, then about 250 clocks a digit).  With COPY, both steps in one launch: a workgroup selects for itself, though it copies only `share` of
+// the head's rows that stay.  That pays while heads are few (one sequence of 611 positions, 32 heads, 512 stay, caches cold: 14.0 -> 11.4 us; 4 sequences
+// of 800, 8 heads: 13.8 -> 11.8); at 512 heads and more the copy in a launch of its own does (64 sequences of 1000, 32 heads: 235 -> 222).
+constexpr int SMALL = 16, SHARES = 512; // keys a lane; heads from which on the copy is a launch of its own
+
+template <bool COPY>
+__global__ __launch_bounds__(COPY ? 256 : 64) void evict_small_kernel(EvictArgs p)
+{
+    __shared__ __align__(16) int hist[256];
+    __shared__ short stays[COPY ? 64 * SMALL : 1];
+    const int head = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+    const bool writes = blockIdx.x == 0; // what is written once a head
+    const int len = min(min(max(p.s.seq_len[b], 0), p.s.max_len), 64 * SMALL);
+    const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
+    const int j0 = COPY ? blockIdx.x * p.share : 0, j1 = COPY ? min(j0 + p.share, m) : 0;
+    if (!writes && j0 >= m)
+        return;
+    if (!COPY || tid < 64) {
+        const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
+        int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
+        float *wo = p.weights_out && writes ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
+        if (head == 0 && writes && lane == 0)
+            p.new_len[b] = m;
+        float held[SMALL];
+        uint32_t key[SMALL];
+#pragma unroll
+        for (int i = 0; i < SMALL; ++i)
+            if (64 * i < len) // uniform, here and below
+                held[i] = w[min(64 * i + lane, len - 1)];
+#pragma unroll
+        for (int i = 0; i < SMALL; ++i)
+            if (64 * i < len)
+                key[i] = weight_key(held[i]);
+        const bool all = need >= old, none = need <= 0;
+        uint32_t prefix = 0;
+        int left = need;
+        if (!all && !none) {
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                *reinterpret_cast<int4 *>(&hist[4 * lane]) = int4{0, 0, 0, 0};
+                __builtin_amdgcn_wave_barrier();
+                const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
+#pragma unroll
+                for (int i = 0; i < SMALL; ++i)
+                    if (64 * i < old) {
+                        if (64 * i + lane < old && (key[i] & mask) == prefix)
+                            atomicAdd(&hist[(key[i] >> shift) & 255], 1);
+                    }
+                __builtin_amdgcn_wave_barrier();
+                const int4 h = *reinterpret_cast<const int4 *>(&hist[252 - 4 * lane]); // four digits a lane, from the highest down
+                const int count[4] = {h.w, h.z, h.y, h.x};
+                int above = lanes_upto(h.x + h.y + h.z + h.w) - (h.x + h.y + h.z + h.w), digit = -1, rest = 0, size = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (above < left && left <= above + count[i]) { // one lane and digit
+                        digit = 255 - 4 * lane - i;
+                        rest = left - above;
+                        size = count[i];
+                    }
+                    above += count[i];
+                }
+                const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));
+                prefix |= (uint32_t)__builtin_amdgcn_readlane(digit, at) << shift;
+                left = __builtin_amdgcn_readlane(rest, at);
+                if (left == __builtin_amdgcn_readlane(size, at)) { // all of them: what is at least this prefix stays
+                    prefix -= 1;
+                    left = 0;
+                    break;
+                }
+            }
+        }
+        const unsigned long long lower = (1ull << lane) - 1;
+        int gt_before = 0, eq_before = 0;
+#pragma unroll
+        for (int i = 0; i < SMALL; ++i)
+            if (64 * i < len) {
+                const int t = 64 * i + lane;
+                const bool gt = t < len && (t >= old || all || (!none && key[i] > prefix)), eq = t < old && !all && !none && key[i] == prefix;
+                const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
+                const int e = eq_before + (int)__popcll(eqs & lower), at = gt_before + (int)__popcll(gts & lower) + min(e, left);
+                if ((gt || (eq && e < left)) && at < m) {
+                    if constexpr (COPY)
+                        stays[at] = (short)t;
+                    if (writes)
+                        kept[at] = t;
+                    if (wo)
+                        wo[at] = held[i];
+                }
+                gt_before += (int)__popcll(gts);
+                eq_before += (int)__popcll(eqs);
+            }
+        if (writes)
+            for (int t = m + lane; t < p.keep; t += 64)
+                kept[t] = -1;
+    }
+    if constexpr (COPY) {
+        __syncthreads();
+        for (int j = j0 + (tid >> 4); j < j1; j += 64) { // four rows a lane's sixteen at a time
+            h8 k[4], v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { // behind the last one that one again
+                const size_t from = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, head, b, stays[min(j + 16 * i, j1 - 1)]) * PD + 8 * (tid & 15);
+                k[i] = *reinterpret_cast<const h8 *>(p.k + from);
+                v[i] = *reinterpret_cast<const h8 *>(p.v + from);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j + 16 * i < j1) {
+                    const size_t to = pool_row(p.dst_table, p.dst_stride, p.s.page_log2, p.dst_pages, p.kv_heads, head, b, j + 16 * i) * PD + 8 * (tid & 15);
+                    *reinterpret_cast<h8 *>(p.k_out + to) = k[i];
+                    *reinterpret_cast<h8 *>(p.v_out + to) = v[i];
+                }
+        }
+    }
 }
 
 } // namespace
@@ -413,13 +446,20 @@ int fq_launch_cache_evict(const fq_paged_batch &batch, const void *k, const void
     a.recent = recent;
     a.dst_stride = dst_stride;
     a.dst_pages = dst_pages;
+    const int most = batch.max_len < keep ? batch.max_len : keep;
+    const long long heads = (long long)kv_heads * batch.seqs;
+    if (batch.max_len <= 64 * SMALL && heads < SHARES) {
+        const int shares = (int)(2 * SHARES / heads), even = (most + shares - 1) / shares;
+        a.share = even < 64 ? 64 : (even + 63) / 64 * 64; // four rows in flight for sixteen lanes
+        hipLaunchKernelGGL(evict_small_kernel<true>, dim3(most > a.share ? (most + a.share - 1) / a.share : 1, kv_heads, batch.seqs), dim3(256), 0, st, a);
+        return (int)hipGetLastError();
+    }
     if (batch.max_len <= 64 * SMALL)
-        hipLaunchKernelGGL(evict_select_small_kernel, dim3(kv_heads, batch.seqs), dim3(64), 0, st, a);
+        hipLaunchKernelGGL(evict_small_kernel<false>, dim3(1, kv_heads, batch.seqs), dim3(64), 0, st, a);
     else
         hipLaunchKernelGGL(evict_select_kernel, dim3(kv_heads, batch.seqs), dim3(SEL), 0, st, a);
     if (int rc = (int)hipGetLastError())
         return rc;
-    const int most = batch.max_len < keep ? batch.max_len : keep;
     if (most == 0)
         return 0;
     hipLaunchKernelGGL(evict_copy_kernel, dim3((most + 15) / 16, kv_heads, batch.seqs), dim3(256), 0, st, a);

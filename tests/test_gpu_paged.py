@@ -567,3 +567,30 @@ def test_both_ways_of_a_call(fq, torch, monkeypatch):
     assert taken == [("qk_norm_rope", 0), ("attn_paged", 0), ("cache_evict", 0)]
     for g, h in zip(*results):
         assert torch.equal(g, h)
+
+
+@pytest.mark.parametrize("seqs", [15, 16, 30], ids=lambda n: f"{n * 32}heads")
+def test_evict_of_many_heads(fq, torch, seqs):
+    """On both sides of the number of heads from which the copy is a launch of its own, at short lengths."""
+    rng = np.random.default_rng(seqs)
+    kv, page, keep, recent = 32, 16, 130, 17
+    lengths = [int(n) for n in rng.integers(0, 300, size=seqs)]
+    table, pages = deal(rng, lengths, page)
+    k, v = (rng.normal(size=(pages, kv, page, 128)).astype(np.float16) for _ in range(2))
+    w = weights_like(rng, (seqs, kv, 300), "ties")
+    dst, dst_pages = deal(rng, [min(S, keep) for S in lengths], page)
+    b = fq.PagedBatch([0] * seqs, lengths, table, page, pages)
+    dk, dv = dev(torch, k), dev(torch, v)
+    ko, vo = (torch.full((dst_pages, kv, page, 128), 9.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    wo = torch.full((seqs, kv, keep), -5.0, device="cuda")
+    kept, new_len = fq.fq_cache_evict(b, dev(torch, w), dk, dv, dev(torch, dst.astype(np.int32)), keep, recent, ko, vo, weights_out=wo)
+    kept, wo, ko, vo = (t.cpu().numpy() for t in (kept, wo, ko, vo))
+    assert new_len.tolist() == [min(S, keep) for S in lengths]
+    for i, S in enumerate(lengths):
+        m, K, V = min(S, keep), ref.rows_of(k, table[i], S), ref.rows_of(v, table[i], S)
+        at = np.arange(m)
+        for h in range(kv):
+            want = ref.evict(w[i, h, :S], keep, recent)
+            assert np.array_equal(kept[i, h, :m], want) and (kept[i, h, m:] == -1).all(), (S, h)
+            assert np.array_equal(wo[i, h, :m].view(np.int32), w[i, h, want].view(np.int32)) and (wo[i, h, m:] == -5).all()
+            assert np.array_equal(ko[dst[i, at // page], h, at % page], K[h, want]) and np.array_equal(vo[dst[i, at // page], h, at % page], V[h, want])

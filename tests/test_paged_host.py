@@ -167,3 +167,11 @@ def test_reference_eviction():
     assert paged_ref.evict(w, 3, 3).tolist() == [4, 5, 6]
     assert paged_ref.evict(w, 2, 0).tolist() == [3, 6]
     assert paged_ref.evict(w[:0], 2, 0).tolist() == []
+
+
+@pytest.mark.parametrize("call, changes", [({"new": 4096 + 4}, {"seq_len": 4096}), ({"new": 4096 - 4}, {"seq_len": 4096}),
+                                           ({"w": 4096, "wo": 4096 + 400 * 4 - 4, "wos": 40}, {}), ({"w": 4096, "wo": 4096 - 160 * 4 + 4, "wos": 40}, {})], ids=str)
+def test_evict_refuses_outputs_over_what_it_reads(call, changes):
+    """Two sequences of two heads: lengths of 8 bytes, weights of 3 * 100 + 100 floats, written ones of 3 * 40 + 40."""
+    assert evict(fq._lib, batch(**changes), **{"new": 1 << 20, "kept": 1 << 21, **call}) == -2
+    assert "must not be" in fq.fq_last_error()
