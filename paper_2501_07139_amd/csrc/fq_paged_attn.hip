@@ -914,11 +914,18 @@ __global__ __launch_bounds__(256) void attn_paged_weights_join_kernel(PagedAttnA
         return;
     const size_t at = ((size_t)b * p.kv_heads + kvh) * p.weights_stride + t;
     float sum = p.weights && t < s.len - s.n ? p.weights[at] : 0.f;
-    for (int part = 0; part < p.parts; ++part) {
-        int lo, hi;
-        part_rows(p, s, t / WK * WK, part, &lo, &hi);
-        if (lo < hi)
-            sum += p.scores[(((size_t)part * p.s.seqs + b) * p.kv_heads + kvh) * p.scores_stride + t];
+    // parts that have rows which see the 256 positions, eight loads at a time
+    const int part0 = max(t / WK * WK - (s.len - s.n), 0) * p.group / p.part_rows, part1 = min((s.n * p.group + p.part_rows - 1) / p.part_rows, p.parts);
+    const size_t stride = (size_t)p.s.seqs * p.kv_heads * p.scores_stride;
+    const float *from = p.scores + ((size_t)b * p.kv_heads + kvh) * p.scores_stride + t;
+    for (int part = part0; part < part1; part += 8) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = from[min(part + e, part1 - 1) * stride];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sum += part + e < part1 ? v[e] : 0.f;
     }
     p.weights_out[at] = sum;
 }
@@ -1005,12 +1012,12 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 
 // How a call is divided: one tile of up to sixteen rows a sequence, or tiles of 64 or 128, and the positions into splits.
 //
-// Single tokens: a step of 128 positions takes a workgroup 1.15 us, of which most is the wait for memory, until about 100 workgroups together
-// reach the rate of HBM; joining splits takes 3 us more, the launch.  So one split where that is no longer than a short one and the join (384
-// positions, or 1024 where sequences and heads fill the chip), else splits as short as keep the workgroups at about 384, but no longer than 512 positions, as
-// sequences differ in length.  Measured (us at splits of 128 / 256 / 512 / 1024 positions): 32 heads, 1000 positions 8.6 / 9.9 / 12.7 / 14.2, 4000
-// 20 / 17.7 / 16.9 / 20.7; 8 heads, 8000 positions 15.8 / 12.8 / 14 / 19; 64 sequences of 8 heads, 700 positions 35 / 35 / 35 / 29 (one split); 64 of 17
-// to 4096 (with the join) 41.7 / 38.2 / 38.7 / 42.1.
+// Single tokens: a step of 128 positions takes a workgroup 1.8 us, nearly all of it the wait for memory, until about 200 workgroups together reach the
+// rate of HBM; joining splits takes 3 us more, the launch.  So one split where that is no longer than short ones and the join (384 positions, and
+// more where sequences and heads fill the chip), else splits as short as keep the workgroups at about 384, but no longer than 512 positions, as
+// sequences differ in length.  Measured with caches cold (us at splits of 128 / 256 / 512 / 1024 positions / one split): 32 heads, 1000 positions
+// 10.3 / 12.0 / 15.2 / 19.3, 4000 19.2 / 17.7 / 17.1 / 24 / 65; 8 heads, 8000 positions 13.4 / 12.4 / 15.9 / 22.9 / 121; 16 sequences of 8 heads, 500
+// positions 13.0 / 13.0 / 12.4 (one), 1000 21.5 / 17.5 / 17.7 / 21.0 (one); 20 of 700 20.6 / 17.3 / 18.9 / 16.4 (one); 64 of 600 38 / 36 / 42 / 28 (one).
 //
 // Chunks: what an estimate (us) of these finds shortest, for tiles of 64 and 128 rows: 6 for the launch, the first loads and the end; a step of 64
 // positions takes a workgroup 0.69 (128 rows: 1.0) by itself, and 256 CUs together do one in 0.9 (1.36) each, as the card lowers its clock
@@ -1019,6 +1026,11 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 // long as the longest).  Some, as measured: 16 tokens, 8 key/value
 // heads of 4 queries, 16000 positions 171 in one split, 23.5 / 21.2 / 24.8 in splits of 1024 / 512 / 256; 2048 tokens of 32 heads 50 in tiles of 128 rows, 66
 // in tiles of 64; 1000 tokens 24.5 and 21.2.
+//
+// Column sums of chunks: into how many rows a workgroup's part goes, by an estimate too: 3.3 us and 1.8 a step of 64 rows for the longest one by itself, or
+// 4 and 2.5 for all of them on 512 places (two a CU); joining the parts 4.5, 0.05 a part, and a write and a read of them at 2 TB/s.  Over 25 sizes of
+// 60 to 2048 tokens and 200 to 30000 positions its choice takes 6 % longer than the best of twelve heights; parts of 512 rows (or what makes eight)
+// took 38 % longer: 223 and 53 tokens of one key/value head of 8 queries 31.9 -> 19.8 us with the attention, 500 tokens of 8 heads of 4 21.7 -> 11.2 without.
 struct AttnPlan {
     int rows, tiles, splits, chunk;
     size_t part_o, part_ml, lse, scores, end; // offsets in the workspace, in floats
@@ -1040,7 +1052,7 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
         s.tiles = b.seqs;
         const long long jobs = (long long)b.seqs * kv_heads;
         const auto pieces = [&](int chunk) { return jobs * ((b.max_len + chunk - 1) / chunk); };
-        const bool one = b.max_len <= 384 || (b.max_len <= 1024 && jobs >= 128);
+        const bool one = b.max_len <= (jobs >= 160 ? 1024 : jobs >= 128 ? 512 : 384);
         s.chunk = one ? (b.max_len + 127) / 128 * 128 : pieces(128) <= 384 ? 128 : pieces(256) <= 384 ? 256 : 512;
     } else {
         double best = 0;
@@ -1064,10 +1076,25 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
     s.splits = s.splits < 1 ? 1 : s.splits;
     const size_t parts = s.splits > 1 ? (size_t)s.splits * items : 0;
     s.scores_stride = (b.max_len + 31) / 32 * 32;
-    // parts of the rows for the column sums: 512 rows, or what makes eight parts
-    s.part_rows = longest > 8 * 512 ? (int)((longest + 8 * WR - 1) / (8 * WR) * WR) : 512;
-    s.parts = (int)((longest + s.part_rows - 1) / s.part_rows);
-    s.parts = s.parts < 1 ? 1 : s.parts;
+    s.parts = s.part_rows = 0;
+    if (weights && s.rows != FEW) {
+        const double blocks = (b.max_len + WK - 1) / WK, alike = (double)rows / longest * kv_heads; // sequences as long as the longest, times heads
+        const double part_seen = blocks - 0.5 * b.max_q / WK > 0.5 ? blocks - 0.5 * b.max_q / WK : 0.5; // blocks that a row is multiplied with
+        double best = 0;
+        for (long long height = WR; best == 0 || height < longest + WR; height += height < 512 ? WR : height / 4 / WR * WR) {
+            const long long parts = (longest + height - 1) / height;
+            if (parts > 8 && blocks * parts * kv_heads > 1 << 20) // the workspace, and the grid
+                continue;
+            const double groups = (parts > 1 ? part_seen * parts : blocks) * alike, steps = part_seen * longest / WR * alike + 0.5 * groups;
+            const double alone = 3.3 + (double)(height < longest ? height : longest) / WR * 1.8, together = (groups * 4 + steps * 2.5) / 512;
+            const double us = (alone > together ? alone : together) + (parts > 1 ? 4.5 + 0.05 * parts + parts * blocks * WK * alike * 8e-6 / 2 : 0);
+            if (best == 0 || us < best) {
+                best = us;
+                s.part_rows = (int)height;
+                s.parts = (int)parts;
+            }
+        }
+    }
     s.scores = 0; // what is a multiple of four floats first
     s.part_o = s.scores + (!weights ? 0 : s.rows == FEW ? items * s.scores_stride : s.parts > 1 ? (size_t)s.parts * b.seqs * kv_heads * s.scores_stride : 0);
     s.part_ml = s.part_o + parts * PD;

@@ -594,3 +594,10 @@ def test_evict_of_many_heads(fq, torch, seqs):
             assert np.array_equal(kept[i, h, :m], want) and (kept[i, h, m:] == -1).all(), (S, h)
             assert np.array_equal(wo[i, h, :m].view(np.int32), w[i, h, want].view(np.int32)) and (wo[i, h, m:] == -5).all()
             assert np.array_equal(ko[dst[i, at // page], h, at % page], K[h, want]) and np.array_equal(vo[dst[i, at // page], h, at % page], V[h, want])
+
+
+@pytest.mark.parametrize("seqs, heads, kv", [([(223, 250), (0, 40), (53, 90)], 8, 1), ([(700, 700)], 4, 1), ([(260, 1300), (17, 2000)], 32, 16),
+                                             ([(1, 300), (90, 20), (300, 301)], 14, 2)], ids=["parts", "prompt", "few-parts", "beyond"])
+def test_column_sums_in_parts(fq, torch, seqs, heads, kv):
+    """Parts of few rows, of sequences of other lengths than the longest; tokens ahead of the first position."""
+    run(fq, torch, np.random.default_rng(len(seqs) + heads), seqs, heads, kv, 32)
