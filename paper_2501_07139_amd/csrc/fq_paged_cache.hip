@@ -275,6 +275,7 @@ __global__ __launch_bounds__(COPY ? 256 : 64) void evict_small_kernel(EvictArgs 
 {
     __shared__ __align__(16) int hist[256];
     __shared__ short stays[COPY ? 64 * SMALL : 1];
+    __shared__ int page_of[2][COPY ? 64 : 1]; // pages read and written, of up to 1024 positions; asked for beside the selection
     const int head = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
     const bool writes = blockIdx.x == 0; // what is written once a head
     const int len = min(min(max(p.s.seq_len[b], 0), p.s.max_len), 64 * SMALL);
@@ -282,6 +283,11 @@ __global__ __launch_bounds__(COPY ? 256 : 64) void evict_small_kernel(EvictArgs 
     const int j0 = COPY ? blockIdx.x * p.share : 0, j1 = COPY ? min(j0 + p.share, m) : 0;
     if (!writes && j0 >= m)
         return;
+    if (COPY && tid >= 64 && tid < 192) {
+        const bool dst = tid >= 128;
+        const int page = dst ? p.dst_table[(size_t)b * p.dst_stride + min(lane, p.dst_stride - 1)] : p.s.table[(size_t)b * p.s.table_stride + min(lane, p.s.table_stride - 1)];
+        page_of[dst][lane] = min(max(page, 0), (dst ? p.dst_pages : p.s.pages) - 1);
+    }
     if (!COPY || tid < 64) {
         const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
         int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
@@ -361,18 +367,21 @@ __global__ __launch_bounds__(COPY ? 256 : 64) void evict_small_kernel(EvictArgs 
     }
     if constexpr (COPY) {
         __syncthreads();
+        const auto row_at = [&](int dst, int t) {
+            return (((((size_t)page_of[dst][t >> p.s.page_log2] * p.kv_heads + head) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * PD + 8 * (tid & 15);
+        };
         for (int j = j0 + (tid >> 4); j < j1; j += 64) { // four rows a lane's sixteen at a time
             h8 k[4], v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) { // behind the last one that one again
-                const size_t from = pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, head, b, stays[min(j + 16 * i, j1 - 1)]) * PD + 8 * (tid & 15);
+                const size_t from = row_at(0, stays[min(j + 16 * i, j1 - 1)]);
                 k[i] = *reinterpret_cast<const h8 *>(p.k + from);
                 v[i] = *reinterpret_cast<const h8 *>(p.v + from);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (j + 16 * i < j1) {
-                    const size_t to = pool_row(p.dst_table, p.dst_stride, p.s.page_log2, p.dst_pages, p.kv_heads, head, b, j + 16 * i) * PD + 8 * (tid & 15);
+                    const size_t to = row_at(1, j + 16 * i);
                     *reinterpret_cast<h8 *>(p.k_out + to) = k[i];
                     *reinterpret_cast<h8 *>(p.v_out + to) = v[i];
                 }
