@@ -264,106 +264,117 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs p)
     *reinterpret_cast<h8 *>(p.v_out + to) = v;
 }
 
-// Selection for up to 1024 positions by one wavefront: no barriers, digits of eight bits, 16 keys a lane.  Bound by latency (the length, then the
-// weights, then about 250 clocks a digit).  With COPY, both steps in one launch: a workgroup selects for itself, though it copies only `share` of
-// the head's rows that stay.  That pays while heads are few (one sequence of 611 positions, 32 heads, 512 stay, caches cold: 14.0 -> 11.4 us; 4 sequences
-// of 800, 8 heads: 13.8 -> 11.8); at 512 heads and more the copy in a launch of its own does (64 sequences of 1000, 32 heads: 235 -> 222).
-constexpr int SMALL = 16, SHARES = 512; // keys a lane; heads from which on the copy is a launch of its own
+// Selection for up to 1024 positions by four wavefronts, 256 positions each: digits of eight bits, counted in a part of LDS of their own so that a
+// digit takes one barrier, and every wavefront scans the counts for itself.  Bound by latency.  With COPY, both steps in one launch: a
+// workgroup selects for itself, though it copies only `share` of the head's rows that stay.  That pays while heads are few (one sequence of 611
+// positions, 32 heads, 512 stay, caches cold: 14.0 -> 11.4 us; 4 sequences of 800, 8 heads: 13.8 -> 11.8); at 512 heads and more the copy in a launch
+// of its own does (64 sequences of 1000, 32 heads: 235 -> 222).
+constexpr int SMALL = 4, SHARES = 512; // keys a thread; heads from which on the copy is a launch of its own
 
 template <bool COPY>
-__global__ __launch_bounds__(COPY ? 256 : 64) void evict_small_kernel(EvictArgs p)
+__global__ __launch_bounds__(256) void evict_small_kernel(EvictArgs p)
 {
-    __shared__ __align__(16) int hist[256];
-    __shared__ short stays[COPY ? 64 * SMALL : 1];
+    __shared__ __align__(16) int hist[4][256];
+    __shared__ int of_wave[4]; // what stays of a wavefront's positions: keys above the last one kept, equal ones in the upper half
+    __shared__ short stays[COPY ? 256 * SMALL : 1];
     __shared__ int page_of[2][COPY ? 64 : 1]; // pages read and written, of up to 1024 positions; asked for beside the selection
-    const int head = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+    const int head = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool writes = blockIdx.x == 0; // what is written once a head
-    const int len = min(min(max(p.s.seq_len[b], 0), p.s.max_len), 64 * SMALL);
+    const int len = min(min(max(p.s.seq_len[b], 0), p.s.max_len), 256 * SMALL);
     const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
     const int j0 = COPY ? blockIdx.x * p.share : 0, j1 = COPY ? min(j0 + p.share, m) : 0;
     if (!writes && j0 >= m)
         return;
-    if (COPY && tid >= 64 && tid < 192) {
-        const bool dst = tid >= 128;
-        const int page = dst ? p.dst_table[(size_t)b * p.dst_stride + min(lane, p.dst_stride - 1)] : p.s.table[(size_t)b * p.s.table_stride + min(lane, p.s.table_stride - 1)];
-        page_of[dst][lane] = min(max(page, 0), (dst ? p.dst_pages : p.s.pages) - 1);
+    const int t0 = 64 * SMALL * wave + lane; // the thread's first position
+    const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
+    float held[SMALL];
+#pragma unroll
+    for (int i = 0; i < SMALL; ++i)
+        held[i] = t0 + 64 * i < len ? w[t0 + 64 * i] : 0.f;
+    *reinterpret_cast<int4 *>(&hist[wave][4 * lane]) = int4{0, 0, 0, 0};
+    if (COPY && tid < 128) {
+        const int page = wave ? p.dst_table[(size_t)b * p.dst_stride + min(lane, p.dst_stride - 1)] : p.s.table[(size_t)b * p.s.table_stride + min(lane, p.s.table_stride - 1)];
+        page_of[wave][lane] = min(max(page, 0), (wave ? p.dst_pages : p.s.pages) - 1);
     }
-    if (!COPY || tid < 64) {
-        const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
-        int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
-        float *wo = p.weights_out && writes ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
-        if (head == 0 && writes && lane == 0)
-            p.new_len[b] = m;
-        float held[SMALL];
-        uint32_t key[SMALL];
+    uint32_t key[SMALL];
 #pragma unroll
-        for (int i = 0; i < SMALL; ++i)
-            if (64 * i < len) // uniform, here and below
-                held[i] = w[min(64 * i + lane, len - 1)];
+    for (int i = 0; i < SMALL; ++i)
+        key[i] = weight_key(held[i]);
+    const bool all = need >= old, none = need <= 0;
+    uint32_t prefix = 0;
+    int left = need; // how many of the keys that match the prefix so far are kept
+    __syncthreads();
+    if (!all && !none) { // the same in every thread, and so is the loop
+        for (int d = 0; d < 4; ++d) {
+            const int shift = 24 - 8 * d;
+            const uint32_t mask = d == 0 ? 0u : 0xffffffffu << (shift + 8);
 #pragma unroll
-        for (int i = 0; i < SMALL; ++i)
-            if (64 * i < len)
-                key[i] = weight_key(held[i]);
-        const bool all = need >= old, none = need <= 0;
-        uint32_t prefix = 0;
-        int left = need;
-        if (!all && !none) {
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                *reinterpret_cast<int4 *>(&hist[4 * lane]) = int4{0, 0, 0, 0};
-                __builtin_amdgcn_wave_barrier();
-                const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
+            for (int i = 0; i < SMALL; ++i)
+                if (t0 + 64 * i < old && (key[i] & mask) == prefix)
+                    atomicAdd(&hist[d][(key[i] >> shift) & 255], 1);
+            __syncthreads();
+            const int4 h = *reinterpret_cast<const int4 *>(&hist[d][252 - 4 * lane]); // four digits a lane, from the highest down
+            const int count[4] = {h.w, h.z, h.y, h.x};
+            int above = lanes_upto(h.x + h.y + h.z + h.w) - (h.x + h.y + h.z + h.w), digit = -1, rest = 0, size = 0;
 #pragma unroll
-                for (int i = 0; i < SMALL; ++i)
-                    if (64 * i < old) {
-                        if (64 * i + lane < old && (key[i] & mask) == prefix)
-                            atomicAdd(&hist[(key[i] >> shift) & 255], 1);
-                    }
-                __builtin_amdgcn_wave_barrier();
-                const int4 h = *reinterpret_cast<const int4 *>(&hist[252 - 4 * lane]); // four digits a lane, from the highest down
-                const int count[4] = {h.w, h.z, h.y, h.x};
-                int above = lanes_upto(h.x + h.y + h.z + h.w) - (h.x + h.y + h.z + h.w), digit = -1, rest = 0, size = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (above < left && left <= above + count[i]) { // one lane and digit
-                        digit = 255 - 4 * lane - i;
-                        rest = left - above;
-                        size = count[i];
-                    }
-                    above += count[i];
+            for (int i = 0; i < 4; ++i) {
+                if (above < left && left <= above + count[i]) { // one lane and digit
+                    digit = 255 - 4 * lane - i;
+                    rest = left - above;
+                    size = count[i];
                 }
-                const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));
-                prefix |= (uint32_t)__builtin_amdgcn_readlane(digit, at) << shift;
-                left = __builtin_amdgcn_readlane(rest, at);
-                if (left == __builtin_amdgcn_readlane(size, at)) { // all of them: what is at least this prefix stays
-                    prefix -= 1;
-                    left = 0;
-                    break;
-                }
+                above += count[i];
+            }
+            const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(digit >= 0));
+            prefix |= (uint32_t)__builtin_amdgcn_readlane(digit, at) << shift;
+            left = __builtin_amdgcn_readlane(rest, at);
+            if (left == __builtin_amdgcn_readlane(size, at)) { // all of them: what is at least this prefix stays (and not everything does, so it is not 0)
+                prefix -= 1;
+                left = 0;
+                break;
             }
         }
-        const unsigned long long lower = (1ull << lane) - 1;
-        int gt_before = 0, eq_before = 0;
+    }
+    // in order: a key above the last one kept stays, equal ones while they last
+    unsigned long long gts[SMALL], eqs[SMALL];
+    int found = 0;
 #pragma unroll
-        for (int i = 0; i < SMALL; ++i)
-            if (64 * i < len) {
-                const int t = 64 * i + lane;
-                const bool gt = t < len && (t >= old || all || (!none && key[i] > prefix)), eq = t < old && !all && !none && key[i] == prefix;
-                const unsigned long long gts = __builtin_amdgcn_ballot_w64(gt), eqs = __builtin_amdgcn_ballot_w64(eq);
-                const int e = eq_before + (int)__popcll(eqs & lower), at = gt_before + (int)__popcll(gts & lower) + min(e, left);
-                if ((gt || (eq && e < left)) && at < m) {
-                    if constexpr (COPY)
-                        stays[at] = (short)t;
-                    if (writes)
-                        kept[at] = t;
-                    if (wo)
-                        wo[at] = held[i];
-                }
-                gt_before += (int)__popcll(gts);
-                eq_before += (int)__popcll(eqs);
-            }
-        if (writes)
-            for (int t = m + lane; t < p.keep; t += 64)
-                kept[t] = -1;
+    for (int i = 0; i < SMALL; ++i) {
+        const int t = t0 + 64 * i;
+        gts[i] = __builtin_amdgcn_ballot_w64(t < len && (t >= old || all || (!none && key[i] > prefix)));
+        eqs[i] = __builtin_amdgcn_ballot_w64(t < old && !all && !none && key[i] == prefix);
+        found += (int)__popcll(gts[i]) | (int)__popcll(eqs[i]) << 16;
+    }
+    if (lane == 0)
+        of_wave[wave] = found;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        before += i < wave ? of_wave[i] : 0;
+    int gt_before = before & 0xffff, eq_before = before >> 16;
+    int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
+    float *wo = p.weights_out && writes ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
+    const unsigned long long lower = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < SMALL; ++i) {
+        const int e = eq_before + (int)__popcll(eqs[i] & lower), at = gt_before + (int)__popcll(gts[i] & lower) + min(e, left);
+        if (((gts[i] >> lane & 1) || ((eqs[i] >> lane & 1) && e < left)) && at < m) {
+            if constexpr (COPY)
+                stays[at] = (short)(t0 + 64 * i);
+            if (writes)
+                kept[at] = t0 + 64 * i;
+            if (wo)
+                wo[at] = held[i];
+        }
+        gt_before += (int)__popcll(gts[i]);
+        eq_before += (int)__popcll(eqs[i]);
+    }
+    if (writes) {
+        if (head == 0 && tid == 0)
+            p.new_len[b] = m;
+        for (int t = m + tid; t < p.keep; t += 256)
+            kept[t] = -1;
     }
     if constexpr (COPY) {
         __syncthreads();
@@ -457,14 +468,14 @@ int fq_launch_cache_evict(const fq_paged_batch &batch, const void *k, const void
     a.dst_pages = dst_pages;
     const int most = batch.max_len < keep ? batch.max_len : keep;
     const long long heads = (long long)kv_heads * batch.seqs;
-    if (batch.max_len <= 64 * SMALL && heads < SHARES) {
+    if (batch.max_len <= 256 * SMALL && heads < SHARES) {
         const int shares = (int)(2 * SHARES / heads), even = (most + shares - 1) / shares;
         a.share = even < 64 ? 64 : (even + 63) / 64 * 64; // four rows in flight for sixteen lanes
         hipLaunchKernelGGL(evict_small_kernel<true>, dim3(most > a.share ? (most + a.share - 1) / a.share : 1, kv_heads, batch.seqs), dim3(256), 0, st, a);
         return (int)hipGetLastError();
     }
-    if (batch.max_len <= 64 * SMALL)
-        hipLaunchKernelGGL(evict_small_kernel<false>, dim3(1, kv_heads, batch.seqs), dim3(64), 0, st, a);
+    if (batch.max_len <= 256 * SMALL)
+        hipLaunchKernelGGL(evict_small_kernel<false>, dim3(1, kv_heads, batch.seqs), dim3(256), 0, st, a);
     else
         hipLaunchKernelGGL(evict_select_kernel, dim3(kv_heads, batch.seqs), dim3(SEL), 0, st, a);
     if (int rc = (int)hipGetLastError())
