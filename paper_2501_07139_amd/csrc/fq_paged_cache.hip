@@ -71,8 +71,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeArgs p)
 
 // ------------------------------------------------------------------- eviction
 // Of a head's len positions the last `recent` stay, and of the others the keep - recent that weigh most (equal weights: the lower
-// position).  Selecting kernel, one workgroup per (sequence, head): the weight that the last one kept has is found eleven bits at a
-// time (radix selection over keys that order like the weights), then one pass in order numbers what stays.
+// position).  The weight that the last one kept has is found eight bits at a time (radix selection over keys that order like the weights), then
+// one pass in order numbers what stays.  Selecting is bound by latency: the length, the weights, a barrier and a scan of 256 counts a digit.  Each
+// wavefront has consecutive positions, few enough to stay in registers, and scans the counts for itself.
+//
+// Where a call has few heads, a head's rows that stay are dealt to several workgroups, each of which selects for itself and then copies its share:
+// one launch, the whole chip copying (caches cold, one launch against two: one sequence of 611 positions, 32 heads, 512 stay 11.4 against 14.0 us in the first
+// form of both and 8.8 now; 2000, 8 heads, half stay 8.7 / 10.0; 9000, 8 heads, 4096 stay 20.5 / 22.6).  Of many heads the copy is a launch of its own (64
+// sequences of 1000, 32 heads 235 / 222; 15 of 9000, 8 heads 129 / 114); level at 64 heads of 9000 positions and at 512 of up to 1024.
 struct EvictArgs {
     PagedSeqs s;
     const _Float16 *k, *v;
@@ -83,9 +89,6 @@ struct EvictArgs {
     float *weights_out;
     int kv_heads, weights_stride, weights_out_stride, keep, recent, dst_stride, dst_pages, share;
 };
-
-constexpr int SEL = 1024, HELD = 16;             // threads; weights a thread keeps in registers: 16384 positions are read once
-constexpr int DIGIT = 11, DIGITS = 1 << DIGIT; // three digits of a key, the last of ten bits
 
 // Larger weight, larger key; -0 and 0 alike; NaN above everything, as it says nothing against its position.
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -108,146 +111,6 @@ __device__ __forceinline__ int lanes_upto(int v)
     return v;
 }
 
-__global__ __launch_bounds__(SEL) void evict_select_kernel(EvictArgs p)
-{
-    constexpr int WAVES = SEL / 64;
-    __shared__ int hist[DIGITS];
-    __shared__ __align__(16) int wave_sum[WAVES];
-    __shared__ int found[3];
-    __shared__ uint32_t counts[HELD * WAVES]; // of a trip and wavefront: keys above the last one kept, equal ones in the upper half
-    const int head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int len = min(max(p.s.seq_len[b], 0), p.s.max_len);
-    const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
-    const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
-    int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
-    float *wo = p.weights_out ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
-    if (head == 0 && tid == 0)
-        p.new_len[b] = m;
-    float held[HELD];
-    uint32_t key[HELD];
-    auto load = [&](int t0) { // trips behind the last position are left out here and below (uniform)
-#pragma unroll
-        for (int i = 0; i < HELD; ++i)
-            if (t0 + SEL * i < len)
-                held[i] = w[min(t0 + SEL * i + tid, len - 1)];
-#pragma unroll
-        for (int i = 0; i < HELD; ++i)
-            if (t0 + SEL * i < len)
-                key[i] = weight_key(held[i]);
-    };
-    const bool once = len <= HELD * SEL; // uniform: the weights are read once
-    if (once)
-        load(0);
-    const bool all = need >= old, none = need <= 0;
-    uint32_t prefix = 0;
-    int left = need; // how many of the keys that match the prefix so far are kept
-    if (!all && !none) {
-        for (int shift = 32 - DIGIT; shift > -DIGIT; shift -= DIGIT) { // 21, 10, and the last ten bits
-            const int low = max(shift, 0), bits = DIGIT + min(shift, 0);
-            for (int d = tid; d < DIGITS; d += SEL)
-                hist[d] = 0;
-            __syncthreads();
-            const uint32_t mask = low + bits == 32 ? 0u : 0xffffffffu << (low + bits);
-            for (int t0 = 0; t0 < old; t0 += HELD * SEL) {
-                if (!once)
-                    load(t0);
-#pragma unroll
-                for (int i = 0; i < HELD; ++i)
-                    if (t0 + SEL * i < old) {
-                        if (t0 + SEL * i + tid < old && (key[i] & mask) == prefix)
-                            atomicAdd(&hist[(key[i] >> low) & ((1u << bits) - 1)], 1);
-                    }
-            }
-            __syncthreads();
-            // thread: two digits, from the highest down; keys of higher digits than these by a scan of the workgroup
-            const int d0 = DIGITS - 1 - 2 * tid, h0 = hist[d0], h1 = hist[d0 - 1];
-            const int upto = lanes_upto(h0 + h1);
-            if (lane == 63)
-                wave_sum[wave] = upto;
-            __syncthreads();
-            int above = upto - h0 - h1;
-#pragma unroll
-            for (int i = 0; i < WAVES; ++i)
-                above += i < wave ? wave_sum[i] : 0;
-            if (above < left && left <= above + h0) { // one thread and digit
-                found[0] = d0;
-                found[1] = left - above;
-                found[2] = h0;
-            } else if (above + h0 < left && left <= above + h0 + h1) {
-                found[0] = d0 - 1;
-                found[1] = left - above - h0;
-                found[2] = h1;
-            }
-            __syncthreads();
-            prefix |= (uint32_t)found[0] << low;
-            left = found[1];
-            if (left == found[2]) { // all of them: what is at least this prefix stays (and not everything does, so the prefix is not 0)
-                prefix -= 1;
-                left = 0;
-                break;
-            }
-        }
-    }
-    // in order: a key above the last one kept stays, equal ones while they last
-    int gt_before = 0, eq_before = 0;
-    for (int t0 = 0; t0 < len; t0 += HELD * SEL) {
-        if (!once)
-            load(t0);
-        unsigned long long gts[HELD], eqs[HELD];
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const int t = t0 + SEL * i + tid;
-            gts[i] = eqs[i] = 0;
-            if (t0 + SEL * i < len) {
-                gts[i] = __builtin_amdgcn_ballot_w64(t < len && (t >= old || all || (!none && key[i] > prefix)));
-                eqs[i] = __builtin_amdgcn_ballot_w64(t < old && !all && !none && key[i] == prefix);
-            }
-            if (lane == 0)
-                counts[WAVES * i + wave] = (uint32_t)__popcll(gts[i]) | (uint32_t)__popcll(eqs[i]) << 16;
-        }
-        __syncthreads();
-        if (tid < 64) { // sums ahead of every entry: four a lane, over the trips' wavefronts in order
-            static_assert(HELD * WAVES == 256 && HELD * SEL < 65536, "four entries a lane, sixteen bits a sum");
-            uint32_t c[4], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[i] = counts[4 * lane + i];
-                sum += c[i];
-            }
-            uint32_t ahead = (uint32_t)lanes_upto((int)sum) - sum;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                counts[4 * lane + i] = ahead;
-                ahead += c[i];
-            }
-            if (lane == 63)
-                found[0] = (int)ahead;
-        }
-        __syncthreads();
-        const unsigned long long lower = (1ull << lane) - 1;
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            if (t0 + SEL * i >= len)
-                continue;
-            const uint32_t ahead = counts[WAVES * i + wave];
-            const int gt = gt_before + (int)(ahead & 0xffffu) + (int)__popcll(gts[i] & lower);
-            const int eq = eq_before + (int)(ahead >> 16) + (int)__popcll(eqs[i] & lower);
-            const bool is_gt = gts[i] >> lane & 1, is_eq = eqs[i] >> lane & 1;
-            const int at = gt + min(eq, left);
-            if ((is_gt || (is_eq && eq < left)) && at < m) {
-                kept[at] = t0 + SEL * i + tid;
-                if (wo)
-                    wo[at] = held[i];
-            }
-        }
-        gt_before += found[0] & 0xffff;
-        eq_before += (int)((uint32_t)found[0] >> 16);
-        __syncthreads();
-    }
-    for (int t = m + tid; t < p.keep; t += SEL)
-        kept[t] = -1;
-}
-
 // Copies the rows that stay, in order, sixteen lanes a row of keys and its row of values.
 __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs p)
 {
@@ -264,42 +127,63 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs p)
     *reinterpret_cast<h8 *>(p.v_out + to) = v;
 }
 
-// Selection for up to 1024 positions by four wavefronts, 256 positions each: digits of eight bits, counted in a part of LDS of their own so that a
-// digit takes one barrier, and every wavefront scans the counts for itself.  Bound by latency.  With COPY, both steps in one launch: a
-// workgroup selects for itself, though it copies only `share` of the head's rows that stay.  That pays while heads are few (one sequence of 611
-// positions, 32 heads, 512 stay, caches cold: 14.0 -> 11.4 us; 4 sequences of 800, 8 heads: 13.8 -> 11.8); at 512 heads and more the copy in a launch
-// of its own does (64 sequences of 1000, 32 heads: 235 -> 222).
-constexpr int SMALL = 4, SHARES = 512; // keys a thread; heads from which on the copy is a launch of its own
+constexpr int share_rows(int waves) { return waves == 4 ? 64 : 128; } // the least rows of a share: what the workgroup's threads have in flight
 
-template <bool COPY>
-__global__ __launch_bounds__(256) void evict_small_kernel(EvictArgs p)
+// One workgroup selects among all positions of a head; WAVES wavefronts have up to K blocks of 64 consecutive positions each, whose weights stay in
+// registers (LONG: several rounds of them, read again for every digit).
+template <int WAVES, int K, bool COPY, bool LONG>
+__global__ __launch_bounds__(64 * WAVES) void evict_kernel(EvictArgs p)
 {
-    __shared__ __align__(16) int hist[4][256];
-    __shared__ int of_wave[4]; // what stays of a wavefront's positions: keys above the last one kept, equal ones in the upper half
-    __shared__ short stays[COPY ? 256 * SMALL : 1];
-    __shared__ int page_of[2][COPY ? 64 : 1]; // pages read and written, of up to 1024 positions; asked for beside the selection
+    // The first digit (sign and seven bits of the exponent) has few values, and additions to one place follow one another: where a workgroup has
+    // thousands of keys it is counted in eight places, by lane (16000 positions of a head 24.3 -> 19.2 us, 2000 of 8 heads 10.3 -> 10.0).
+    constexpr int THREADS = 64 * WAVES, ROUND = THREADS * K, PLACES = WAVES > 4 ? 8 : 1;
+    static_assert(ROUND <= 16384, "counts in halves of 32 bits, positions in 16");
+    __shared__ __align__(16) int hist[4][256], first_digit[PLACES > 1 ? 256 : 1][8];
+    __shared__ int of_wave[2][WAVES]; // what stays of a wavefront's positions: keys above the last one kept, equal ones in the upper half
+    __shared__ short stays[COPY ? ROUND : 1];
+    __shared__ int page_of[2][COPY ? ROUND / 16 : 1]; // pages read and written; asked for beside the selection
     const int head = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool writes = blockIdx.x == 0; // what is written once a head
-    const int len = min(min(max(p.s.seq_len[b], 0), p.s.max_len), 256 * SMALL);
+    const int most = min(max(p.s.seq_len[b], 0), p.s.max_len), len = LONG ? most : min(most, ROUND);
     const int m = min(len, p.keep), old = len - min(p.recent, m), need = m - (len - old);
     const int j0 = COPY ? blockIdx.x * p.share : 0, j1 = COPY ? min(j0 + p.share, m) : 0;
     if (!writes && j0 >= m)
         return;
-    const int t0 = 64 * SMALL * wave + lane; // the thread's first position
+    const int blocks = LONG || K <= 4 ? K : min((len + THREADS - 1) / THREADS, K); // of 64 positions a wavefront
+    const int first = 64 * blocks * wave + lane;
     const float *w = p.weights + ((size_t)b * p.kv_heads + head) * p.weights_stride;
-    float held[SMALL];
+    float held[K];
+    uint32_t key[K];
+    auto load = [&](int r0) {
 #pragma unroll
-    for (int i = 0; i < SMALL; ++i)
-        held[i] = t0 + 64 * i < len ? w[t0 + 64 * i] : 0.f;
-    *reinterpret_cast<int4 *>(&hist[wave][4 * lane]) = int4{0, 0, 0, 0};
-    if (COPY && tid < 128) {
-        const int page = wave ? p.dst_table[(size_t)b * p.dst_stride + min(lane, p.dst_stride - 1)] : p.s.table[(size_t)b * p.s.table_stride + min(lane, p.s.table_stride - 1)];
-        page_of[wave][lane] = min(max(page, 0), (wave ? p.dst_pages : p.s.pages) - 1);
-    }
-    uint32_t key[SMALL];
+        for (int i = 0; i < K; ++i)
+            if (i < blocks) {
+                const int t = r0 + first + 64 * i;
+                held[i] = t < len ? w[t] : 0.f;
+            }
+    };
+    auto keys = [&] {
 #pragma unroll
-    for (int i = 0; i < SMALL; ++i)
-        key[i] = weight_key(held[i]);
+        for (int i = 0; i < K; ++i)
+            key[i] = weight_key(held[i]);
+    };
+    if constexpr (!LONG)
+        load(0);
+    if (tid < 256)
+        *reinterpret_cast<int4 *>(&hist[tid >> 6][4 * lane]) = int4{0, 0, 0, 0};
+    if constexpr (PLACES > 1)
+        for (int i = tid; i < 512; i += THREADS)
+            *reinterpret_cast<int4 *>(&first_digit[i >> 1][4 * (i & 1)]) = int4{0, 0, 0, 0};
+    if constexpr (COPY)
+        for (int i = tid; i < ROUND / 8; i += THREADS) {
+            const int dst = i >= ROUND / 16, at = i & (ROUND / 16 - 1);
+            if (at << p.s.page_log2 >= ROUND)
+                continue;
+            const int page = dst ? p.dst_table[(size_t)b * p.dst_stride + min(at, p.dst_stride - 1)] : p.s.table[(size_t)b * p.s.table_stride + min(at, p.s.table_stride - 1)];
+            page_of[dst][at] = min(max(page, 0), (dst ? p.dst_pages : p.s.pages) - 1);
+        }
+    if constexpr (!LONG)
+        keys();
     const bool all = need >= old, none = need <= 0;
     uint32_t prefix = 0;
     int left = need; // how many of the keys that match the prefix so far are kept
@@ -308,11 +192,26 @@ __global__ __launch_bounds__(256) void evict_small_kernel(EvictArgs p)
         for (int d = 0; d < 4; ++d) {
             const int shift = 24 - 8 * d;
             const uint32_t mask = d == 0 ? 0u : 0xffffffffu << (shift + 8);
+            for (int r0 = 0; r0 < (LONG ? old : 1); r0 += ROUND) {
+                if constexpr (LONG) {
+                    load(r0);
+                    keys();
+                }
 #pragma unroll
-            for (int i = 0; i < SMALL; ++i)
-                if (t0 + 64 * i < old && (key[i] & mask) == prefix)
-                    atomicAdd(&hist[d][(key[i] >> shift) & 255], 1);
+                for (int i = 0; i < K; ++i)
+                    if (i < blocks) {
+                        if (r0 + first + 64 * i < old && (key[i] & mask) == prefix)
+                            atomicAdd(PLACES > 1 && d == 0 ? &first_digit[key[i] >> 24][lane & 7] : &hist[d][(key[i] >> shift) & 255], 1);
+                    }
+            }
             __syncthreads();
+            if (PLACES > 1 && d == 0) {
+                if (tid < 256) {
+                    const int4 x = *reinterpret_cast<const int4 *>(&first_digit[tid][0]), y = *reinterpret_cast<const int4 *>(&first_digit[tid][4]);
+                    hist[0][tid] = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+                }
+                __syncthreads();
+            }
             const int4 h = *reinterpret_cast<const int4 *>(&hist[d][252 - 4 * lane]); // four digits a lane, from the highest down
             const int count[4] = {h.w, h.z, h.y, h.x};
             int above = lanes_upto(h.x + h.y + h.z + h.w) - (h.x + h.y + h.z + h.w), digit = -1, rest = 0, size = 0;
@@ -336,68 +235,101 @@ __global__ __launch_bounds__(256) void evict_small_kernel(EvictArgs p)
         }
     }
     // in order: a key above the last one kept stays, equal ones while they last
-    unsigned long long gts[SMALL], eqs[SMALL];
-    int found = 0;
-#pragma unroll
-    for (int i = 0; i < SMALL; ++i) {
-        const int t = t0 + 64 * i;
-        gts[i] = __builtin_amdgcn_ballot_w64(t < len && (t >= old || all || (!none && key[i] > prefix)));
-        eqs[i] = __builtin_amdgcn_ballot_w64(t < old && !all && !none && key[i] == prefix);
-        found += (int)__popcll(gts[i]) | (int)__popcll(eqs[i]) << 16;
-    }
-    if (lane == 0)
-        of_wave[wave] = found;
-    __syncthreads();
-    int before = 0;
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-        before += i < wave ? of_wave[i] : 0;
-    int gt_before = before & 0xffff, eq_before = before >> 16;
     int *kept = p.kept + ((size_t)b * p.kv_heads + head) * p.keep;
     float *wo = p.weights_out && writes ? p.weights_out + ((size_t)b * p.kv_heads + head) * p.weights_out_stride : nullptr;
     const unsigned long long lower = (1ull << lane) - 1;
-#pragma unroll
-    for (int i = 0; i < SMALL; ++i) {
-        const int e = eq_before + (int)__popcll(eqs[i] & lower), at = gt_before + (int)__popcll(gts[i] & lower) + min(e, left);
-        if (((gts[i] >> lane & 1) || ((eqs[i] >> lane & 1) && e < left)) && at < m) {
-            if constexpr (COPY)
-                stays[at] = (short)(t0 + 64 * i);
-            if (writes)
-                kept[at] = t0 + 64 * i;
-            if (wo)
-                wo[at] = held[i];
+    int gt_rounds = 0, eq_rounds = 0, parity = 0; // of the rounds before
+    for (int r0 = 0; r0 < (LONG ? len : 1); r0 += ROUND, parity ^= 1) {
+        if constexpr (LONG) {
+            load(r0);
+            keys();
         }
-        gt_before += (int)__popcll(gts[i]);
-        eq_before += (int)__popcll(eqs[i]);
+        unsigned long long gts[K], eqs[K];
+        int found = 0;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int t = r0 + first + 64 * i;
+            gts[i] = eqs[i] = 0;
+            if (i < blocks) {
+                gts[i] = __builtin_amdgcn_ballot_w64(t < len && (t >= old || all || (!none && key[i] > prefix)));
+                eqs[i] = __builtin_amdgcn_ballot_w64(t < old && !all && !none && key[i] == prefix);
+                found += (int)__popcll(gts[i]) | (int)__popcll(eqs[i]) << 16;
+            }
+        }
+        if (lane == 0)
+            of_wave[parity][wave] = found;
+        __syncthreads();
+        int before = 0, whole = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            before += i < wave ? of_wave[parity][i] : 0;
+            whole += of_wave[parity][i];
+        }
+        int gt_before = gt_rounds + (before & 0xffff), eq_before = eq_rounds + (before >> 16);
+        gt_rounds += whole & 0xffff;
+        eq_rounds += whole >> 16;
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i < blocks) {
+                const int t = r0 + first + 64 * i, e = eq_before + (int)__popcll(eqs[i] & lower);
+                const int at = gt_before + (int)__popcll(gts[i] & lower) + min(e, left);
+                if (((gts[i] >> lane & 1) || ((eqs[i] >> lane & 1) && e < left)) && at < m) {
+                    if constexpr (COPY)
+                        stays[at] = (short)t;
+                    if (writes)
+                        kept[at] = t;
+                    if (wo)
+                        wo[at] = held[i];
+                }
+                gt_before += (int)__popcll(gts[i]);
+                eq_before += (int)__popcll(eqs[i]);
+            }
     }
     if (writes) {
         if (head == 0 && tid == 0)
             p.new_len[b] = m;
-        for (int t = m + tid; t < p.keep; t += 256)
+        for (int t = m + tid; t < p.keep; t += THREADS)
             kept[t] = -1;
     }
     if constexpr (COPY) {
+        constexpr int U = share_rows(WAVES) / (THREADS / 16); // rows that sixteen lanes have in flight
         __syncthreads();
         const auto row_at = [&](int dst, int t) {
             return (((((size_t)page_of[dst][t >> p.s.page_log2] * p.kv_heads + head) << p.s.page_log2) | (size_t)(t & ((1 << p.s.page_log2) - 1)))) * PD + 8 * (tid & 15);
         };
-        for (int j = j0 + (tid >> 4); j < j1; j += 64) { // four rows a lane's sixteen at a time
-            h8 k[4], v[4];
+        for (int j = j0 + (tid >> 4); j < j1; j += U * (THREADS / 16)) {
+            h8 k[U], v[U];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { // behind the last one that one again
-                const size_t from = row_at(0, stays[min(j + 16 * i, j1 - 1)]);
+            for (int i = 0; i < U; ++i) { // behind the last one that one again
+                const size_t from = row_at(0, stays[min(j + THREADS / 16 * i, j1 - 1)]);
                 k[i] = *reinterpret_cast<const h8 *>(p.k + from);
                 v[i] = *reinterpret_cast<const h8 *>(p.v + from);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (j + 16 * i < j1) {
-                    const size_t to = row_at(1, j + 16 * i);
+            for (int i = 0; i < U; ++i)
+                if (j + THREADS / 16 * i < j1) {
+                    const size_t to = row_at(1, j + THREADS / 16 * i);
                     *reinterpret_cast<h8 *>(p.k_out + to) = k[i];
                     *reinterpret_cast<h8 *>(p.v_out + to) = v[i];
                 }
         }
     }
+}
+
+// Whether the copy went with it.
+template <int WAVES, int K>
+bool launch_evict(EvictArgs &a, int most, int kv_heads, int seqs, fq_stream st)
+{
+    constexpr int MANY = WAVES == 4 ? 512 : 64, GROUPS = WAVES == 4 ? 1024 : 256; // heads; workgroups of the one launch, about
+    const long long heads = (long long)kv_heads * seqs;
+    if (heads >= MANY) {
+        hipLaunchKernelGGL((evict_kernel<WAVES, K, false, false>), dim3(1, kv_heads, seqs), dim3(64 * WAVES), 0, st, a);
+        return false;
+    }
+    const int shares = (int)(GROUPS / heads), even = (most + shares - 1) / shares, step = share_rows(WAVES);
+    a.share = even < step ? step : (even + step - 1) / step * step;
+    hipLaunchKernelGGL((evict_kernel<WAVES, K, true, false>), dim3(most > a.share ? (most + a.share - 1) / a.share : 1, kv_heads, seqs), dim3(64 * WAVES), 0, st, a);
+    return true;
 }
 
 } // namespace
@@ -467,20 +399,18 @@ int fq_launch_cache_evict(const fq_paged_batch &batch, const void *k, const void
     a.dst_stride = dst_stride;
     a.dst_pages = dst_pages;
     const int most = batch.max_len < keep ? batch.max_len : keep;
-    const long long heads = (long long)kv_heads * batch.seqs;
-    if (batch.max_len <= 256 * SMALL && heads < SHARES) {
-        const int shares = (int)(2 * SHARES / heads), even = (most + shares - 1) / shares;
-        a.share = even < 64 ? 64 : (even + 63) / 64 * 64; // four rows in flight for sixteen lanes
-        hipLaunchKernelGGL(evict_small_kernel<true>, dim3(most > a.share ? (most + a.share - 1) / a.share : 1, kv_heads, batch.seqs), dim3(256), 0, st, a);
-        return (int)hipGetLastError();
-    }
-    if (batch.max_len <= 256 * SMALL)
-        hipLaunchKernelGGL(evict_small_kernel<false>, dim3(1, kv_heads, batch.seqs), dim3(256), 0, st, a);
+    bool copied = false;
+    if (batch.max_len <= 1024)
+        copied = launch_evict<4, 4>(a, most, kv_heads, batch.seqs, st);
+    else if (batch.max_len <= 4096)
+        copied = launch_evict<16, 4>(a, most, kv_heads, batch.seqs, st);
+    else if (batch.max_len <= 16384)
+        copied = launch_evict<16, 16>(a, most, kv_heads, batch.seqs, st);
     else
-        hipLaunchKernelGGL(evict_select_kernel, dim3(kv_heads, batch.seqs), dim3(SEL), 0, st, a);
+        hipLaunchKernelGGL((evict_kernel<16, 16, false, true>), dim3(1, kv_heads, batch.seqs), dim3(1024), 0, st, a);
     if (int rc = (int)hipGetLastError())
         return rc;
-    if (most == 0)
+    if (copied || most == 0)
         return 0;
     hipLaunchKernelGGL(evict_copy_kernel, dim3((most + 15) / 16, kv_heads, batch.seqs), dim3(256), 0, st, a);
     return (int)hipGetLastError();

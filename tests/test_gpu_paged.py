@@ -601,3 +601,33 @@ def test_evict_of_many_heads(fq, torch, seqs):
 def test_column_sums_in_parts(fq, torch, seqs, heads, kv):
     """Parts of few rows, of sequences of other lengths than the longest; tokens ahead of the first position."""
     run(fq, torch, np.random.default_rng(len(seqs) + heads), seqs, heads, kv, 32)
+
+
+@pytest.mark.parametrize("lengths, kv, keep, recent", [
+    ([1025, 4096, 0, 17], 1, 2000, 100), ([4096, 3000, 1], 40, 700, 0), ([4097, 16384, 5, 9001], 2, 4100, 1000), ([9001, 5], 32, 2500, 64),
+    ([16385, 33000, 100], 2, 20000, 8)], ids=["up-to-4096", "up-to-4096-many", "up-to-16384", "up-to-16384-many", "beyond"])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd"])
+def test_evict_of_long_sequences(fq, torch, lengths, kv, keep, recent, kind):
+    """Every way that long sequences are selected in, few heads and many."""
+    rng = np.random.default_rng(keep)
+    page = 64
+    table, pages = deal(rng, lengths, page)
+    w = weights_like(rng, (len(lengths), kv, max(lengths) + 1), kind)
+    dst, dst_pages = deal(rng, [min(S, keep) for S in lengths], page)
+    b = fq.PagedBatch([0] * len(lengths), lengths, table, page, pages)
+    k, v = (torch.randn(pages, kv, page, 128, device="cuda").half() for _ in range(2))
+    ko, vo = (torch.full((dst_pages, kv, page, 128), 9.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    wo = torch.full((len(lengths), kv, keep), -5.0, device="cuda")
+    kept, new_len = fq.fq_cache_evict(b, dev(torch, w), k, v, dev(torch, dst.astype(np.int32)), keep, recent, ko, vo, weights_out=wo)
+    kept, wo = kept.cpu().numpy(), wo.cpu().numpy()
+    assert new_len.tolist() == [min(S, keep) for S in lengths]
+    for i, S in enumerate(lengths):
+        m = min(S, keep)
+        pg, d = (torch.from_numpy(t[i].astype(np.int64)).cuda() for t in (table, dst))
+        for h in range(kv):
+            want = ref.evict(w[i, h, :S], keep, recent)
+            assert np.array_equal(kept[i, h, :m], want) and (kept[i, h, m:] == -1).all(), (S, h)
+            assert np.array_equal(wo[i, h, :m].view(np.int32), w[i, h, want].view(np.int32)) and (wo[i, h, m:] == -5).all()
+            t, at = torch.from_numpy(want.astype(np.int64)).cuda(), torch.arange(m, device="cuda")
+            for src, out in ((k, ko), (v, vo)):
+                assert torch.equal(out[d[at // page], h, at % page], src[pg[t // page], h, t % page]), (S, h)
