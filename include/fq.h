@@ -446,7 +446,7 @@ int fq_prefill_forward(const fq_layer *layers, int L, const uint8_t *bitvec, con
  * states bounds for them.  What the arrays say beyond those bounds is cut to them, and a page number outside the pool is
  * taken for the nearest one inside: results are then wrong, but no access leaves the buffers.  Entries of the table behind
  * a sequence's last page are not used.  max_q and max_len decide how a call is divided (and with the sizes what workspace
- * it needs): state what the arrays hold, or what they will hold at most.  tokens * n_heads must be below 2^26, seqs * n_kv_heads
+ * it needs), positions and pairs help: state what the arrays hold, or what they will hold at most.  tokens * n_heads must be below 2^26, seqs * n_kv_heads
  * below 2^23, and with column sums max_len * n_kv_heads below 2^28.
  */
 typedef struct {
@@ -460,6 +460,8 @@ typedef struct {
     int table_stride;
     int page;               /* positions of a page */
     int pages;              /* pages of the pools */
+    int64_t positions;      /* of all sequences that have tokens, together, and */
+    int64_t pairs;          /* (token, position that it sees) pairs: guide how a call is divided, nothing else; 0: not known */
 } fq_paged_batch;
 
 /*

@@ -48,7 +48,7 @@ class fq_layer(ctypes.Structure):
 class fq_paged_batch(ctypes.Structure):
     _fields_ = [("q_start", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("table", ctypes.c_void_p), ("seqs", ctypes.c_int),
                 ("tokens", ctypes.c_int), ("max_q", ctypes.c_int), ("max_len", ctypes.c_int), ("table_stride", ctypes.c_int),
-                ("page", ctypes.c_int), ("pages", ctypes.c_int)]
+                ("page", ctypes.c_int), ("pages", ctypes.c_int), ("positions", ctypes.c_longlong), ("pairs", ctypes.c_longlong)]
 
 
 def _load() -> ctypes.CDLL:
@@ -696,7 +696,8 @@ class PagedBatch:
         self.seqs, self.tokens, self.page, self.pages = seqs, tokens, page, pages
         self.max_q, self.max_len, self.device = int(q_lens.max()), int(seq_lens.max()), self._all.device
         self.struct = fq_paged_batch(_dp(self.q_start), _dp(self.seq_len), _dp(self.table), seqs, tokens, self.max_q, self.max_len,
-                                     table.shape[1], page, pages)
+                                     table.shape[1], page, pages, int(seq_lens[q_lens > 0].sum()),
+                                     int((q_lens * (np.maximum(seq_lens - q_lens, 0)) + np.minimum(q_lens, seq_lens) ** 2 // 2).sum()))
 
 
 def _rows(t, width: int, what: str):

@@ -1026,7 +1026,10 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 //
 // Chunks: what an estimate (us) of these finds shortest, for tiles of 64 and 128 rows: 6 for the launch, the first loads and the end; a step of 64
 // positions takes a workgroup 0.69 (128 rows: 1.0) by itself, and 256 CUs together do one in 0.9 (1.36) each, as the card lowers its clock
-// under that load; joining splits takes 4 and two passes over the parts at 4 TB/s.  Over 37 sizes of 5 to 3000 tokens and 256
+// under that load; joining splits takes 4 and two passes over the parts at 4 TB/s.  Where the caller says how many positions and (token, position) pairs
+// several sequences have together, those are the steps and the parts, workgroups without work are 0.001 each, and the longest tile's steps count by 0.3 in
+// any case, as such tiles come late and alone: 300 tokens and 63 single ones, one of them at
+// the end of 32768 positions, 528 -> 109 us, and 500 with 15 at up to 16384 185 -> 65 (three of 67 tokens at most 13.6 -> 15.1, the worst of 17); without, all are taken to be half as long as the longest.  Over 37 sizes of 5 to 3000 tokens and 256
 // to 16000 positions its choice takes 1.8 % longer than the best of both heights and six lengths, at most 8 % (17 % where several sequences are all as
 // long as the longest).  Some, as measured: 16 tokens, 8 key/value
 // heads of 4 queries, 16000 positions 171 in one split, 23.5 / 21.2 / 24.8 in splits of 1024 / 512 / 256; 2048 tokens of 32 heads 50 in tiles of 128 rows, 66
@@ -1060,20 +1063,35 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
         const bool one = b.max_len <= (jobs >= 160 ? 1024 : jobs >= 128 ? 512 : 384);
         s.chunk = one ? (b.max_len + 127) / 128 * 128 : pieces(128) <= 384 ? 128 : pieces(256) <= 384 ? 256 : 512;
     } else {
-        double best = 0;
-        // steps of a tile, all splits together; several sequences are taken to be half as long as the longest
+        // steps of a tile, all splits together; several sequences are taken to be half as long as the longest where the caller does not say
         const double mean = (b.max_len > b.max_q ? b.max_len - 0.5 * b.max_q : 0.5 * b.max_len) / KT * (b.seqs > 1 ? 0.5 : 1.0) + 0.5;
-        for (int rows = 64; rows <= 128; rows *= 2)
-            for (int splits = 1; splits == 1 || b.max_len / splits > 128; splits *= 2) { // none shorter than 256 positions
-                const int chunk = ((b.max_len + splits - 1) / splits + 127) / 128 * 128;
-                const double alone = (double)chunk / KT * (rows == 64 ? 0.69 : 1.0), together = tiles(rows) * kv_heads * mean / 256 * (rows == 64 ? 0.9 : 1.36);
-                const double us = 6 + (alone > together ? alone : together) + (splits > 1 ? 4 + items * splits * 1040e-6 / 4 : 0);
-                if (best == 0 || us < best) {
-                    best = us;
-                    s.rows = rows;
-                    s.chunk = chunk;
+        const auto steps = [&](int height, bool known) {
+            if (!known)
+                return tiles(height) * mean;
+            const double full = (double)b.pairs * group / height, open = 1 - full / b.positions; // of a sequence's last tile
+            return (full + b.positions * (open > 0.5 ? open : 0.5)) / KT + 0.5 * tiles(height);
+        };
+        const auto choose = [&](int lowest, int highest, bool known) {
+            double best = 0;
+            for (int rows = lowest; rows <= highest; rows *= 2)
+                for (int splits = 1; splits == 1 || b.max_len / splits > 128; splits *= 2) { // none shorter than 256 positions
+                    const int chunk = ((b.max_len + splits - 1) / splits + 127) / 128 * 128;
+                    const double alone = (double)chunk / KT * (rows == 64 ? 0.69 : 1.0), together = steps(rows, known) * kv_heads / 256 * (rows == 64 ? 0.9 : 1.36);
+                    const double all = (double)items * splits, longer = (double)b.pairs * heads / chunk + items, parts = known && longer < all ? longer : all;
+                    if (known && splits > 1 && all > 1 << 20) // the workspace has room for every split of every row
+                        continue;
+                    const double us = 6 + (alone > together ? alone : together) + (splits > 1 ? 4 + parts * 1040e-6 / 4 : 0) +
+                                      (known ? 0.3 * alone + (splits > 1 ? 0.001 * tiles(rows) * kv_heads * splits : 0) : 0);
+                    if (best == 0 || us < best) {
+                        best = us;
+                        s.rows = rows;
+                        s.chunk = chunk;
+                    }
                 }
-            }
+        };
+        choose(64, 128, false);
+        if (b.seqs > 1 && b.positions > 0 && b.pairs > 0) // the height stays: it is set by the whole call's work
+            choose(s.rows, s.rows, true);
         s.tiles = (int)tiles(s.rows);
     }
     s.chunk = s.chunk < 128 ? 128 : s.chunk;

@@ -631,3 +631,14 @@ def test_evict_of_long_sequences(fq, torch, lengths, kv, keep, recent, kind):
             t, at = torch.from_numpy(want.astype(np.int64)).cuda(), torch.arange(m, device="cuda")
             for src, out in ((k, ko), (v, vo)):
                 assert torch.equal(out[d[at // page], h, at % page], src[pg[t // page], h, t % page]), (S, h)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("heads, kv", [(8, 2), (4, 4)])
+def test_chunk_beside_a_long_sequence(fq, torch, heads, kv, page):
+    """Splits that most sequences have nothing in."""
+    seqs = [(60, 60), (1, 5000), (1, 33), (0, 400), (2, 1), (9, 700)]
+    table, pages = deal(np.random.default_rng(0), [S for _, S in seqs], page)
+    b = fq.PagedBatch([n for n, _ in seqs], [S for _, S in seqs], table, page, pages)
+    assert fq.fq_attn_paged_route(b, heads, kv)[1] > 4
+    run(fq, torch, np.random.default_rng(heads), seqs, heads, kv, page)

@@ -175,3 +175,20 @@ def test_evict_refuses_outputs_over_what_it_reads(call, changes):
     """Two sequences of two heads: lengths of 8 bytes, weights of 3 * 100 + 100 floats, written ones of 3 * 40 + 40."""
     assert evict(fq._lib, batch(**changes), **{"new": 1 << 20, "kept": 1 << 21, **call}) == -2
     assert "must not be" in fq.fq_last_error()
+
+
+def test_division_of_sequences_of_other_lengths():
+    """Positions and pairs are those of the sequences with tokens; a chunk beside one long sequence is split, and known lengths do not change one sequence's call."""
+    b = fq.PagedBatch([1, 4, 0, 3], [17, 35, 400, 2], np.zeros((4, 25), dtype=np.int64), 16, 8, device="cpu")
+    assert b.struct.positions == 17 + 35 + 2 and b.struct.pairs == 16 + 31 * 4 + 8 + 2
+    lone = fq.PagedBatch([300] + [1] * 20, [300] + [200] * 19 + [30000], np.zeros((21, 1876), dtype=np.int64), 16, 8, device="cpu")
+    rows, splits, chunk = fq.fq_attn_paged_route(lone, 32, 8)
+    assert splits > 4 and (splits - 1) * chunk < 30000 <= splits * chunk
+    most = fq.fq_attn_paged_workspace_bytes(lone, 32, 8)
+    assert 0 < most < 1 << 30
+    lone.struct.positions = lone.struct.pairs = 0
+    assert fq.fq_attn_paged_route(lone, 32, 8)[0] == rows
+    one = fq.PagedBatch([300], [5000], np.zeros((1, 313), dtype=np.int64), 16, 8, device="cpu")
+    with_lengths = fq.fq_attn_paged_route(one, 32, 8)
+    one.struct.positions = one.struct.pairs = 0
+    assert fq.fq_attn_paged_route(one, 32, 8) == with_lengths
