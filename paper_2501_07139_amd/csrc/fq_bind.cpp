@@ -34,7 +34,7 @@ struct Entries {
     decltype(&fq_cache_evict) evict;
 } entry;
 
-PyObject *s_packed, *s_scales, *s_zeros, *s_n, *s_k, *s_bits, *s_struct, *s_positions, *s_slots;
+PyObject *s_packed, *s_scales, *s_zeros, *s_n, *s_k, *s_bits, *s_struct, *s_positions, *s_slots, *s_q_start, *s_seq_len, *s_table;
 
 // A contiguous device tensor of plain type, else nullptr.
 const at::Tensor *device_tensor(PyObject *o, at::ScalarType type)
@@ -253,8 +253,20 @@ bool float_of(PyObject *o, float *v)
     return true;
 }
 
-// The C structure of a PagedBatch.
-bool batch_of(PyObject *o, fq_paged_batch *b)
+// Whether an attribute is an int32 tensor on dev at this address.
+bool ints_at(PyObject *o, PyObject *name, c10::Device dev, const int32_t *at)
+{
+    PyObject *a = PyObject_GetAttr(o, name);
+    if (!a)
+        return false;
+    const at::Tensor *t = device_tensor(a, at::kInt);
+    const bool ok = t && t->device() == dev && t->data_ptr() == at;
+    Py_DECREF(a);
+    return ok;
+}
+
+// The C structure of a PagedBatch whose arrays are on dev: the structure itself has bare addresses, which may be the host's or another device's.
+bool batch_of(PyObject *o, c10::Device dev, fq_paged_batch *b)
 {
     PyObject *a = PyObject_GetAttr(o, s_struct);
     if (!a)
@@ -268,7 +280,7 @@ bool batch_of(PyObject *o, fq_paged_batch *b)
         PyBuffer_Release(&view);
     }
     Py_DECREF(a);
-    return ok;
+    return ok && ints_at(o, s_q_start, dev, b->q_start) && ints_at(o, s_seq_len, dev, b->seq_len) && ints_at(o, s_table, dev, b->table);
 }
 
 // None, or a contiguous device tensor of this type on dev.
@@ -341,7 +353,7 @@ PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) // q, k, v,
     return guarded(n, 12, [&](int *rc) {
         fq_paged_batch b;
         const at::Tensor *rope = device_tensor(a[4], at::kFloat), *out = device_tensor(a[10], at::kHalf);
-        if (!out || out->dim() != 2 || !shape_is(rope, {-1, 64, 2}) || rope->size(0) > INT_MAX || !batch_of(a[3], &b) || b.tokens == 0)
+        if (!out || out->dim() != 2 || !shape_is(rope, {-1, 64, 2}) || rope->size(0) > INT_MAX || !batch_of(a[3], out->device(), &b) || b.tokens == 0)
             return false;
         const c10::Device dev = out->device();
         const int64_t tokens = b.tokens, width = out->size(1);
@@ -375,7 +387,7 @@ PyObject *attn_paged(PyObject *, PyObject *const *a, Py_ssize_t n) // q, batch, 
     return guarded(n, 11, [&](int *rc) {
         fq_paged_batch b;
         const at::Tensor *out = device_tensor(a[5], at::kHalf), *ws = a[9] == Py_None ? nullptr : device_tensor(a[9], at::kByte);
-        if (!out || out->dim() != 2 || (!ws && a[9] != Py_None) || !batch_of(a[1], &b) || b.tokens == 0)
+        if (!out || out->dim() != 2 || (!ws && a[9] != Py_None) || !batch_of(a[1], out->device(), &b) || b.tokens == 0)
             return false;
         const c10::Device dev = out->device();
         const int64_t tokens = b.tokens, width = out->size(1);
@@ -418,7 +430,7 @@ PyObject *cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
                          *len = device_tensor(a[10], at::kInt);
         int keep, recent;
         void *stream;
-        if (!w || !dst || !kept || !len || !batch_of(a[0], &b) || !int_of(a[5], &keep) || !int_of(a[6], &recent) || !stream_of(a[12], &stream))
+        if (!w || !dst || !kept || !len || !batch_of(a[0], w->device(), &b) || !int_of(a[5], &keep) || !int_of(a[6], &recent) || !stream_of(a[12], &stream))
             return false;
         const c10::Device dev = w->device();
         const void *pk, *pv, *ko, *vo, *wout;
@@ -477,6 +489,9 @@ PyMODINIT_FUNC PyInit__bind()
     s_struct = PyUnicode_InternFromString("struct");
     s_positions = PyUnicode_InternFromString("positions");
     s_slots = PyUnicode_InternFromString("slots");
+    s_q_start = PyUnicode_InternFromString("q_start");
+    s_seq_len = PyUnicode_InternFromString("seq_len");
+    s_table = PyUnicode_InternFromString("table");
     PyObject *m = PyModule_Create(&module);
     if (m && PyModule_AddStringConstant(m, "torch_version", FQ_TORCH_VERSION) != 0) { // tensors are read by this version's layout
         Py_DECREF(m);

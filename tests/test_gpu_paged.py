@@ -642,3 +642,36 @@ def test_chunk_beside_a_long_sequence(fq, torch, heads, kv, page):
     b = fq.PagedBatch([n for n, _ in seqs], [S for _, S in seqs], table, page, pages)
     assert fq.fq_attn_paged_route(b, heads, kv)[1] > 4
     run(fq, torch, np.random.default_rng(heads), seqs, heads, kv, page)
+
+
+def test_batches_on_the_host_are_refused_with_and_without_outputs(fq, torch, monkeypatch):
+    """A batch whose arrays are host memory reaches no entry point, by either way; the entry points are replaced, so that nothing is launched."""
+    import ctypes
+
+    names = ("fq_qlinear_tile", "fq_qlinear_mixed", "fq_dense_f16", "fq_head_nll", "fq_token_nll", "fq_logit_l2", "fq_qk_norm_rope",
+             "fq_attn_paged", "fq_cache_evict")
+    reached = []
+    stubs = {n: ctypes.CFUNCTYPE(ctypes.c_int, *getattr(fq._lib, n).argtypes)(lambda *a, n=n: reached.append(n) or -2) for n in names[6:]}
+    real = [ctypes.cast(getattr(fq._lib, n), ctypes.c_void_p).value for n in names]
+    x, pool = (torch.zeros(s, dtype=torch.float16, device="cuda") for s in ((2, 256), (3, 2, 16, 128)))
+    rope, w = torch.zeros(32, 64, 2, device="cuda"), torch.zeros(2, 2, 20, device="cuda")
+    ws, out = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"), torch.zeros_like(x)
+    dst, kept, new_len = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((2, 1), (2, 2, 8), (2,)))
+    calls = (lambda b: fq.fq_qk_norm_rope(x, x, x, b, rope, pool, pool, out=out), lambda b: fq.fq_attn_paged(x, b, pool, pool, out=out, workspace=ws),
+             lambda b: fq.fq_attn_paged(x, b, pool, pool, out=out, weights_out=w, workspace=ws), lambda b: fq.fq_attn_paged(x, b, pool, pool),
+             lambda b: fq.fq_cache_evict(b, w, pool, pool, dst, 8, 2, kept=kept, new_len=new_len), lambda b: fq.fq_cache_evict(b, w, pool, pool, dst, 8, 2))
+    host, there = (fq.PagedBatch([1, 1], [20, 3], [[0, 1], [2, -1]], 16, 3, device=d) for d in ("cpu", "cuda"))
+    for n, stub in stubs.items():
+        monkeypatch.setattr(fq._lib, n, stub)
+    try:
+        fq._bind.bind(*real[:6], *(ctypes.cast(stubs[n], ctypes.c_void_p).value for n in names[6:]))
+        for call in calls:
+            with pytest.raises((TypeError, ValueError)):
+                call(host)
+        assert reached == []
+        for call in calls:
+            with pytest.raises(fq.FqError):
+                call(there)
+        assert reached == [names[6], names[7], names[7], names[7], names[8], names[8]]
+    finally:
+        fq._bind.bind(*real)
