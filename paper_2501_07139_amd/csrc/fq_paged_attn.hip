@@ -8,8 +8,11 @@
 // The (token, head of the group) pairs of one key/value head are the rows of the matrix products, token after token, so heads that
 // share keys share their loads.  With keys as the first operand of 16x16x32 MFMAs a lane holds scores of ONE row (column l % 16 of
 // S^T = K . Q^T): maximum and sum need in-lane work and two cross-lane steps, and exp(S - max), rounded to fp16, is the second
-// operand of O^T = V^T . P^T as it stands.  The weights are fp16 (their sum and lse are of the unrounded fp32 ones): an error of at most
-// 2^-11 of each term, as the output's own rounding.  V^T comes from row-major values through the transposing LDS read.
+// operand of O^T = V^T . P^T as it stands.  The weights are fp16 (their sum and lse are of the unrounded fp32 ones) and taken 2^15 or 2^7 times too large, so
+// that fp16's least normal number, 2^-14, is 2^-29 or 2^-21 of the largest: above that an error of at most 2^-11 of each term, as the output's own
+// rounding, and below it at most 2^-40 or 2^-32 of the largest, however many positions one row's reference spans (as they stood, terms below 2^-25 were lost
+// from the product and kept in the sum: a row whose many positions have 2^-23 of the largest each was off by a fifth).
+// V^T comes from row-major values through the transposing LDS read.
 #include "fq_paged.h"
 
 namespace {
@@ -113,6 +116,7 @@ __device__ __forceinline__ h4 lds_column(const _Float16 *at)
 // of the cache (one token of 32 heads over 100003 positions of 8 key/value heads: 410 MB in 69 us, 5.9 TB/s, and 6 for the join), short calls by the chain of
 // loads: length and table, keys and values, output (330 positions of 32 heads 7.5 us).  With SCORES the scaled scores of every row are left for the column sums, which need the sum over all splits first.
 constexpr int FEW = 16;
+constexpr float RAISE_FEW = 15.f, DOWN_FEW = 0x1p-15f; // powers of two; a weight is at most 1 here, and 65504 the largest in fp16
 
 typedef const __attribute__((address_space(4))) int *const_ints; // read through the scalar cache; nothing writes them in these kernels
 
@@ -258,11 +262,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         }
         h8 pb;
         float sum = 0.f;
+        const float low = mref - RAISE_FEW;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const float e = __builtin_amdgcn_exp2f(st[i][v] - mref);
+                const float e = __builtin_amdgcn_exp2f(st[i][v] - low);
                 sum += e;
                 pb[4 * i + v] = (_Float16)e;
             }
@@ -315,7 +320,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     float w[4], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(ms[i][col] - mref);
+        w[i] = __builtin_amdgcn_exp2f(ms[i][col] - mref) * DOWN_FEW;
         sum += w[i] * ls[i][col];
     }
     const bool only = len <= p.chunk; // no other split has any of it
@@ -355,6 +360,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
 // 1.06 ms, 1.01 PFLOP/s; an exponential takes sixteen clocks, a step of 128 rows 32 of them and 32 products a wavefront), short chunks by the latency of
 // their steps.
 constexpr int KT = 64; // positions of a tile
+constexpr float LAG = 8.f, RAISE = 7.f, DOWN = 0x1p-7f; // powers of two: the largest weight is at most LAG + RAISE = 15, fp16 ends at 16
 
 constexpr int tile_rows_of(int KS) { return 128 / KS; }
 
@@ -525,9 +531,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
                 for (int v = 0; v < 16; ++v)
                     top = fmaxf(top, st[kb][v]);
             top = other_half(top, larger) * p.scale;
-            // The reference that exponentials are taken from follows the maximum once that is 2^8 above it: weights up to 256 are as good in
-            // fp16 as those up to 1, and the outputs are rescaled that much less often.
-            if (__builtin_amdgcn_ballot_w64(top > mx + 8.f) != 0) {
+            // The reference that exponentials are taken from follows the maximum once that is 2^LAG above it: the outputs are rescaled that
+            // much less often, and weights up to 2^15 are as good in fp16 as those up to 1.
+            if (__builtin_amdgcn_ballot_w64(top > mx + LAG) != 0) {
                 const float mnew = fmaxf(mx, top);
                 const float alpha = __builtin_amdgcn_exp2f(mx - (mnew == -INFINITY ? 0.f : mnew));
                 mx = mnew;
@@ -536,14 +542,14 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
                 for (int i = 0; i < 4; ++i)
                     acc[i] *= alpha;
             }
-            const float mref = mx == -INFINITY ? 0.f : mx;
+            const float raise = RAISE - (mx == -INFINITY ? 0.f : mx);
             float sum = 0.f;
             h8 pb[KB][2];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(st[kb][v], p.scale, -mref));
+                    const float e = __builtin_amdgcn_exp2f(fmaf(st[kb][v], p.scale, raise));
                     sum += e;
                     pb[kb][v >> 3][v & 7] = (_Float16)e;
                 }
@@ -647,16 +653,16 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
             *reinterpret_cast<h4 *>(p.out + at * PD + 8 * i + 4 * h) = o;
         }
         if (h == 0 && p.lse)
-            p.lse[at] = (mx + log2f(l)) * LN2; // log2(0) is -inf
+            p.lse[at] = (mx + log2f(l * DOWN)) * LN2; // log2(0) is -inf
     } else {
         const size_t part = ((size_t)split * p.s.tokens + tile.s.first + token) * p.heads + head;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             *reinterpret_cast<f4 *>(p.part_o + part * PD + 8 * i + 4 * h) =
-                f4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]};
+                f4{acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2], acc[i >> 2][4 * (i & 3) + 3]} * DOWN;
         if (h == 0) {
             p.part_ml[2 * part] = mx;
-            p.part_ml[2 * part + 1] = l;
+            p.part_ml[2 * part + 1] = l * DOWN;
         }
     }
 }

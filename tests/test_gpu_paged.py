@@ -675,3 +675,42 @@ def test_batches_on_the_host_are_refused_with_and_without_outputs(fq, torch, mon
         assert reached == [names[6], names[7], names[7], names[7], names[8], names[8]]
     finally:
         fq._bind.bind(*real)
+
+
+@pytest.mark.parametrize("lag", [0.0, 7.9])
+@pytest.mark.parametrize("n, S, heads, kv, route", [(1, 380, 8, 8, (16, 1)), (3, 380, 8, 2, (16, 1)), (1, 3000, 8, 2, (16, 24)), (300, 3000, 8, 8, (64, 4)),
+                                                    (1500, 3000, 16, 8, (64, 1)), (1024, 4000, 32, 8, (128, 1))], ids=str)
+def test_weights_far_below_the_largest(fq, torch, n, S, heads, kv, route, lag):
+    """One position takes nearly all of the softmax and has a value of zero: the outputs are the many others, each 2.5 * 2^-24 of it.
+    As fp16 numbers of that size they would be off by a fifth.  Terms are held to u of each, or 2^-32 of the largest.  `lag`: the first positions lie that
+    many powers of two below the largest."""
+    rng = np.random.default_rng(67)
+    page = 64
+    table, pages = deal(rng, [S], page)
+    b = fq.PagedBatch([n], [S], table, page, pages)
+    assert fq.fq_attn_paged_route(b, heads, kv)[:2] == route
+    top = np.zeros(S)
+    top[[100, 132, 164, 196]] = 1.0  # a wavefront of single tokens has 32 positions of every 128
+    V = np.where(top[:, None] > 0, 0.0, rng.uniform(50.0, 150.0, size=(kv, S, 128))).astype(np.float16)
+    height = (24 - np.log2(2.5)) * np.log(2.0)
+    K = np.zeros((S, 128), dtype=np.float16)
+    K[:, 0] = np.where(top > 0, height / 2, 0.0)
+    K[[1, 33, 65, 97], 0] = (height - lag * np.log(2.0)) / 2
+    V[:, [1, 33, 65, 97]] = 0.0
+    k, v = (np.zeros((pages, kv, page, 128), dtype=np.float16) for _ in range(2))
+    for t in range(S):
+        k[table[0, t // page], :, t % page], v[table[0, t // page], :, t % page] = K[t], V[:, t]
+    q = np.zeros((n, heads * 128), dtype=np.float16)
+    q[:, ::128] = 2.0
+    lse = torch.empty(n, heads, device="cuda")
+    got = fq.fq_attn_paged(dev(torch, q), b, dev(torch, k), dev(torch, v), scale=1.0, lse=lse).cpu().numpy().astype(np.float64).reshape(n, kv, heads // kv, 128)
+    w = np.exp(2.0 * K[:, 0].astype(np.float64))  # of every row that sees the position
+    norm, rows = np.cumsum(w), np.arange(S - n, S)
+    assert np.abs(lse.cpu().numpy() - np.log(norm[rows])[:, None]).max() <= 130 * 2.0 ** -24 * height + 2.0 ** -20 * (1 + np.log(norm[-1]))
+    e = 130 * 2.0 ** -24 * height + 2.0 ** -20
+    for g in range(kv):
+        mass = np.cumsum(w[:, None] * V[g].astype(np.float64), 0)[rows] / norm[rows, None]
+        count = np.cumsum(V[g].astype(np.float64), 0)[rows] * 2.0 ** -32
+        bound = (2 * U * 1.01 + 2 * e) * mass + count + 2.0 ** -25
+        err = np.abs(got[:, g] - mass[:, None])
+        assert (err <= bound[:, None]).all(), float((err / bound[:, None]).max())
