@@ -66,7 +66,7 @@ class PagedServer:
             raise ValueError("a pair of gains for every block")
         if keep is not None and not 0 <= recent <= keep <= (limit if limit is not None else keep):
             raise ValueError("need 0 <= recent <= keep <= limit")
-        self.heads, self.kv_heads, self.L = q.N // 128, k.N // 128, stack.L
+        self.heads, self.kv_heads, self.L, self.hidden = q.N // 128, k.N // 128, stack.L, q.K
         self.pool = PagePool(pages, page)
         self.max_positions, self.device = max_positions, torch.device(device)
         self.keep, self.recent, self.limit = keep, recent, keep if limit is None else limit
@@ -108,32 +108,69 @@ class PagedServer:
     # ----------------------------------------------------------------------- steps
     def step(self, stack: Stack, bitvec, tokens: Dict[int, torch.Tensor]) -> Dict[int, torch.Tensor]:
         """tokens: for some slots the hidden states of their next tokens, fp16 [n, hidden] (one token, or a chunk of a prompt).
-        Returns the last block's output for each.  Nothing is changed if the pages do not suffice."""
+        Returns the last block's output for each.  Pages, lengths and positions change only with a step that has gone through: after an error
+        they are as before, and the same tokens may be given again (of an error behind the first block, memory that cannot be
+        had, the weights that cuts go by may have that attempt's share)."""
         order = sorted(tokens)
         if not order:
             return {}
-        rows = {i: tokens[i].shape[0] for i in order}
+        rows = {}
         for i in order:
-            s = self.seqs[i]
+            s, t = self.seqs[i], tokens[i]
+            if t.dim() != 2 or t.shape[1] != self.hidden or t.dtype != torch.float16 or t.device != self.k.device:
+                raise ValueError(f"slot {i}: tokens must be fp16 [n, {self.hidden}] on {self.k.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            rows[i] = t.shape[0]
             if rows[i] == 0:
                 raise ValueError(f"slot {i}: no tokens")
             if s.position + rows[i] > self.max_positions:
                 raise FqError(-2, f"slot {i}: position {s.position + rows[i]} of {self.max_positions}")
+        matrices = self._matrices(stack, bitvec)
         more = {i: self.pool.need(self.seqs[i].length + rows[i]) - len(self.seqs[i].pages) for i in order}
         if sum(more.values()) > self.pool.free:
             raise MemoryError(f"{sum(more.values())} pages needed, {self.pool.free} free of {self.pool.pages}")
+        taken = {i: self.pool.take(more[i]) for i in order}
+        try:
+            x = self._blocks(matrices, order, tokens, rows, taken)
+        except BaseException:
+            for i in reversed(order):
+                self.pool.give(taken[i])
+            raise
         for i in order:
-            self.seqs[i].pages += self.pool.take(more[i])
-            self.seqs[i].length += rows[i]
+            s = self.seqs[i]
+            s.pages += taken[i]
+            s.length += rows[i]
+            s.position += rows[i]
+        if self.keep is not None:
+            self.cut([i for i in self.seqs if self.seqs[i].length > self.limit])
+        return dict(zip(order, torch.split(x, [rows[i] for i in order])))
+
+    def _matrices(self, stack: Stack, bitvec) -> List[list]:
+        """The matrices that the bit vector picks, seven a block: all there, and of shapes that go together."""
+        bitvec = np.asarray(bitvec, dtype=np.uint8).reshape(-1)
+        if stack.L != self.L or bitvec.size != 7 * self.L:
+            raise ValueError(f"{stack.L} blocks, {bitvec.size} bit widths; the server has {self.L} blocks of seven matrices")
+        picked = []
+        for l, bits in enumerate(bitvec.reshape(self.L, 7).tolist()):
+            for j, n in enumerate(bits):
+                if n not in stack.layers[l][j]:
+                    raise ValueError(f"block {l}, matrix {j}: no packing of {n} bits")
+            w = [stack.layers[l][j][n] for j, n in enumerate(bits)]
+            H, Q, KV, F = self.hidden, 128 * self.heads, 128 * self.kv_heads, w[4].N
+            if [(m.N, m.K) for m in w] != [(Q, H), (KV, H), (KV, H), (H, Q), (F, H), (F, H), (H, F)]:
+                raise ValueError(f"block {l}: matrices of shapes {[(m.N, m.K) for m in w]}")
+            picked.append(w)
+        return picked
+
+    def _blocks(self, matrices: List[list], order: List[int], tokens: Dict[int, torch.Tensor], rows: Dict[int, int],
+                taken: Dict[int, List[int]]) -> torch.Tensor:
+        """All blocks over the tokens, their sequences as long as they are with them; the account stays as it is."""
         positions = [np.arange(self.seqs[i].position, self.seqs[i].position + rows[i]) for i in order]
         batch = PagedBatch([rows.get(i, 0) for i in range(self.slots)],
-                           [self.seqs[i].length if i in self.seqs else 0 for i in range(self.slots)],
-                           self._table({i: s.pages for i, s in self.seqs.items()}), self.pool.page, self.pool.pages,
+                           [self.seqs[i].length + rows.get(i, 0) if i in self.seqs else 0 for i in range(self.slots)],
+                           self._table({i: s.pages + taken.get(i, []) for i, s in self.seqs.items()}), self.pool.page, self.pool.pages,
                            positions=np.concatenate(positions), device=self.device)
         x = torch.cat([tokens[i] for i in order])
-        bitvec = np.asarray(bitvec, dtype=np.uint8).reshape(self.L, 7)
-        for l in range(self.L):
-            w = [stack.layers[l][j][int(bitvec[l, j])] for j in range(7)]
+        for l, w in enumerate(matrices):
             q_gain, k_gain = self.gains[l] if self.gains is not None else (None, None)
             acc = None if self.weights is None else self.weights[l]
             u = fq_glue(0, x)
@@ -144,11 +181,7 @@ class PagedServer:
             u = fq_glue(0, x1)
             m = fq_glue(5, fq_qlinear(u, w[4]), fq_qlinear(u, w[5]))
             x = fq_glue(2, x1, fq_qlinear(m, w[6]))
-        for i in order:
-            self.seqs[i].position += rows[i]
-        if self.keep is not None:
-            self.cut([i for i in self.seqs if self.seqs[i].length > self.limit])
-        return dict(zip(order, torch.split(x, [rows[i] for i in order])))
+        return x
 
     def cut(self, slots: List[int]) -> List[int]:
         """Cut these sequences to `keep` positions a head, into pages of their own; their old pages are free afterwards.  All at once

@@ -176,3 +176,84 @@ def test_cuts_wait_for_room(gpu):
     server.close(a)
     server.step(stack, bitvec, {b: x[:1]})
     assert server.length(c) == 30 and server.length(b) == 31 and server.pool.free == 9 - 4
+
+
+class Matrix:
+    def __init__(self, N, K):
+        self.N, self.K = N, K
+
+
+def on_the_host(monkeypatch, L=2, heads=4, kv=2, ffn=640, **options):
+    """A server whose calls of the library are replaced by ones that only name themselves, with matrices that are shapes."""
+    import torch
+
+    from paper_2501_07139_amd import serve
+
+    H = 128 * heads
+    shapes = [(H, H), (128 * kv, H), (128 * kv, H), (H, H), (ffn, H), (ffn, H), (H, ffn)]
+
+    class Blocks:
+        pass
+
+    stack = Blocks()
+    stack.L, stack.layers = L, [[{4: Matrix(*s), 8: Matrix(*s)} for s in shapes] for _ in range(L)]
+    calls = []
+
+    def name(what, result):
+        def call(*a, **k):
+            calls.append(what)
+            return result(*a, **k)
+        monkeypatch.setattr(serve, what, call)
+
+    name("fq_glue", lambda op, a, b=None: a)
+    name("fq_qlinear", lambda x, w: torch.zeros(len(x), w.N, dtype=torch.float16))
+    name("fq_qk_norm_rope", lambda q, *a, **k: q)
+    name("fq_attn_paged", lambda q, *a, **k: q)
+    server = serve.PagedServer(stack, slots=2, pages=12, page=16, max_positions=128, device="cpu", **options)
+    return torch, server, stack, np.full(7 * L, 4, dtype=np.uint8), calls
+
+
+def account(server):
+    return {i: (list(s.pages), s.length, s.position) for i, s in server.seqs.items()}, list(server.pool._free)
+
+
+def test_a_step_that_fails_changes_nothing(monkeypatch):
+    """Tokens of another width, type or rank, bit widths that are not stored, shapes that do not go together, and an error in the last block."""
+    torch, server, stack, bitvec, calls = on_the_host(monkeypatch)
+    a, b = server.open(), server.open()
+    x = torch.zeros(40, 512, dtype=torch.float16)
+    server.step(stack, bitvec, {a: x[:20], b: x[:3]})
+    before = account(server)
+    assert [v[1:] for v in before[0].values()] == [(20, 20), (3, 3)] and len(before[1]) == 12 - 3
+    odd = [list(m) for m in stack.layers]
+    odd[1] = [dict(m) for m in odd[1]]
+    odd[1][3] = {4: Matrix(256, 512)}
+    other = type(stack)()
+    other.L, other.layers = 2, odd
+    short = type(stack)()
+    short.L, short.layers = 1, stack.layers[:1]
+    bad = np.array(bitvec)
+    bad[-1] = 3
+    del calls[:]
+    for s, bits, tokens in ((stack, bitvec, {a: x[:, :256], b: x}), (stack, bitvec, {a: x[:, :256]}), (stack, bitvec, {a: x.float()}),
+                            (stack, bitvec, {a: x[0]}), (stack, bitvec, {a: x.to("meta")}), (stack, bad, {a: x}), (stack, bitvec[:7], {a: x}),
+                            (stack, np.tile(bitvec, 2), {a: x}), (other, bitvec, {a: x}), (short, bitvec[:7], {a: x})):
+        with pytest.raises(ValueError):
+            server.step(s, bits, tokens)
+        assert account(server) == before and calls == []
+    from paper_2501_07139_amd import serve
+
+    real, count = serve.fq_qlinear, []
+
+    def fails(*args):
+        count.append(1)
+        if len(count) == 12:  # in the second block
+            raise RuntimeError("no memory")
+        return real(*args)
+
+    monkeypatch.setattr(serve, "fq_qlinear", fails)
+    with pytest.raises(RuntimeError):
+        server.step(stack, bitvec, {a: x, b: x[:30]})
+    assert len(count) == 12 and account(server) == before
+    out = server.step(stack, bitvec, {a: x, b: x[:30]})
+    assert [len(out[i]) for i in (a, b)] == [40, 30] and (server.length(a), server.length(b)) == (60, 33)
