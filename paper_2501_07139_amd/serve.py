@@ -64,8 +64,8 @@ class PagedServer:
             raise ValueError("q and k must have 128 rows a head, the query heads a multiple of the key/value heads")
         if gains is not None and len(gains) != stack.L:
             raise ValueError("a pair of gains for every block")
-        if keep is not None and not 0 <= recent <= keep <= (limit if limit is not None else keep):
-            raise ValueError("need 0 <= recent <= keep <= limit")
+        if keep is not None and not (0 <= recent <= keep <= (limit if limit is not None else keep) and keep > 0):
+            raise ValueError("need 0 <= recent <= keep <= limit, 0 < keep")
         self.heads, self.kv_heads, self.L, self.hidden = q.N // 128, k.N // 128, stack.L, q.K
         self.pool = PagePool(pages, page)
         self.max_positions, self.device = max_positions, torch.device(device)

@@ -257,3 +257,11 @@ def test_a_step_that_fails_changes_nothing(monkeypatch):
     assert len(count) == 12 and account(server) == before
     out = server.step(stack, bitvec, {a: x, b: x[:30]})
     assert [len(out[i]) for i in (a, b)] == [40, 30] and (server.length(a), server.length(b)) == (60, 33)
+
+
+def test_a_cut_to_nothing_is_refused(monkeypatch):
+    """The library cuts to one position at least: refused where the server is made, not by the first cut."""
+    for options in (dict(keep=0), dict(keep=0, limit=5), dict(keep=3, recent=-1), dict(keep=3, limit=2)):
+        with pytest.raises(ValueError):
+            on_the_host(monkeypatch, **options)
+    on_the_host(monkeypatch, keep=1, recent=1, limit=1)
