@@ -185,33 +185,39 @@ class PagedServer:
 
     def cut(self, slots: List[int]) -> List[int]:
         """Cut these sequences to `keep` positions a head, into pages of their own; their old pages are free afterwards.  All at once
-        if the free pages hold the new rows of all, else one after the other.  Returns the slots for which there was no room:
-        they stay as they are, and the next step tries again."""
+        if the free pages hold the new rows of all, else one after the other.  Returns the slots for which there was no room, of
+        pages or of device memory: they stay as they are, and the next step tries again."""
+        slots = list(dict.fromkeys(slots))
         need = {i: self.pool.need(min(self.keep, self.seqs[i].length)) for i in slots}
-        if sum(need.values()) <= self.pool.free:
-            self._cut(slots)
+        if sum(need.values()) <= self.pool.free and self._cut(slots):
             return []
-        left = []
-        for i in slots:
-            if need[i] <= self.pool.free:
-                self._cut([i])
-            else:
-                left.append(i)
-        return left
+        return [i for i in slots if need[i] > self.pool.free or not self._cut([i])]
 
-    def _cut(self, slots: List[int]) -> None:
+    def _cut(self, slots: List[int]) -> bool:
+        """False, and nothing changed, if the device's memory does not suffice."""
         if not slots:
-            return
-        batch = PagedBatch([0] * len(slots), [self.seqs[i].length for i in slots], self._table({n: self.seqs[i].pages for n, i in enumerate(slots)})
-                           [:len(slots)], self.pool.page, self.pool.pages, device=self.device)
-        new = [self.pool.take(self.pool.need(min(self.keep, self.seqs[i].length))) for i in slots]
-        dst = torch.from_numpy(self._table(dict(enumerate(new)))[:len(slots)].astype(np.int32)).to(self.device)
-        index = torch.tensor(slots, device=self.device)
-        for l in range(self.L):
-            kept = torch.zeros((len(slots), self.kv_heads, self.max_positions), dtype=torch.float32, device=self.device)
-            fq_cache_evict(batch, self.weights[l].index_select(0, index), self.k[l], self.v[l], dst, self.keep, self.recent, weights_out=kept)
-            self.weights[l].index_copy_(0, index, kept)
+            return True
+        lengths = [self.seqs[i].length for i in slots]
+        new = [self.pool.take(self.pool.need(min(self.keep, n))) for n in lengths]
+        try:
+            batch = PagedBatch([0] * len(slots), lengths, self._table({n: self.seqs[i].pages for n, i in enumerate(slots)})[:len(slots)],
+                               self.pool.page, self.pool.pages, device=self.device)
+            dst = torch.from_numpy(self._table(dict(enumerate(new)))[:len(slots)].astype(np.int32)).to(self.device)
+            index = torch.tensor(slots, device=self.device)
+            most = max(lengths)
+            kept = torch.zeros((self.L, len(slots), self.kv_heads, most), dtype=torch.float32, device=self.device)
+            for l in range(self.L):  # the running weights stay until every block's rows are copied
+                fq_cache_evict(batch, self.weights[l, :, :, :most].index_select(0, index), self.k[l], self.v[l], dst, self.keep, self.recent,
+                               weights_out=kept[l])
+            self.weights[:, :, :, :most].index_copy_(1, index, kept)  # zeros behind what stays
+        except BaseException as e:
+            for pages in reversed(new):
+                self.pool.give(pages)
+            if isinstance(e, torch.OutOfMemoryError):
+                return False
+            raise
         for i, pages in zip(slots, new):
             s = self.seqs[i]
             self.pool.give(s.pages)
             s.pages, s.length = pages, min(self.keep, s.length)
+        return True

@@ -265,3 +265,38 @@ def test_a_cut_to_nothing_is_refused(monkeypatch):
         with pytest.raises(ValueError):
             on_the_host(monkeypatch, **options)
     on_the_host(monkeypatch, keep=1, recent=1, limit=1)
+
+
+def test_a_cut_that_fails_changes_nothing(monkeypatch):
+    """An error in the last block leaves pages, lengths and the weights of all blocks; want of device memory is want of room."""
+    import copy
+
+    torch, server, stack, bitvec, calls = on_the_host(monkeypatch, keep=20, recent=4, limit=30)
+    from paper_2501_07139_amd import serve
+
+    a, b = server.open(), server.open()
+    x = torch.zeros(60, 512, dtype=torch.float16)
+    server.step(stack, bitvec, {a: x[:30], b: x[:25]})
+    server.weights[:] = torch.rand(server.weights.shape)
+    before, weights = copy.deepcopy(account(server)), server.weights.clone()
+    blocks, error = [], [RuntimeError("launch")]
+
+    def evict(batch, w, k, v, dst, keep, recent, weights_out):
+        blocks.append(batch.seqs)
+        if len(blocks) % 2 == 0 and error:
+            raise error[0]
+        weights_out[:, :, :min(keep, w.shape[2])] = w[:, :, -keep:]
+
+    monkeypatch.setattr(serve, "fq_cache_evict", evict)
+    with pytest.raises(RuntimeError):
+        server.cut([a])
+    assert account(server) == before and torch.equal(server.weights, weights)
+    error[0] = torch.OutOfMemoryError("none left")
+    assert server.cut([a, b]) == [a, b] and account(server) == before and torch.equal(server.weights, weights)
+    out = server.step(stack, bitvec, {a: x[:10]})  # longer than the limit then: its output is there although the cut finds no room
+    assert len(out[a]) == 10 and server.length(a) == 40 and torch.equal(server.weights, weights)
+    del error[:]
+    pages = server.pool.free
+    assert server.cut([a, a]) == [] and server.length(a) == 20 and server.pool.free == pages + 1  # three pages, two for what stays
+    assert torch.equal(server.weights[:, a, :, :20], weights[:, a, :, 20:40]) and bool((server.weights[:, a, :, 20:40] == 0).all())
+    assert torch.equal(server.weights[:, b], weights[:, b]) and server.length(b) == 25
