@@ -204,7 +204,7 @@ class PagedServer:
                                self.pool.page, self.pool.pages, device=self.device)
             dst = torch.from_numpy(self._table(dict(enumerate(new)))[:len(slots)].astype(np.int32)).to(self.device)
             index = torch.tensor(slots, device=self.device)
-            most = max(lengths)
+            most = max(1, *lengths)  # the library wants weights for sequences without positions, too
             kept = torch.zeros((self.L, len(slots), self.kv_heads, most), dtype=torch.float32, device=self.device)
             for l in range(self.L):  # the running weights stay until every block's rows are copied
                 fq_cache_evict(batch, self.weights[l, :, :, :most].index_select(0, index), self.k[l], self.v[l], dst, self.keep, self.recent,

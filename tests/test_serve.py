@@ -300,3 +300,23 @@ def test_a_cut_that_fails_changes_nothing(monkeypatch):
     assert server.cut([a, a]) == [] and server.length(a) == 20 and server.pool.free == pages + 1  # three pages, two for what stays
     assert torch.equal(server.weights[:, a, :, :20], weights[:, a, :, 20:40]) and bool((server.weights[:, a, :, 20:40] == 0).all())
     assert torch.equal(server.weights[:, b], weights[:, b]) and server.length(b) == 25
+
+
+@pytest.mark.gpu
+def test_a_cut_of_what_is_short_or_empty(gpu):
+    """Sequences below the limit, without any position among them, are copied whole; the next step goes on from there."""
+    fq, torch = gpu
+    from paper_2501_07139_amd.serve import PagedServer
+
+    stack, bitvec = build(fq, kv_heads=2, L=2)
+    server = PagedServer(stack, slots=3, pages=12, page=16, max_positions=64, keep=20, recent=4, limit=40)
+    a, b, c = server.open(), server.open(), server.open()
+    x = torch.randn(30, 512, device="cuda").half()
+    assert server.cut([c]) == [] and (server.length(c), server.pool.free) == (0, 12)
+    server.step(stack, bitvec, {a: x[:17], b: x})
+    rows = lambda i, n: server.k[:, torch.tensor(server.seqs[i].pages, device="cuda")].transpose(1, 2).reshape(2, 2, -1, 128)[:, :, :n].clone()
+    before, weights = rows(a, 17), server.weights.clone()
+    assert server.cut([c, a, b]) == [] and [server.length(i) for i in (a, b, c)] == [17, 20, 0] and server.pool.free == 12 - 2 - 2
+    assert torch.equal(rows(a, 17), before) and torch.equal(server.weights[:, a], weights[:, a]) and bool((server.weights[:, b, :, 20:] == 0).all())
+    out = server.step(stack, bitvec, {c: x[:2], a: x[:1]})
+    assert all(bool(torch.isfinite(t).all()) for t in out.values()) and server.length(c) == 2
