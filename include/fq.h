@@ -487,7 +487,7 @@ int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *
  * over q; lse fp32 [tokens][n_heads].
  * With weights_out (fp32 [seqs][n_kv_heads][weights_stride], else NULL), what every position has received is added up:
  *   weights_out[b][h][t] = (t < S - n ? weights[b][h][t] : 0) + sum of p[t] over the tokens and the query heads of h,
- * t < S; weights may be weights_out, or NULL for zeros.  Sums are taken in a fixed order.
+ * t < S; weights may be weights_out (but not overlap it otherwise), or NULL for zeros.  Sums are taken in a fixed order.
  * workspace: device scratch of fq_attn_paged_workspace_bytes(batch, n_heads, n_kv_heads, weights_out != NULL) bytes
  * (may be 0, and NULL then), 16-byte aligned, contents undefined afterwards.
  */

@@ -811,6 +811,14 @@ bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
     return x < y + b_bytes && y < x + a_bytes;
 }
 
+// The same of two arrays of as many rows, `stride` bytes apart and `row` of them used: rows of one may lie between those of the other.
+bool rows_overlap(const void *a, const void *b, size_t rows, size_t stride, size_t row)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), d = x < y ? y - x : x - y;
+    const size_t at = d / stride, off = d % stride; // the later array's first row, in rows of the earlier one
+    return (at < rows && off < row) || (at + 1 < rows && stride - off < row);
+}
+
 bool stride_ok(int ld, int width) { return ld >= width && ld % 8 == 0; }
 
 } // namespace
@@ -884,6 +892,9 @@ extern "C" int fq_attn_paged(const fq_paged_batch *batch, const void *q, int ldq
     if (weights_out && (weights_stride < batch->max_len || (long long)batch->max_len * n_kv_heads >= 1 << 28))
         return fq_fail(FQ_ERR_SHAPE, "%s: weights_stride=%d max_len=%d n_kv_heads=%d (need weights_stride >= max_len, max_len * n_kv_heads "
                        "below 2^28)", fn, weights_stride, batch->max_len, n_kv_heads);
+    if (weights && weights != weights_out && batch->max_len > 0 &&
+        rows_overlap(weights, weights_out, (size_t)batch->seqs * n_kv_heads, (size_t)weights_stride * 4, (size_t)batch->max_len * 4))
+        return fq_fail(FQ_ERR_SHAPE, "%s: weights_out overlaps weights other than place by place", fn);
     const size_t need = fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, weights_out != nullptr);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fq_fail(FQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);

@@ -192,3 +192,15 @@ def test_division_of_sequences_of_other_lengths():
     with_lengths = fq.fq_attn_paged_route(one, 32, 8)
     one.struct.positions = one.struct.pairs = 0
     assert fq.fq_attn_paged_route(one, 32, 8) == with_lengths
+
+
+@pytest.mark.parametrize("weights, out, stride", [(4096, 4096 + 4, 100), (4096, 4096 + 400 * 4 - 4, 100), (4096 + 400 * 4 - 4, 4096, 100), (4096, 4096 - 120 * 4, 100),
+                                                  (4096, 4096 + 404, 200), (4096, 4096 + 396, 200), (4096 + 2 * 800 + 404, 4096, 200)])
+def test_attention_refuses_weights_over_part_of_what_it_adds_to(weights, out, stride):
+    """Two sequences of two heads: 3 * 100 + 100 floats each; sums that one workgroup writes are read by another."""
+    assert attn(fq._lib, batch(), weights=weights, weights_out=out, stride=stride) == -2
+    assert "weights_out overlaps weights" in fq.fq_last_error()
+    for apart, stride in ((4096 + 400 * 4, 100), (4096, 100), (4096 + 400, 200), (4096 - 400 - 800, 200), (4096 - 400 * 4, 100)):
+        # side by side, the same, or row between row: the next check's refusal
+        assert attn(fq._lib, batch(), weights=4096, weights_out=apart, stride=stride, ws=None) == -6
+    assert attn(fq._lib, batch(max_len=0), weights=4096, weights_out=4100, stride=0, ws=None) == -6  # rows of nothing
