@@ -471,7 +471,7 @@ typedef struct {
  * fp32 in between, one rounding.  q, k, v fp16, device: row m at m * ldq (ldk, ldv) elements, multiples of 8 (columns of
  * one product, for instance); q_gain, k_gain fp16 [128] or NULL; positions, slots int32 [tokens]; a slot outside the pools (-1)
  * marks a token that is not cached; a position outside the table takes its nearest row.  q_out fp16 [tokens][n_heads * 128]
- * (may be q if that is contiguous).  Two tokens of one slot leave either.
+ * (may be q if that is contiguous; not over k or v).  Two tokens of one slot leave either.
  */
 int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const void *v, int ldv, int tokens, int n_heads,
                     int n_kv_heads, const int32_t *positions, const int32_t *slots, const float *rope, int rope_rows,

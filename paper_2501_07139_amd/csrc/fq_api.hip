@@ -819,6 +819,14 @@ bool rows_overlap(const void *a, const void *b, size_t rows, size_t stride, size
     return (at < rows && off < row) || (at + 1 < rows && stride - off < row);
 }
 
+// Whether rows of `row` bytes, `stride` (at least that) apart, reach into a run of bytes.
+bool rows_in(const void *a, size_t rows, size_t stride, size_t row, const void *run, size_t bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(run);
+    const size_t first = y < x + row ? 0 : (y - x - row) / stride + 1; // the first row that ends behind the run's start
+    return first < rows && x + first * stride < y + bytes;
+}
+
 bool stride_ok(int ld, int width) { return ld >= width && ld % 8 == 0; }
 
 } // namespace
@@ -844,6 +852,9 @@ extern "C" int fq_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, c
     const size_t row = (size_t)n_heads * 128 * 2;
     if (tokens > 0 && !(q_out == q && (ldq == n_heads * 128 || tokens == 1)) && overlap(q, (size_t)(tokens - 1) * ldq * 2 + row, q_out, tokens * row))
         return fq_fail(FQ_ERR_SHAPE, "%s: q_out overlaps q other than row by row", fn);
+    const size_t kv_row = (size_t)n_kv_heads * 128 * 2;
+    if (tokens > 0 && (rows_in(k, tokens, (size_t)ldk * 2, kv_row, q_out, tokens * row) || rows_in(v, tokens, (size_t)ldv * 2, kv_row, q_out, tokens * row)))
+        return fq_fail(FQ_ERR_SHAPE, "%s: q_out overlaps k or v", fn);
     if (tokens == 0)
         return FQ_OK;
     return check_hip(fq_launch_qk_norm_rope(q, ldq, k, ldk, v, ldv, tokens, n_heads, n_kv_heads, positions, slots, rope, rope_rows, q_gain, k_gain,

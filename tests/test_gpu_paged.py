@@ -714,3 +714,22 @@ def test_weights_far_below_the_largest(fq, torch, n, S, heads, kv, route, lag):
         bound = (2 * U * 1.01 + 2 * e) * mass + count + 2.0 ** -25
         err = np.abs(got[:, g] - mass[:, None])
         assert (err <= bound[:, None]).all(), float((err / bound[:, None]).max())
+
+
+def test_rotation_between_the_rows_it_reads(fq, torch):
+    """q_out right behind a row of keys and ahead of the next is no overlap; a place further on it is."""
+    rng = np.random.default_rng(71)
+    x = [dev(torch, rng.normal(size=(2, 256)).astype(np.float16)) for _ in range(3)]
+    b = fq.PagedBatch([2], [20], [[0, 1]], 16, 2)
+    rope = fq.rope_table(20)
+    kp, vp, kp1, vp1 = (torch.zeros(2, 2, 16, 128, dtype=torch.float16, device="cuda") for _ in range(4))
+    want = fq.fq_qk_norm_rope(*x, b, rope, kp, vp)
+    room = torch.zeros(1024, dtype=torch.float16, device="cuda")
+    k = room.as_strided((2, 256), (768, 1))
+    k.copy_(x[1])
+    got = fq.fq_qk_norm_rope(x[0], k, x[2], b, rope, kp1, vp1, out=room[256:768].view(2, 256))
+    assert torch.equal(got, want) and torch.equal(kp1, kp) and torch.equal(vp1, vp) and torch.equal(k, x[1])
+    for at in (248, 264):
+        with pytest.raises(fq.FqError) as e:
+            fq.fq_qk_norm_rope(x[0], k, x[2], b, rope, kp1, vp1, out=room[at:at + 512].view(2, 256))
+        assert e.value.code == -2

@@ -204,3 +204,11 @@ def test_attention_refuses_weights_over_part_of_what_it_adds_to(weights, out, st
         # side by side, the same, or row between row: the next check's refusal
         assert attn(fq._lib, batch(), weights=4096, weights_out=apart, stride=stride, ws=None) == -6
     assert attn(fq._lib, batch(max_len=0), weights=4096, weights_out=4100, stride=0, ws=None) == -6  # rows of nothing
+
+
+@pytest.mark.parametrize("call", [{"k": 1 << 20}, {"v": 1 << 20}, {"k": (1 << 20) + 1536 - 16}, {"v": (1 << 20) - 1536 + 16}, {"k": (1 << 20) - 8192, "ldk": 4096 + 128},
+                                  {"v": (1 << 20) - 8192 - 512, "ldv": 4096 + 256}], ids=str)
+def test_norm_rope_refuses_q_out_over_keys_or_values(call):
+    """Three tokens of two heads, rows of 512 bytes: one workgroup would write what another reads."""
+    assert rope(fq._lib, **call) == -2
+    assert "q_out overlaps k or v" in fq.fq_last_error()
