@@ -706,7 +706,10 @@ def _rows(t, width: int, what: str):
         raise TypeError(f"{what} must be a device tensor [tokens, width] of torch.float16")
     if t.shape[1] != width or (t.shape[0] and width > 1 and t.stride(1) != 1):
         raise ValueError(f"{what} must be [tokens, {width}] with contiguous rows, got {tuple(t.shape)}")
-    return t.stride(0) if t.shape[0] > 1 else (width + 7) // 8 * 8
+    ld = t.stride(0) if t.shape[0] > 1 else (width + 7) // 8 * 8
+    if ld >= 1 << 31:  # it would reach the library without its upper bits
+        raise ValueError(f"{what}: rows {ld} elements apart (below 2^31)")
+    return ld
 
 
 def _pools(batch, k_pages, v_pages, pages: int, what: str):

@@ -733,3 +733,15 @@ def test_rotation_between_the_rows_it_reads(fq, torch):
         with pytest.raises(fq.FqError) as e:
             fq.fq_qk_norm_rope(x[0], k, x[2], b, rope, kp1, vp1, out=room[at:at + 512].view(2, 256))
         assert e.value.code == -2
+
+
+def test_rows_too_far_apart_are_refused(fq, torch):
+    """A distance of rows whose lower 32 bits look like a small one."""
+    b = fq.PagedBatch([2], [2], [[0]], 16, 1)
+    far = torch.zeros((1 << 32) + 512, dtype=torch.float16, device="cuda").as_strided((2, 256), ((1 << 32) + 256, 1))
+    near, pool, rope = torch.zeros(2, 256, dtype=torch.float16, device="cuda"), torch.zeros(1, 2, 16, 128, dtype=torch.float16, device="cuda"), fq.rope_table(2)
+    for out in (None, torch.zeros_like(near)):
+        for call in (lambda: fq.fq_attn_paged(far, b, pool, pool, out=out), lambda: fq.fq_qk_norm_rope(far, near, near, b, rope, pool, pool, out=out),
+                     lambda: fq.fq_qk_norm_rope(near, far, near, b, rope, pool, pool, out=out), lambda: fq.fq_qk_norm_rope(near, near, far, b, rope, pool, pool, out=out)):
+            with pytest.raises(ValueError):
+                call()
