@@ -681,7 +681,7 @@ class PagedBatch:
         place = np.arange(tokens) - q_start[seq] + (seq_lens - q_lens)[seq]  # of every token in its sequence; below 0: not in it
         at = np.maximum(place, 0)
         slots = np.where(place < 0, -1, table[seq, at // page] * page + at % page) if tokens else np.zeros(0, dtype=np.int64)
-        positions = at if positions is None else np.asarray(positions, dtype=np.int64).reshape(-1)
+        positions = at if positions is None else np.clip(np.asarray(positions, dtype=np.int64).reshape(-1), -2 ** 31, 2 ** 31 - 1)
         if len(positions) != tokens:
             raise FqError(-2, f"PagedBatch: {len(positions)} positions for {tokens} tokens")
         parts, offset = (q_start, seq_lens, np.where(used, table, -1).reshape(-1), positions, slots), [0]

@@ -212,3 +212,9 @@ def test_norm_rope_refuses_q_out_over_keys_or_values(call):
     """Three tokens of two heads, rows of 512 bytes: one workgroup would write what another reads."""
     assert rope(fq._lib, **call) == -2
     assert "q_out overlaps k or v" in fq.fq_last_error()
+
+
+def test_batch_keeps_positions_on_their_side():
+    """Positions that int32 does not hold stay beyond the table's end, or ahead of its start."""
+    b = fq.PagedBatch([4], [4], [[0]], 16, 4, positions=[2 ** 31 + 5, -2 ** 31 - 5, 2 ** 32, 7], device="cpu")
+    assert b.positions.tolist() == [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 7]
