@@ -115,7 +115,7 @@ __device__ __forceinline__ h4 lds_column(const _Float16 *at)
 // operands, values through a part of LDS of the wavefront's own (no barrier in the loop), and one merge of the four at the end.  Bound by the read
 // of the cache (one token of 32 heads over 100003 positions of 8 key/value heads: 410 MB in 69 us, 5.9 TB/s, and 6 for the join), short calls by the chain of
 // loads: length and table, keys and values, output (330 positions of 32 heads 7.5 us).  With SCORES the scaled scores of every row are left for the column sums, which need the sum over all splits first.
-constexpr int FEW = 16;
+constexpr int FEW = 16, FEW_CHUNK = 16 * 64; // rows; the most positions of a split: a lane of a wavefront has the page of sixteen
 constexpr float RAISE_FEW = 15.f, DOWN_FEW = 0x1p-15f; // powers of two; a weight is at most 1 here, and 65504 the largest in fp16
 
 typedef const __attribute__((address_space(4))) int *const_ints; // read through the scalar cache; nothing writes them in these kernels
@@ -162,10 +162,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         return;
     const int begin = split * p.chunk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // The pages of 64 blocks of sixteen positions, a lane each, asked for together with the lengths: one wait less ahead of the cache.
-    const int *table = p.s.table + (size_t)b * p.s.table_stride;
-    const auto block_pages = [&](int t) { return table[min(((t >> 4) + lane) >> (p.s.page_log2 - 4), p.s.table_stride - 1)]; };
-    int pages = block_pages(begin);
+    // The pages of all blocks of sixteen positions of the split, a lane each, asked for together with the lengths: one wait less ahead of the cache.
+    const int pages = p.s.table[(size_t)b * p.s.table_stride + min(((begin >> 4) + lane) >> (p.s.page_log2 - 4), p.s.table_stride - 1)];
     const int q0 = ((const_ints)p.s.q_start)[b], q1 = ((const_ints)p.s.q_start)[b + 1], len = min(max(((const_ints)p.s.seq_len)[b], 0), p.s.max_len);
     const int first = min(max(q0, 0), p.s.tokens), n = min(max(q1, first), p.s.tokens) - first, rows = min(n * p.group, FEW);
     const int end = min(len, begin + p.chunk);
@@ -198,12 +196,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
     // Read once, and past the caches' usual order of eviction: a token over 100003 positions 83.8 -> 75.6 us, with column sums of 24 sequences 70 -> 63.
     for (int t0 = begin + 32 * wave; t0 < end; t0 += 128) {
         const int block = (t0 - begin) >> 4; // of the split
-        if ((block & 63) < 8 && block >= 64) // the wavefront's first step among the next 64 blocks
-            pages = block_pages(begin + 16 * (block & ~63));
         h8 kk[2][4], vv[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int page = min(max(__builtin_amdgcn_readlane(pages, (block + i) & 63), 0), p.s.pages - 1);
+            const int page = min(max(__builtin_amdgcn_readlane(pages, block + i), 0), p.s.pages - 1);
             const size_t at = ((((size_t)page * p.kv_heads + kvh) << p.s.page_log2) | (size_t)((t0 + 16 * i) & ((1 << p.s.page_log2) - 1))) * PD;
             const _Float16 *k = p.k + at, *v = p.v + at;
 #pragma unroll
@@ -1066,7 +1062,7 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
         s.tiles = b.seqs;
         const long long jobs = (long long)b.seqs * kv_heads;
         const auto pieces = [&](int chunk) { return jobs * ((b.max_len + chunk - 1) / chunk); };
-        const bool one = b.max_len <= (jobs >= 160 ? 1024 : jobs >= 128 ? 512 : 384);
+        const bool one = b.max_len <= (jobs >= 160 ? FEW_CHUNK : jobs >= 128 ? 512 : 384); // no split is longer than FEW_CHUNK
         s.chunk = one ? (b.max_len + 127) / 128 * 128 : pieces(128) <= 384 ? 128 : pieces(256) <= 384 ? 256 : 512;
     } else {
         // steps of a tile, all splits together; several sequences are taken to be half as long as the longest where the caller does not say

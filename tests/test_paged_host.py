@@ -218,3 +218,17 @@ def test_batch_keeps_positions_on_their_side():
     """Positions that int32 does not hold stay beyond the table's end, or ahead of its start."""
     b = fq.PagedBatch([4], [4], [[0]], 16, 4, positions=[2 ** 31 + 5, -2 ** 31 - 5, 2 ** 32, 7], device="cpu")
     assert b.positions.tolist() == [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 7]
+
+
+def test_splits_of_single_tokens_are_within_a_wavefront_of_pages():
+    """At most 1024 positions, 64 blocks of sixteen: a lane holds the page of one, and nothing asks for more on the way."""
+    rng = np.random.default_rng(1)
+    for _ in range(3000):
+        kv, group, seqs, S = (int(2 ** rng.uniform(0, t)) for t in (6, 4, 8, 20))
+        n = int(rng.integers(1, max(16 // group, 1) + 1))
+        b = batch(seqs=seqs, tokens=seqs * n, max_q=n, max_len=S, table_stride=(S + 15) // 16)
+        if n * seqs * kv * group >= 1 << 26:
+            continue
+        out = np.zeros(3, dtype=np.int32)
+        assert fq._lib.fq_attn_paged_route(ctypes.byref(b), kv * group, kv, out.ctypes.data_as(ctypes.c_void_p)) == 0
+        assert out[0] == 16 and 128 <= out[2] <= 1024 and (out[1] - 1) * out[2] < S <= out[1] * out[2], (kv, group, seqs, n, S)
