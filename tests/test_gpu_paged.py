@@ -745,3 +745,47 @@ def test_rows_too_far_apart_are_refused(fq, torch):
                      lambda: fq.fq_qk_norm_rope(near, far, near, b, rope, pool, pool, out=out), lambda: fq.fq_qk_norm_rope(near, near, far, b, rope, pool, pool, out=out)):
             with pytest.raises(ValueError):
                 call()
+
+
+@pytest.mark.parametrize("most, heads, kv, splits", [(1400, 8, 4, 3), (2500, 16, 4, 5), (9000, 4, 2, 18)])
+def test_single_tokens_of_many_long_sequences(fq, torch, most, heads, kv, splits):
+    """More sequences than a wavefront has lanes, more workgroups than are resident, several splits: workgroups find their sequence and split by
+    the lengths.  Some sequences have no tokens, no positions, or two tokens."""
+    rng = np.random.default_rng(most)
+    lengths = np.exp(rng.uniform(0, np.log(most), 150)).astype(int)
+    lengths[[3, 64, 127, 149]] = 0, most, most - 1, 1
+    seqs = [(int(rng.choice((0, 1, 1, 1, 2))), int(S)) for S in lengths]
+    seqs[64], seqs[3] = (1, most), (1, 0)
+    table, pages = deal(np.random.default_rng(0), [S for _, S in seqs], 64)
+    b = fq.PagedBatch([n for n, _ in seqs], [S for _, S in seqs], table, 64, pages)
+    assert fq.fq_attn_paged_route(b, heads, kv)[:2] == (16, splits) and len(seqs) * kv * splits > 768
+    run(fq, torch, rng, seqs, heads, kv, 64)
+
+
+@pytest.mark.parametrize("n, S, heads, kv, splits", [(1, 9000, 4, 1, 71), (2, 40000, 8, 1, 313), (1, 70000, 2, 2, 137)])
+def test_tokens_with_more_splits_than_lanes(fq, torch, n, S, heads, kv, splits):
+    """Sixteen wavefronts join the splits of a row."""
+    table, pages = deal(np.random.default_rng(0), [S], 256)
+    assert fq.fq_attn_paged_route(fq.PagedBatch([n], [S], table, 256, pages), heads, kv)[:2] == (16, splits)
+    run(fq, torch, np.random.default_rng(S), [(n, S)], heads, kv, 256)
+
+
+def test_rotation_of_more_tokens_than_a_grid_has_rows(fq, torch):
+    """Two launches: tokens from the 65536th on have their own positions and slots."""
+    T, page = 65535 + 300, 256
+    rng = np.random.default_rng(79)
+    pages = -(-T // page)
+    table = rng.permutation(pages)[None]
+    b = fq.PagedBatch([T], [T], table, page, pages, positions=np.arange(T)[::-1] % 1000)
+    x = rng.normal(size=(3, T, 128)).astype(np.float16)
+    rope, gain = fq.rope_table(1000), (1 + 0.3 * rng.normal(size=(2, 128))).astype(np.float16)
+    kp, vp = (torch.zeros(pages, 1, page, 128, dtype=torch.float16, device="cuda") for _ in range(2))
+    out = fq.fq_qk_norm_rope(*(dev(torch, t) for t in x), b, rope, kp, vp, *(dev(torch, g) for g in gain))
+    at = torch.from_numpy(table[0]).cuda()
+    rows_k, rows_v = (p[at].reshape(-1, 128)[:T].cpu().numpy() for p in (kp, vp))
+    assert np.array_equal(rows_v, x[2])
+    for got, t, g in ((out.cpu().numpy(), x[0], gain[0]), (rows_k, x[1], gain[1])):
+        y = ref.norm_rope(t, b.positions.cpu().numpy(), rope.cpu().numpy(), g)
+        size = ref.norm_rope(np.abs(t), b.positions.cpu().numpy(), np.abs(rope.cpu().numpy()) * [1, -1], np.abs(g))
+        pair = np.maximum(size.reshape(T, -1, 2).max(-1), np.abs(y).reshape(T, -1, 2).max(-1))
+        assert (np.abs(got - y) <= U * np.abs(y) + 2.0 ** -18 * 2 * np.repeat(pair, 2, axis=1) + 2.0 ** -24).all()
