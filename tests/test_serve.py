@@ -320,3 +320,42 @@ def test_a_cut_of_what_is_short_or_empty(gpu):
     assert torch.equal(rows(a, 17), before) and torch.equal(server.weights[:, a], weights[:, a]) and bool((server.weights[:, b, :, 20:] == 0).all())
     out = server.step(stack, bitvec, {c: x[:2], a: x[:1]})
     assert all(bool(torch.isfinite(t).all()) for t in out.values()) and server.length(c) == 2
+
+
+@pytest.mark.gpu
+def test_serving_goes_on_across_a_move_of_the_hosted_model(gpu):
+    """Sequences served by an elastic model that moves between steps (one move queued while a step is served), cut on the way: as by blocks with every
+    packing resident, bit for bit; bit widths that are no longer resident are refused and change nothing."""
+    fq, torch = gpu
+    from paper_2501_07139_amd import elastic
+    from paper_2501_07139_amd.serve import PagedServer
+
+    H, kv, ffn, L = 512, 2, 640, 2
+    shapes = [(H, H), (128 * kv, H), (128 * kv, H), (H, H), (ffn, H), (ffn, H), (H, ffn)]
+    quantized = [[{b: oracle.quantize_rtn(fq_synth.weights(90 + 16 * l + j, N, K), b) for b in (3, 4, 8)} for j, (N, K) in enumerate(shapes)] for l in range(L)]
+    full = fq.Stack([[{b: fq.PackedMatrix.from_host(*m[b], b) for b in m} for m in block] for block in quantized])
+    path = [(8,) * 14, (8,) * 9 + (4,) + (8,) * 4, (4, 8, 8) + (8,) * 6 + (4,) + (8,) * 4, (4,) * 14, (3,) * 14]
+    model = elastic.ElasticModel(elastic.HostStore(quantized), path)
+    moving, fixed = (PagedServer(s, slots=2, pages=20, page=16, max_positions=128, keep=24, recent=6, limit=36) for s in (model.stack, full))
+    slots = [moving.open(), moving.open()]
+    assert [fixed.open(), fixed.open()] == slots
+    x = torch.randn(40, H, device="cuda").half()
+    at = 0
+    for target, rows in ((0, (20, 3)), (2, (1, 9)), (4, (17, 1)), (1, (1, 1)), (3, (5, 12))):
+        if target == 1:
+            model.begin_move(target)
+            before = [(moving.length(i), moving.seqs[i].position) for i in slots]
+            with pytest.raises(ValueError):
+                moving.step(model.stack, path[target], {slots[0]: x[:1]})  # not committed: those packings are not in the table yet
+            assert [(moving.length(i), moving.seqs[i].position) for i in slots] == before
+            model.commit()
+        else:
+            model.move_to(target)
+        assert model.index == target and tuple(model.bitvec) == path[target]
+        tokens = {i: x[at % 20:][:n] for i, n in zip(slots, rows)}
+        at += 7
+        got, want = moving.step(model.stack, model.bitvec, tokens), fixed.step(full, path[target], tokens)
+        for i in slots:
+            assert torch.equal(got[i].view(torch.int16), want[i].view(torch.int16)) and moving.length(i) == fixed.length(i)
+    assert moving.length(slots[0]) < moving.seqs[slots[0]].position  # it has been cut
+    assert model.resident_bytes() == model.footprints[3] and torch.equal(moving.weights, fixed.weights)
