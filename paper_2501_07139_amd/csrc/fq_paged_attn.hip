@@ -1030,8 +1030,10 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 // positions takes a workgroup 0.69 (128 rows: 1.0) by itself, and 256 CUs together do one in 0.9 (1.36) each, as the card lowers its clock
 // under that load; joining splits takes 4 and two passes over the parts at 4 TB/s.  Where the caller says how many positions and (token, position) pairs
 // several sequences have together, those are the steps and the parts, workgroups without work are 0.001 each, and the longest tile's steps count by 0.3 in
-// any case, as such tiles come late and alone: 300 tokens and 63 single ones, one of them at
-// the end of 32768 positions, 528 -> 109 us, and 500 with 15 at up to 16384 185 -> 65 (three of 67 tokens at most 13.6 -> 15.1, the worst of 17); without, all are taken to be half as long as the longest.  Over 37 sizes of 5 to 3000 tokens and 256
+// any case, as such tiles come late and alone, and more than 8 splits cost 4 more (a workgroup a row joins them); without, all are taken to be half as
+// long as the longest.  That choice stays unless the other is to save 2.5 us, which is how far the estimate is off on calls of 15 to 30 us: 300 tokens and 63 single
+// ones, one of them at the end of 32768 positions, 528 -> 111 us, and 500 with 15 at up to 16384 185 -> 65; of 720 ragged batches of 2 to 8 chunks
+// 158 are divided otherwise and take 20 % less on average, three of them over 5 % longer, at most 11 % (without the two, 18 of 300, at most 24 %).  Over 37 sizes of 5 to 3000 tokens and 256
 // to 16000 positions its choice takes 1.8 % longer than the best of both heights and six lengths, at most 8 % (17 % where several sequences are all as
 // long as the longest).  Some, as measured: 16 tokens, 8 key/value
 // heads of 4 queries, 16000 positions 171 in one split, 23.5 / 21.2 / 24.8 in splits of 1024 / 512 / 256; 2048 tokens of 32 heads 50 in tiles of 128 rows, 66
@@ -1073,17 +1075,23 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
             const double full = (double)b.pairs * group / height, open = 1 - full / b.positions; // of a sequence's last tile
             return (full + b.positions * (open > 0.5 ? open : 0.5)) / KT + 0.5 * tiles(height);
         };
+        const auto estimate = [&](int rows, int chunk, int splits, bool known) {
+            const double alone = (double)chunk / KT * (rows == 64 ? 0.69 : 1.0), together = steps(rows, known) * kv_heads / 256 * (rows == 64 ? 0.9 : 1.36);
+            const double all = (double)items * splits, longer = (double)b.pairs * heads / chunk + items, parts = known && longer < all ? longer : all;
+            return 6 + (alone > together ? alone : together) + (splits > 1 ? 4 + parts * 1040e-6 / 4 : 0) +
+                   (known ? 0.3 * alone + (splits > 1 ? 0.001 * tiles(rows) * kv_heads * splits : 0) + ((b.max_len + chunk - 1) / chunk > 8 ? 4 : 0) : 0);
+        };
+        const auto roomy = [&](int splits) { return splits > 1 && (double)items * splits > 1 << 20; }; // the workspace has room for every split of every row
         const auto choose = [&](int lowest, int highest, bool known) {
             double best = 0;
+            if (const int splits = known ? (b.max_len + s.chunk - 1) / s.chunk : 0; known && !roomy(splits))
+                best = estimate(s.rows, s.chunk, splits, true) - 2.5; // what is to be undercut
             for (int rows = lowest; rows <= highest; rows *= 2)
                 for (int splits = 1; splits == 1 || b.max_len / splits > 128; splits *= 2) { // none shorter than 256 positions
                     const int chunk = ((b.max_len + splits - 1) / splits + 127) / 128 * 128;
-                    const double alone = (double)chunk / KT * (rows == 64 ? 0.69 : 1.0), together = steps(rows, known) * kv_heads / 256 * (rows == 64 ? 0.9 : 1.36);
-                    const double all = (double)items * splits, longer = (double)b.pairs * heads / chunk + items, parts = known && longer < all ? longer : all;
-                    if (known && splits > 1 && all > 1 << 20) // the workspace has room for every split of every row
+                    if (known && roomy(splits))
                         continue;
-                    const double us = 6 + (alone > together ? alone : together) + (splits > 1 ? 4 + parts * 1040e-6 / 4 : 0) +
-                                      (known ? 0.3 * alone + (splits > 1 ? 0.001 * tiles(rows) * kv_heads * splits : 0) : 0);
+                    const double us = estimate(rows, chunk, splits, known);
                     if (best == 0 || us < best) {
                         best = us;
                         s.rows = rows;
