@@ -165,9 +165,9 @@ class PagedServer:
                 taken: Dict[int, List[int]]) -> torch.Tensor:
         """All blocks over the tokens, their sequences as long as they are with them; the account stays as it is."""
         positions = [np.arange(self.seqs[i].position, self.seqs[i].position + rows[i]) for i in order]
-        batch = PagedBatch([rows.get(i, 0) for i in range(self.slots)],
-                           [self.seqs[i].length + rows.get(i, 0) if i in self.seqs else 0 for i in range(self.slots)],
-                           self._table({i: s.pages + taken.get(i, []) for i, s in self.seqs.items()}), self.pool.page, self.pool.pages,
+        # sequences without tokens count as empty: nothing of theirs is read or changed, and the longest decides how a call is divided
+        batch = PagedBatch([rows.get(i, 0) for i in range(self.slots)], [self.seqs[i].length + rows[i] if i in rows else 0 for i in range(self.slots)],
+                           self._table({i: self.seqs[i].pages + taken[i] for i in order}), self.pool.page, self.pool.pages,
                            positions=np.concatenate(positions), device=self.device)
         x = torch.cat([tokens[i] for i in order])
         for l, w in enumerate(matrices):

@@ -359,3 +359,20 @@ def test_serving_goes_on_across_a_move_of_the_hosted_model(gpu):
             assert torch.equal(got[i].view(torch.int16), want[i].view(torch.int16)) and moving.length(i) == fixed.length(i)
     assert moving.length(slots[0]) < moving.seqs[slots[0]].position  # it has been cut
     assert model.resident_bytes() == model.footprints[3] and torch.equal(moving.weights, fixed.weights)
+
+
+def test_sequences_without_tokens_do_not_size_a_step(monkeypatch):
+    """A long sequence that waits takes no part in how the others' step is divided, nor in its workspace."""
+    torch, server, stack, bitvec, calls = on_the_host(monkeypatch)
+    from paper_2501_07139_amd import serve
+
+    batches = []
+    monkeypatch.setattr(serve, "fq_attn_paged", lambda q, batch, *a, **k: batches.append(batch) or q)
+    a, b = server.open(), server.open()
+    x = torch.zeros(100, 512, dtype=torch.float16)
+    server.step(stack, bitvec, {a: x})
+    server.step(stack, bitvec, {b: x[:9]})
+    server.step(stack, bitvec, {b: x[:1]})
+    server.step(stack, bitvec, {a: x[:1], b: x[:1]})
+    assert [t.max_len for t in batches[::2]] == [100, 9, 10, 101] and [t.seq_len.tolist() for t in batches[::2]] == [[100, 0], [0, 9], [0, 10], [101, 11]]
+    assert server.length(a) == 101 and server.length(b) == 11
