@@ -755,7 +755,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_ker
 // step through double-buffered LDS, straight from memory; with lse known a weight is one exponential.  Rows are the first operand here, so that a
 // lane has sixteen weights of ONE position and adds them up in place; what differs by row (lse, positions seen) is laid beside the rows.  One
 // workgroup owns its sums and the parts are added in order: no atomics, the same sums every time.  Bound by the exponentials and the unequal work of the
-// workgroups (three prompts, 2628 tokens of 32 heads and 8 key/value heads: 33 us beside the attention's 41, and 4.7 for the join).
+// workgroups (three prompts, 2628 tokens of 32 heads and 8 key/value heads: 33 us beside the attention's 41, and 4.6 for the join).
 constexpr int WK = 256, WR = 64; // positions of a workgroup, rows of a step
 
 // Rows of part `part` that see positions from t0 on: [lo, hi).
@@ -1032,7 +1032,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_weights_kernel(PagedAttnAr
 // several sequences have together, those are the steps and the parts, workgroups without work are 0.001 each, and the longest tile's steps count by 0.3 in
 // any case, as such tiles come late and alone, and more than 8 splits cost 4 more (a workgroup a row joins them); without, all are taken to be half as
 // long as the longest.  That choice stays unless the other is to save 2.5 us, which is how far the estimate is off on calls of 15 to 30 us: 300 tokens and 63 single
-// ones, one of them at the end of 32768 positions, 528 -> 111 us, and 500 with 15 at up to 16384 185 -> 65; of 720 ragged batches of 2 to 8 chunks
+// ones, one of them at the end of 32768 positions, 528 -> 110 us, and 500 with 15 at up to 16384 185 -> 65; of 720 ragged batches of 2 to 8 chunks
 // 158 are divided otherwise and take 20 % less on average, three of them over 5 % longer, at most 11 % (without the two, 18 of 300, at most 24 %).  Over 37 sizes of 5 to 3000 tokens and 256
 // to 16000 positions its choice takes 1.8 % longer than the best of both heights and six lengths, at most 8 % (17 % where several sequences are all as
 // long as the longest).  Some, as measured: 16 tokens, 8 key/value

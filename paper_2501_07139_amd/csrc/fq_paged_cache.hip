@@ -74,7 +74,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeArgs p)
 // Of a head's len positions the last `recent` stay, and of the others the keep - recent that weigh most (equal weights: the lower
 // position).  The weight that the last one kept has is found eight bits at a time (radix selection over keys that order like the weights), then
 // one pass in order numbers what stays.  Selecting is bound by latency: the length, the weights, a barrier and a scan of 256 counts a digit.  Each
-// wavefront has consecutive positions, few enough to stay in registers, and scans the counts for itself.
+// wavefront has consecutive positions, few enough to stay in registers, and scans the counts for itself.  Beyond 16384 positions they are read again for every digit
+// by the one workgroup of a head (100003 positions of 8 heads, 4096 stay: 117 us, and 8 for the copy).
 //
 // Where a call has few heads, a head's rows that stay are dealt to several workgroups, each of which selects for itself and then copies its share:
 // one launch, the whole chip copying (caches cold, one launch against two: one sequence of 611 positions, 32 heads, 512 stay 11.4 against 14.0 us in the first
