@@ -729,11 +729,12 @@ def _same_device(what: str, device, *tensors):
 def _fresh(shape, dtype, device, stream):
     """A tensor made by a call for work on `stream`: told to the allocator, so that its memory is not given away before."""
     t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None and t.numel():
-        s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
-        if s != torch.cuda.current_stream(device):
-            s.wait_stream(torch.cuda.current_stream(device))  # its memory may still be in use by what was queued here
-            t.record_stream(s)
+    here = None if stream is None or not t.numel() else torch.cuda.current_stream(device)
+    if here is not None and (_stream(stream) or 0) != here.cuda_stream:
+        if isinstance(stream, int):  # 0: the default stream, which is no external one (torch takes a stream of its own for it)
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        stream.wait_stream(here)  # its memory may still be in use by what was queued here
+        t.record_stream(stream)
     return t
 
 

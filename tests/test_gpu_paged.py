@@ -789,3 +789,29 @@ def test_rotation_of_more_tokens_than_a_grid_has_rows(fq, torch):
         size = ref.norm_rope(np.abs(t), b.positions.cpu().numpy(), np.abs(rope.cpu().numpy()) * [1, -1], np.abs(g))
         pair = np.maximum(size.reshape(T, -1, 2).max(-1), np.abs(y).reshape(T, -1, 2).max(-1))
         assert (np.abs(got - y) <= U * np.abs(y) + 2.0 ** -18 * 2 * np.repeat(pair, 2, axis=1) + 2.0 ** -24).all()
+
+
+def test_handles_of_streams(fq, torch, monkeypatch):
+    """What a call makes for a stream that is not the current one waits for the current one and is told to the allocator for that very stream, the
+    default one (handle 0) among them."""
+    side, device, waits, records = torch.cuda.Stream(), torch.device("cuda", torch.cuda.current_device()), [], []
+    wait, record = torch.cuda.Stream.wait_stream, torch.Tensor.record_stream
+    monkeypatch.setattr(torch.cuda.Stream, "wait_stream", lambda self, other: (waits.append((self.cuda_stream, other.cuda_stream)), wait(self, other))[1])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: (records.append(s.cuda_stream), record(self, s))[1])
+    with torch.cuda.stream(side):
+        for handle in (0, torch.cuda.default_stream()):
+            fq._fresh((8,), torch.float32, device, handle)
+        for handle in (None, side, side.cuda_stream):
+            fq._fresh((8,), torch.float32, device, handle)
+    fq._fresh((8,), torch.float32, device, side.cuda_stream)
+    fq._fresh((8,), torch.float32, device, 0)
+    assert waits == [(0, side.cuda_stream)] * 2 + [(side.cuda_stream, 0)] and records == [0, 0, side.cuda_stream]
+    rng = np.random.default_rng(83)
+    table, pages, k, v, q = case(rng, [(1, 900)], 4, 1, 32)
+    args = (dev(torch, q), fq.PagedBatch([1], [900], table, 32, pages), dev(torch, k), dev(torch, v))
+    want = fq.fq_attn_paged(*args)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = fq.fq_attn_paged(*args, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
