@@ -518,6 +518,82 @@ int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void 
                    int dst_stride, int dst_pages, void *k_out, void *v_out, int32_t *kept, int32_t *new_len,
                    float *weights_out, int weights_out_stride, void *stream);
 
+/*
+ * Several continuations of a sequence at once (drafted trees whose tokens the model checks in one pass, and beams).  The last `tail` positions
+ * of a sequence are nodes: each has a mask of the nodes that it sees, its own bit among them where it sees itself, in words of 64 bits (bit j of
+ * word w is node 64 w + j, counted from the tail's first position).  Positions ahead of the tail are seen by all.  Masks have 1 to
+ * FQ_TREE_WORDS words a row.
+ */
+#define FQ_TREE_WORDS 64
+
+/*
+ * The arrays of a batch from request lengths, on the device, so that a captured step can follow lengths that the host does not know: page
+ * tables with pages dealt from a stack of free ones, slots and positions of the tokens, masks of drafted trees.  Of sequence b
+ *   new_tokens[b] < 0: it is closed: its held[b] pages go back on the stack, in order, after those of the closed sequences ahead of it
+ *     (its table row stays as it is), seq_len[b] = held_out[b] = 0;
+ *   else it has cached[b] positions in its pages and gets n = new_tokens[b] tokens (cut to max_q, to max_len - cached[b] positions and to
+ *     what is left of `tokens`): seq_len[b] = cached[b] + n, and where its held[b] pages do not hold these, pages are taken from
+ *     the top of the stack, sequence after sequence, all given ones being on it first.
+ * q_start[b] counts the tokens ahead.  Token i: slots = its place in the pools, or -1 where no page was left for it; positions = next_position[b]
+ * (NULL: cached[b]) + i.  With parents (int32 [tokens]: of each token the one that it goes on from, counted within its sequence; what is not
+ * a token ahead of it, -1 for instance, makes it a root) positions = next_position[b] + its depth, and mask (or NULL), uint64
+ * [tokens][mask_words], has its own bit and those of its ancestors; max_q at most 64 mask_words then, and 64 FQ_TREE_WORDS without a mask.  Rows of
+ * positions, slots and mask behind the last token: 0, -1, 0.
+ * batch: its sizes are the bounds; its arrays q_start, seq_len and table (all columns; those behind what is held are written as pages are
+ * taken) are the output.  free_pages int32 [pages], of which the first free_count[0] are free; free_out[0] of them are free afterwards.
+ * lacking[0]: pages that the stack did not have; held_out counts those that a sequence has, and the table has -1 for the others.
+ * In place: cached may be seq_len, held held_out, free_count free_out; no output may overlap an input or another otherwise.
+ */
+int fq_paged_plan(const fq_paged_batch *batch, const int32_t *new_tokens, const int32_t *cached, const int32_t *next_position,
+                  const int32_t *parents, const int32_t *held, int32_t *held_out, int32_t *free_pages, const int32_t *free_count,
+                  int32_t *free_out, int32_t *lacking, int32_t *positions, int32_t *slots, uint64_t *mask, int mask_words, void *stream);
+
+/*
+ * fq_attn_paged where tokens are nodes: token i of a sequence of S positions sees t < S - tail, and of the tail's positions those whose bit
+ * t - (S - tail) its mask has (bits behind the mask's words are 0).  tail int32 [seqs], cut to 0..S; NULL: the tokens of the call.  With beams it is
+ * longer than those: their earlier steps are in it.  mask uint64 [tokens][mask_words].  Everything else, rows that see nothing and values
+ * that are not finite among it, as there; a token whose own bit is not set does not see itself.
+ */
+size_t fq_attn_tree_workspace_bytes(const fq_paged_batch *batch, int n_heads, int n_kv_heads);
+int fq_attn_tree(const fq_paged_batch *batch, const uint64_t *mask, int mask_words, const int32_t *tail, const void *q, int ldq, int n_heads,
+                 int n_kv_heads, const void *k_pages, const void *v_pages, float scale, void *out, float *lse, void *workspace,
+                 size_t workspace_bytes, void *stream);
+
+/*
+ * What of a tree stays: the rows of a path through it are moved together, right behind the positions ahead of the tail, in the pools of all
+ * layers, k_pages and v_pages fp16 [layers][pages][n_kv_heads][page][128].  path int32 [seqs][path_stride]: nodes in rising order, accepted[b]
+ * of them; position S - tail + path[b][k] goes to S - tail + k, and new_len[b] = S - tail + accepted[b].  Positions without a page (-1) stay out.
+ * With parents, drafted and following (int32 [tokens]) the path is found here and written: the first token of a sequence is on it, and
+ * from token c it goes on with the first token i > c whose parents[i] is c and whose drafted[i] is following[c], what the model itself says comes
+ * after c; until there is none, or path_stride tokens.  bonus[b] (or NULL) = following of the last one, -1 for a sequence without tokens; behind
+ * the path there is -1.  The tail is the tokens of the call then, and `tail` NULL.
+ * With none of the three, path and accepted are read (the beam that won, for instance; accepted is cut to path_stride and to the tail, a node
+ * below its place in the path is taken for that place, one behind the tail for its last), bonus NULL; tail as in fq_attn_tree.
+ * Outputs overlap neither inputs (new_len is not seq_len) nor each other.
+ */
+int fq_tree_commit(const fq_paged_batch *batch, const int32_t *tail, const int32_t *parents, const int32_t *drafted, const int32_t *following,
+                   void *k_pages, void *v_pages, int layers, int n_kv_heads, int32_t *path, int path_stride, int32_t *accepted,
+                   int32_t *bonus, int32_t *new_len, void *stream);
+
+/*
+ * One step of beam search: of the continuations of a request's beams by every token,
+ *   total[b][v] = scores[b] + logits[b][v] - log sum_u exp(logits[b][u]),
+ * the `width` largest, largest first, of equal ones the lower b * vocab + v.  Held in 64 bits; scores_out is rounded to fp32 once.
+ * logits fp16, row (request * beams + beam) at that many times ld elements; scores fp32 [requests][beams]: -inf (or NaN) for beams that are not there.
+ * done int32 [requests][beams] or NULL: beams that have ended go on as they are, with token eos and their score.  A total that is NaN (a row with a NaN or
+ * +inf, or of -inf only) or -inf (a token that is masked out) is never taken; where fewer than `width` are left, parent and token are -1, the
+ * score -inf, done 1 and the mask 0.
+ * parent, token int32 [requests][width], scores_out fp32, done_out int32 (or NULL): done[parent], or token is eos (eos < 0: no token is).
+ * mask_out (or NULL) uint64 [requests][width][mask_words] = mask [requests][beams][mask_words] (NULL: zeros) of the parent, and bit tail[request]
+ * (NULL: 0) + place, the node that the beam's token will be: with it the beams are a tree for fq_attn_tree, and nothing of the cache moves.
+ * beams and width 1 to 64, vocab up to 2^18, requests * beams below 2^24.  workspace: fq_beam_step_workspace_bytes bytes, 16-byte aligned.
+ * Outputs and workspace overlap neither inputs nor each other.
+ */
+size_t fq_beam_step_workspace_bytes(int requests, int beams, int vocab, int width);
+int fq_beam_step(const void *logits, int64_t ld, const float *scores, const int32_t *done, int eos, int requests, int beams, int vocab, int width,
+                 int32_t *parent, int32_t *token, float *scores_out, int32_t *done_out, const uint64_t *mask, uint64_t *mask_out,
+                 int mask_words, const int32_t *tail, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -103,6 +103,12 @@ def _load() -> ctypes.CDLL:
         "fq_attn_paged_route": (ci, [ctypes.POINTER(fq_paged_batch), ci, ci, vp]),
         "fq_attn_paged": (ci, [ctypes.POINTER(fq_paged_batch), vp, ci, ci, ci, vp, vp, ctypes.c_float, vp, vp, vp, vp, ci, vp, sz, vp]),
         "fq_cache_evict": (ci, [ctypes.POINTER(fq_paged_batch), vp, vp, ci, vp, ci, ci, ci, vp, ci, ci, vp, vp, vp, vp, vp, ci, vp]),
+        "fq_paged_plan": (ci, [ctypes.POINTER(fq_paged_batch), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ci, vp]),
+        "fq_attn_tree_workspace_bytes": (sz, [ctypes.POINTER(fq_paged_batch), ci, ci]),
+        "fq_attn_tree": (ci, [ctypes.POINTER(fq_paged_batch), vp, ci, vp, vp, ci, ci, ci, vp, vp, ctypes.c_float, vp, vp, vp, sz, vp]),
+        "fq_tree_commit": (ci, [ctypes.POINTER(fq_paged_batch), vp, vp, vp, vp, vp, vp, ci, ci, vp, ci, vp, vp, vp, vp]),
+        "fq_beam_step_workspace_bytes": (sz, [ci, ci, ci, ci]),
+        "fq_beam_step": (ci, [vp, ctypes.c_int64, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -126,7 +132,7 @@ def _load_bind():
                       "`python paper_2501_07139_amd/build.py` builds it", RuntimeWarning, stacklevel=2)
         return None
     names = ("fq_qlinear_tile", "fq_qlinear_mixed", "fq_dense_f16", "fq_head_nll", "fq_token_nll", "fq_logit_l2", "fq_qk_norm_rope",
-             "fq_attn_paged", "fq_cache_evict")
+             "fq_attn_paged", "fq_cache_evict", "fq_paged_plan", "fq_attn_tree", "fq_tree_commit", "fq_beam_step")
     _bind.bind(*(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
     return _bind
 
@@ -141,7 +147,8 @@ EXPORTS = ("fq_last_error", "fq_version", "fq_quantize_rtn", "fq_packed_bytes", 
            "fq_decode_give_up_ticks", "fq_async_error", "fq_clear_async_error", "fq_decode_partition", "fq_decode_persistent",
            "fq_decode_persistent_launches", "fq_qlinear_route", "fq_qlinear_tall_tile", "fq_dense_route",
            "fq_qk_norm_rope", "fq_attn_paged_workspace_bytes", "fq_attn_paged", "fq_attn_paged_route",
-           "fq_cache_evict")
+           "fq_cache_evict", "fq_paged_plan", "fq_attn_tree_workspace_bytes", "fq_attn_tree", "fq_tree_commit",
+           "fq_beam_step_workspace_bytes", "fq_beam_step")
 
 
 # The calls below that small ones are made of go through _bind where nothing is to be allocated; it answers None to whatever it does
@@ -651,6 +658,7 @@ def fq_prefill_forward(stack: Stack, bitvec, x, k_cache, v_cache, rope, out=None
 
 # ------------------------------------------------------------ paged cache
 PAGE_SIZES = (16, 32, 64, 128, 256)
+TREE_WORDS = 64
 
 
 class PagedBatch:
@@ -698,6 +706,29 @@ class PagedBatch:
         self.struct = fq_paged_batch(_dp(self.q_start), _dp(self.seq_len), _dp(self.table), seqs, tokens, self.max_q, self.max_len,
                                      table.shape[1], page, pages, int(seq_lens[q_lens > 0].sum()),
                                      int((q_lens * (np.maximum(seq_lens - q_lens, 0)) + np.minimum(q_lens, seq_lens) ** 2 // 2).sum()))
+
+    @classmethod
+    def reserve(cls, seqs: int, tokens: int, max_q: int, max_len: int, page: int, pages: int, mask_words: int = 0, device="cuda"):
+        """A batch whose arrays ``fq_paged_plan`` fills on the device: room for `tokens` rows, of one sequence at most `max_q`, and for
+        sequences of up to `max_len` positions.  It holds no pages at first: `held` int32 [seqs] and `free_pages` int32 [pages], of which the first
+        `free_count` [1] are free, are the state that a plan starts from and leaves; `lacking` [1] is what it was short of.  With
+        mask_words, `mask` int64 [tokens, mask_words] takes the masks of drafted trees."""
+        if page not in PAGE_SIZES or not 0 < pages <= (2 ** 31 - 1) // page:
+            raise FqError(-2, f"PagedBatch.reserve: {pages} pages of {page} positions (pages of {PAGE_SIZES}, 2^31 - 1 positions at most)")
+        if not 1 <= seqs <= 65535 or not 0 <= max_q <= tokens <= seqs * max_q or tokens >= 1 << 29 or not 1 <= max_len <= 1 << 24:
+            raise FqError(-2, f"PagedBatch.reserve: {seqs} sequences, {tokens} tokens, at most {max_q} of one, {max_len} positions")
+        if not 0 <= mask_words <= TREE_WORDS or (mask_words and max_q > 64 * mask_words):
+            raise FqError(-2, f"PagedBatch.reserve: {mask_words} words of masks (at most {TREE_WORDS}) for {max_q} tokens of a sequence")
+        b = cls.__new__(cls)
+        ints = lambda *shape, fill=0: torch.full(shape, fill, dtype=torch.int32, device=device)
+        b.q_start, b.seq_len, b.table = ints(seqs + 1), ints(seqs), ints(seqs, -(-max_len // page), fill=-1)
+        b.positions, b.slots, b.held, b.lacking = ints(tokens), ints(tokens, fill=-1), ints(seqs), ints(1)
+        b.free_pages = torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device)  # page 0 is taken first
+        b.free_count = ints(1, fill=pages)
+        b.mask = torch.zeros((tokens, mask_words), dtype=torch.int64, device=device) if mask_words else None
+        b.seqs, b.tokens, b.page, b.pages, b.max_q, b.max_len, b.device = seqs, tokens, page, pages, max_q, max_len, b.q_start.device
+        b.struct = fq_paged_batch(_dp(b.q_start), _dp(b.seq_len), _dp(b.table), seqs, tokens, max_q, max_len, b.table.shape[1], page, pages, 0, 0)
+        return b
 
 
 def _rows(t, width: int, what: str):
@@ -863,3 +894,198 @@ def fq_cache_evict(batch: PagedBatch, weights, k_pages, v_pages, dst_table, keep
                                dst_table.shape[1], k_out.shape[0], _dp(k_out), _dp(v_out), _dp(kept), _dp(new_len), _dp(weights_out),
                                0 if weights_out is None else weights_out.shape[2], _stream(stream)))
     return kept, new_len
+
+
+# ------------------------------------------------------------ trees of tokens
+def _on_current(what: str, device) -> None:
+    """The library launches on the current device: a call for another one's tensors would run on the wrong card."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _ints(t, shape, what: str):
+    if t is not None and tuple(_dev(t, torch.int32, what).shape) != tuple(shape):
+        raise ValueError(f"{what} must be int32 {list(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _masks(t, shape, what: str) -> int:
+    """Words of a row of masks."""
+    if _dev(t, torch.int64, what).dim() != len(shape) + 1 or tuple(t.shape[:-1]) != tuple(shape) or not 1 <= t.shape[-1] <= TREE_WORDS:
+        raise ValueError(f"{what} must be int64 {list(shape) + [f'1 to {TREE_WORDS}']}, got {tuple(t.shape)}")
+    return t.shape[-1]
+
+
+def fq_paged_plan(batch: PagedBatch, new_tokens, cached, next_position=None, parents=None, held_out=None, free_out=None, stream=None):
+    """Fills a batch made by ``PagedBatch.reserve`` from request lengths on the device, int32 [sequences] each: new_tokens (below 0: the
+    sequence is closed, and its pages are free), cached positions (may be batch.seq_len: a step after the one before) and, if not those,
+    the position of the next token.  parents int32 [tokens]: the tokens of a sequence are a drafted tree, each goes on from one ahead of
+    it (-1: a root); positions go by depth, and batch.mask has who sees whom.  What is held and free is changed in place, or left in
+    held_out [sequences] and free_out [1].  Returns the batch."""
+    if _bind is not None:
+        rc = _bind.paged_plan(batch, new_tokens, cached, next_position, parents, held_out, free_out, stream)
+        if rc is not None:
+            _check(rc)
+            return batch
+    if getattr(batch, "held", None) is None:
+        raise ValueError("fq_paged_plan: the batch must be one of PagedBatch.reserve")
+    n = batch.seqs
+    held_out, free_out = batch.held if held_out is None else held_out, batch.free_count if free_out is None else free_out
+    for t, shape, what in ((new_tokens, (n,), "new_tokens"), (cached, (n,), "cached"), (held_out, (n,), "held_out"), (free_out, (1,), "free_out"),
+                           (batch.positions, (batch.tokens,), "positions"), (batch.slots, (batch.tokens,), "slots"), (batch.held, (n,), "held"),
+                           (batch.free_pages, (batch.pages,), "free_pages"), (batch.free_count, (1,), "free_count"), (batch.lacking, (1,), "lacking")):
+        if t is None:
+            raise TypeError(f"{what} must be a device tensor")
+        _ints(t, shape, what)
+    _ints(next_position, (n,), "next_position")
+    _ints(parents, (batch.tokens,), "parents")
+    mask = batch.mask if parents is not None else None
+    words = 0 if mask is None else _masks(mask, (batch.tokens,), "mask")
+    _same_device("fq_paged_plan", batch.device, new_tokens, cached, next_position, parents, held_out, free_out, batch.positions, batch.slots, batch.held,
+                 batch.free_pages, batch.free_count, batch.lacking, mask)
+    _on_current("fq_paged_plan", batch.device)
+    _check(_lib.fq_paged_plan(batch.struct, _dp(new_tokens), _dp(cached), _dp(next_position), _dp(parents), _dp(batch.held), _dp(held_out),
+                              _dp(batch.free_pages), _dp(batch.free_count), _dp(free_out), _dp(batch.lacking), _dp(batch.positions), _dp(batch.slots),
+                              _dp(mask), words, _stream(stream)))
+    return batch
+
+
+def fq_attn_tree_workspace_bytes(batch: PagedBatch, n_heads: int, n_kv_heads: int) -> int:
+    return _lib.fq_attn_tree_workspace_bytes(batch.struct, n_heads, n_kv_heads)
+
+
+def fq_attn_tree(q, batch: PagedBatch, mask, k_pages, v_pages, tail=None, scale: Optional[float] = None, out=None, lse=None, workspace=None,
+                 stream=None):
+    """``fq_attn_paged`` for tokens that are nodes of a tree: each sees all positions ahead of its sequence's tail, and of the tail those whose bit
+    its mask has.  mask int64 [tokens, words], bit j of word w: position 64 w + j of the tail; tail int32 [sequences]: positions of
+    each one's tail, the tokens of the call if not given.  lse fp32 [tokens, heads] is written if given."""
+    scale = 128 ** -0.5 if scale is None else scale
+    if _bind is not None and out is not None:
+        rc = _bind.attn_tree(q, batch, mask, k_pages, v_pages, tail, scale, out, lse, workspace, stream)
+        if rc is not None:
+            _check(rc)
+            return out
+    n_kv = _pools(batch, k_pages, v_pages, batch.pages, "fq_attn_tree")
+    width = q.shape[-1]
+    ldq = _rows(q, width, "q")
+    heads = width // 128
+    if width % 128 or q.shape[0] != batch.tokens or heads % n_kv:
+        raise ValueError(f"fq_attn_tree: q [{batch.tokens}, 128 heads], heads a multiple of {n_kv}")
+    words = _masks(mask, (batch.tokens,), "mask")
+    _ints(tail, (batch.seqs,), "tail")
+    if out is None:
+        out = _fresh((batch.tokens, width), torch.float16, q.device, stream)
+    if _dev(out, torch.float16, "out").shape != q.shape:
+        raise ValueError("fq_attn_tree: out must have the shape of q")
+    if lse is not None and tuple(_dev(lse, torch.float32, "lse").shape) != (batch.tokens, heads):
+        raise ValueError(f"fq_attn_tree: lse [{batch.tokens}, {heads}]")
+    if workspace is None:
+        nbytes = fq_attn_tree_workspace_bytes(batch, heads, n_kv)
+        workspace = _fresh((nbytes,), torch.uint8, q.device, stream) if nbytes else None
+    elif not workspace.is_contiguous():
+        raise TypeError("fq_attn_tree: the workspace must be contiguous")
+    _same_device("fq_attn_tree", batch.device, q, mask, k_pages, v_pages, tail, out, lse, workspace)
+    _on_current("fq_attn_tree", batch.device)
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.fq_attn_tree(batch.struct, _dp(mask), words, _dp(tail), _dp(q), ldq, heads, n_kv, _dp(k_pages), _dp(v_pages), scale, _dp(out), _dp(lse),
+                             _dp(workspace), nbytes, _stream(stream)))
+    return out
+
+
+def fq_tree_commit(batch: PagedBatch, k_pages, v_pages, parents=None, drafted=None, following=None, tail=None, path=None, accepted=None, bonus=None,
+                   new_len=None, stream=None):
+    """Keeps a path through the tree at the end of every sequence: its rows move together in the pools, fp16 [layers, pages, kv heads, page, 128] (or
+    without layers).  With parents, drafted and following, int32 [tokens] each, the path is found first: from the first token on to the token that goes on from
+    it and is drafted as the one that the model has following it.  Without, path int32 [sequences, n] and accepted [sequences] say which nodes of the tail
+    stay.  Returns (path, accepted, bonus, new_len): nodes on the path, -1 behind them; how many; what follows the last one (None where the path was
+    given); positions that the sequence has now."""
+    if _bind is not None and path is not None and accepted is not None and new_len is not None:
+        rc = _bind.tree_commit(batch, k_pages, v_pages, parents, drafted, following, tail, path, accepted, bonus, new_len, stream)
+        if rc is not None:
+            _check(rc)
+            return path, accepted, bonus, new_len
+    k_pages, v_pages = _dev(k_pages, torch.float16, "k_pages"), _dev(v_pages, torch.float16, "v_pages")
+    if k_pages.dim() not in (4, 5) or tuple(k_pages.shape[-2:]) != (batch.page, 128) or k_pages.shape[-4] != batch.pages or v_pages.shape != k_pages.shape:
+        raise ValueError(f"fq_tree_commit: pools [layers, {batch.pages}, n_kv_heads, {batch.page}, 128]")
+    walk = parents is not None
+    if (drafted is not None) != walk or (following is not None) != walk:
+        raise ValueError("fq_tree_commit: parents, drafted and following go together")
+    for t, what in ((parents, "parents"), (drafted, "drafted"), (following, "following")):
+        _ints(t, (batch.tokens,), what)
+    _ints(tail, (batch.seqs,), "tail")
+    if not walk and (path is None or accepted is None):
+        raise ValueError("fq_tree_commit: without a tree to check, path and accepted say what stays")
+    if path is None:
+        path = _fresh((batch.seqs, max(batch.max_q, 1)), torch.int32, k_pages.device, stream)
+    if _dev(path, torch.int32, "path").dim() != 2 or path.shape[0] != batch.seqs or path.shape[1] < 1:
+        raise ValueError(f"fq_tree_commit: path [{batch.seqs}, nodes]")
+    accepted = _fresh((batch.seqs,), torch.int32, k_pages.device, stream) if accepted is None else accepted
+    new_len = _fresh((batch.seqs,), torch.int32, k_pages.device, stream) if new_len is None else new_len
+    if walk and bonus is None:
+        bonus = _fresh((batch.seqs,), torch.int32, k_pages.device, stream)
+    for t, what in ((accepted, "accepted"), (bonus, "bonus"), (new_len, "new_len")):
+        _ints(t, (batch.seqs,), what)
+    _same_device("fq_tree_commit", batch.device, k_pages, v_pages, parents, drafted, following, tail, path, accepted, bonus, new_len)
+    _on_current("fq_tree_commit", batch.device)
+    _check(_lib.fq_tree_commit(batch.struct, _dp(tail), _dp(parents), _dp(drafted), _dp(following), _dp(k_pages), _dp(v_pages),
+                               k_pages.shape[0] if k_pages.dim() == 5 else 1, k_pages.shape[-3], _dp(path), path.shape[1], _dp(accepted), _dp(bonus),
+                               _dp(new_len), _stream(stream)))
+    return path, accepted, bonus, new_len
+
+
+def fq_beam_step_workspace_bytes(requests: int, beams: int, vocab: int, width: int) -> int:
+    return _lib.fq_beam_step_workspace_bytes(requests, beams, vocab, width)
+
+
+def fq_beam_step(logits, scores, width: int, done=None, eos: int = -1, mask=None, tail=None, parent=None, token=None, scores_out=None, done_out=None,
+                 mask_out=None, workspace=None, stream=None):
+    """The `width` best continuations of every request's beams: logits fp16 [requests * beams, vocabulary], scores fp32 [requests, beams] (-inf: no
+    such beam).  done int32 [requests, beams]: beams that go on as they are, with token eos.  mask int64 [requests, beams, words] and tail int32 [requests]:
+    the beams as nodes of a tree (``fq_attn_tree``), each one that goes on being node tail + its place.  Returns (parent, token, scores, done, mask), [requests,
+    width] each, best first; done is None without done or eos, mask without mask or mask_out."""
+    if _bind is not None and parent is not None and token is not None and scores_out is not None:
+        rc = _bind.beam_step(logits, scores, width, done, eos, mask, tail, parent, token, scores_out, done_out, mask_out, workspace, stream)
+        if rc is not None:
+            _check(rc)
+            return parent, token, scores_out, done_out, mask_out
+    if _dev(scores, torch.float32, "scores").dim() != 2 or scores.numel() == 0:
+        raise ValueError("fq_beam_step: scores [requests, beams]")
+    requests, beams = scores.shape
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dtype != torch.float16 or logits.dim() != 2:
+        raise TypeError("logits must be a device tensor [requests * beams, vocabulary] of torch.float16")
+    vocab = logits.shape[1]
+    if logits.shape[0] != requests * beams or vocab == 0 or (vocab > 1 and logits.stride(1) != 1):
+        raise ValueError(f"fq_beam_step: logits [{requests * beams}, vocabulary] with contiguous rows, got {tuple(logits.shape)}")
+    ld = logits.stride(0) if logits.shape[0] > 1 else vocab
+    if not 1 <= width <= 64:
+        raise FqError(-2, f"fq_beam_step: width={width} (1 to 64)")
+    _ints(done, (requests, beams), "done")
+    _ints(tail, (requests,), "tail")
+    words = 0
+    if mask is not None:
+        words = _masks(mask, (requests, beams), "mask")
+        if mask_out is None:
+            mask_out = _fresh((requests, width, words), torch.int64, logits.device, stream)
+    if mask_out is not None:
+        if words and _masks(mask_out, (requests, width), "mask_out") != words:
+            raise ValueError(f"fq_beam_step: mask_out has {mask_out.shape[2]} words, mask {words}")
+        words = _masks(mask_out, (requests, width), "mask_out")
+    parent = _fresh((requests, width), torch.int32, logits.device, stream) if parent is None else parent
+    token = _fresh((requests, width), torch.int32, logits.device, stream) if token is None else token
+    scores_out = _fresh((requests, width), torch.float32, logits.device, stream) if scores_out is None else scores_out
+    if done_out is None and (done is not None or eos >= 0):
+        done_out = _fresh((requests, width), torch.int32, logits.device, stream)
+    for t, what in ((parent, "parent"), (token, "token"), (done_out, "done_out")):
+        _ints(t, (requests, width), what)
+    if tuple(_dev(scores_out, torch.float32, "scores_out").shape) != (requests, width):
+        raise ValueError(f"fq_beam_step: scores_out [{requests}, {width}]")
+    if workspace is None:
+        workspace = _fresh((fq_beam_step_workspace_bytes(requests, beams, vocab, width),), torch.uint8, logits.device, stream)
+    elif not workspace.is_contiguous():
+        raise TypeError("fq_beam_step: the workspace must be contiguous")
+    _same_device("fq_beam_step", logits.device, scores, done, mask, tail, parent, token, scores_out, done_out, mask_out, workspace)
+    _on_current("fq_beam_step", logits.device)
+    _check(_lib.fq_beam_step(_dp(logits), ld, _dp(scores), _dp(done), eos, requests, beams, vocab, width, _dp(parent), _dp(token), _dp(scores_out),
+                             _dp(done_out), _dp(mask), _dp(mask_out), words, _dp(tail), _dp(workspace), workspace.numel() * workspace.element_size(),
+                             _stream(stream)))
+    return parent, token, scores_out, done_out, mask_out

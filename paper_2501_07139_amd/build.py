@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libfq.so")
 BIND = os.path.join(PKG, "_bind" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["fq_host.cpp", "fq_api.hip", "fq_gemv.hip", "fq_decode.hip", "fq_skinny.hip", "fq_gemm.hip", "fq_dense.hip", "fq_attn.hip", "fq_rowops.hip",
-           "fq_paged_cache.hip", "fq_paged_attn.hip"]
+           "fq_paged_cache.hip", "fq_paged_attn.hip", "fq_tree.hip", "fq_beam.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

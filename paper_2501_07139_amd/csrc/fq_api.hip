@@ -948,3 +948,182 @@ extern "C" int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, 
                                            dst_pages, k_out, v_out, kept, new_len, weights_out, weights_out_stride,
                                            static_cast<fq_stream>(stream)), "fq_cache_evict launch");
 }
+
+// ------------------------------------------------------------------ trees of tokens
+extern "C" int fq_paged_plan(const fq_paged_batch *batch, const int32_t *new_tokens, const int32_t *cached, const int32_t *next_position,
+                             const int32_t *parents, const int32_t *held, int32_t *held_out, int32_t *free_pages, const int32_t *free_count,
+                             int32_t *free_out, int32_t *lacking, int32_t *positions, int32_t *slots, uint64_t *mask, int mask_words, void *stream)
+{
+    const char *fn = "fq_paged_plan";
+    if (int rc = check_batch(fn, batch, 1))
+        return rc;
+    if (!new_tokens || !cached || !held || !held_out || !free_pages || !free_count || !free_out || !lacking || (batch->tokens > 0 && (!positions || !slots)))
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    if (batch->tokens >= 1 << 29)
+        return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d (below 2^29)", fn, batch->tokens);
+    if (mask && !parents)
+        return fq_fail(FQ_ERR_NULL, "%s: a mask without parents", fn);
+    if (mask ? mask_words <= 0 || mask_words > FQ_TREE_WORDS || batch->max_q > 64 * mask_words : mask_words != 0)
+        return fq_fail(FQ_ERR_SHAPE, "%s: mask_words=%d for trees of up to %d tokens (64 a word, at most %d words; 0 without a mask)", fn, mask_words,
+                       batch->max_q, FQ_TREE_WORDS);
+    if (parents && batch->max_q > 64 * FQ_TREE_WORDS)
+        return fq_fail(FQ_ERR_SHAPE, "%s: trees of up to %d tokens (at most %d)", fn, batch->max_q, 64 * FQ_TREE_WORDS);
+    if (reinterpret_cast<uintptr_t>(mask) & 7)
+        return fq_fail(FQ_ERR_ALIGN, "%s: mask must be 8-byte aligned", fn);
+    // Everything that is written is an array of its own, but for what may be changed in place.
+    const size_t n = batch->seqs, m = batch->tokens;
+    struct Run {
+        const void *at;
+        size_t bytes;
+    };
+    const Run out[] = {{batch->q_start, (n + 1) * 4}, {batch->seq_len, n * 4}, {batch->table, n * batch->table_stride * 4}, {held_out, n * 4},
+                       {free_pages, (size_t)batch->pages * 4}, {free_out, 4}, {lacking, 4}, {positions, m * 4}, {slots, m * 4}, {mask, m * mask_words * 8}};
+    const Run in[] = {{new_tokens, n * 4}, {cached, n * 4}, {next_position, n * 4}, {parents, m * 4}, {held, n * 4}, {free_count, 4}};
+    for (const Run &o : out) {
+        for (const Run &i : in) {
+            const bool in_place = (i.at == cached && o.at == batch->seq_len) || (i.at == held && o.at == held_out) || (i.at == free_count && o.at == free_out);
+            if (i.at && o.at && o.bytes && i.bytes && overlap(o.at, o.bytes, i.at, i.bytes) && !(in_place && i.at == o.at))
+                return fq_fail(FQ_ERR_SHAPE, "%s: an output overlaps an input (cached may be seq_len, held held_out, free_count free_out)", fn);
+        }
+        for (const Run &x : out)
+            if (&x < &o && x.at && o.at && x.bytes && o.bytes && overlap(o.at, o.bytes, x.at, x.bytes))
+                return fq_fail(FQ_ERR_SHAPE, "%s: two outputs overlap", fn);
+    }
+    const fq_plan_arrays a{new_tokens, cached, next_position, parents, held, held_out, free_pages, free_count, free_out, lacking, positions, slots, mask, mask_words};
+    return check_hip(fq_launch_paged_plan(*batch, a, static_cast<fq_stream>(stream)), "fq_paged_plan launch");
+}
+
+extern "C" size_t fq_attn_tree_workspace_bytes(const fq_paged_batch *batch, int n_heads, int n_kv_heads)
+{
+    const char *fn = "fq_attn_tree_workspace_bytes";
+    if (check_batch(fn, batch, n_kv_heads) || check_heads(fn, batch->tokens, n_heads, n_kv_heads))
+        return 0;
+    return align_up(fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, false));
+}
+
+extern "C" int fq_attn_tree(const fq_paged_batch *batch, const uint64_t *mask, int mask_words, const int32_t *tail, const void *q, int ldq, int n_heads,
+                            int n_kv_heads, const void *k_pages, const void *v_pages, float scale, void *out, float *lse, void *workspace,
+                            size_t workspace_bytes, void *stream)
+{
+    const char *fn = "fq_attn_tree";
+    if (int rc = check_batch(fn, batch, n_kv_heads))
+        return rc;
+    if (int rc = check_heads(fn, batch->tokens, n_heads, n_kv_heads))
+        return rc;
+    if (!k_pages || !v_pages || (batch->tokens > 0 && (!q || !out || !mask)))
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    if (mask_words <= 0 || mask_words > FQ_TREE_WORDS)
+        return fq_fail(FQ_ERR_SHAPE, "%s: mask_words=%d (1 to %d)", fn, mask_words, FQ_TREE_WORDS);
+    if (!stride_ok(ldq, n_heads * 128))
+        return fq_fail(FQ_ERR_SHAPE, "%s: ldq=%d (at least the row, a multiple of 8)", fn, ldq);
+    if (!(scale > 0.f) || scale > 1e30f)
+        return fq_fail(FQ_ERR_SHAPE, "%s: scale=%g (must be positive and finite)", fn, scale);
+    const size_t need = fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, false);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fq_fail(FQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(mask) & 7))
+        return fq_fail(FQ_ERR_ALIGN, "%s: pointers must be 16-byte aligned, the mask 8-byte", fn);
+    const size_t row = (size_t)n_heads * 128 * 2;
+    if (batch->tokens > 0 && overlap(q, (size_t)(batch->tokens - 1) * ldq * 2 + row, out, batch->tokens * row))
+        return fq_fail(FQ_ERR_SHAPE, "%s: out overlaps q, which every part of the call reads", fn);
+    if (batch->tokens == 0)
+        return FQ_OK;
+    return check_hip(fq_launch_attn_paged(*batch, q, ldq, n_heads, n_kv_heads, k_pages, v_pages, scale, out, lse, nullptr, nullptr, 0, workspace,
+                                          static_cast<fq_stream>(stream), mask, mask_words, tail), "fq_attn_tree launch");
+}
+
+extern "C" int fq_tree_commit(const fq_paged_batch *batch, const int32_t *tail, const int32_t *parents, const int32_t *drafted, const int32_t *following,
+                              void *k_pages, void *v_pages, int layers, int n_kv_heads, int32_t *path, int path_stride, int32_t *accepted,
+                              int32_t *bonus, int32_t *new_len, void *stream)
+{
+    const char *fn = "fq_tree_commit";
+    if (int rc = check_batch(fn, batch, n_kv_heads))
+        return rc;
+    if (!k_pages || !v_pages || !path || !accepted || !new_len)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    const bool walk = parents || drafted || following;
+    if (walk && (!parents || !drafted || !following))
+        return fq_fail(FQ_ERR_NULL, "%s: parents, drafted and following go together", fn);
+    if (walk ? tail != nullptr : bonus != nullptr)
+        return fq_fail(FQ_ERR_SHAPE, walk ? "%s: the tail of a tree that is checked is the tokens of the call" : "%s: bonus without a tree to check", fn);
+    if (layers <= 0 || layers > 65535 || (long long)layers * n_kv_heads * batch->seqs >= 1 << 25 || path_stride <= 0 || path_stride > 1 << 24)
+        return fq_fail(FQ_ERR_SHAPE, "%s: layers=%d n_kv_heads=%d seqs=%d path_stride=%d (product of the first three below 2^25)", fn, layers, n_kv_heads,
+                       batch->seqs, path_stride);
+    if (!aligned16(k_pages) || !aligned16(v_pages))
+        return fq_fail(FQ_ERR_ALIGN, "%s: pools must be 16-byte aligned", fn);
+    const size_t pool = (size_t)layers * batch->pages * n_kv_heads * batch->page * 256, n = batch->seqs;
+    if (overlap(k_pages, pool, v_pages, pool))
+        return fq_fail(FQ_ERR_SHAPE, "%s: the pools overlap", fn);
+    // what every part of the call reads is not what one of them writes
+    const void *const written[] = {path, accepted, bonus, new_len};
+    const size_t size[] = {n * path_stride * 4, n * 4, n * 4, n * 4};
+    const void *const read[] = {batch->q_start, batch->seq_len, batch->table, tail, parents, drafted, following};
+    const size_t read_size[] = {(n + 1) * 4, n * 4, n * batch->table_stride * 4, n * 4, (size_t)batch->tokens * 4, (size_t)batch->tokens * 4,
+                                (size_t)batch->tokens * 4};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 7; ++j)
+            if (written[i] && read[j] && read_size[j] && overlap(written[i], size[i], read[j], read_size[j]))
+                return fq_fail(FQ_ERR_SHAPE, "%s: an output overlaps an input", fn);
+        for (int j = 0; j < i; ++j)
+            if (written[i] && written[j] && overlap(written[i], size[i], written[j], size[j]))
+                return fq_fail(FQ_ERR_SHAPE, "%s: two of path, accepted, bonus and new_len overlap", fn);
+    }
+    return check_hip(fq_launch_tree_commit(*batch, tail, parents, drafted, following, k_pages, v_pages, layers, n_kv_heads, path, path_stride, accepted,
+                                           bonus, new_len, static_cast<fq_stream>(stream)), "fq_tree_commit launch");
+}
+
+namespace {
+
+int check_beams(const char *fn, int requests, int beams, int vocab, int width)
+{
+    if (requests <= 0 || beams <= 0 || beams > 64 || width <= 0 || width > 64 || vocab <= 0 || vocab > 1 << 18 || (long long)requests * beams >= 1 << 24)
+        return fq_fail(FQ_ERR_SHAPE, "%s: requests=%d beams=%d vocab=%d width=%d (beams and width 1 to 64, vocab up to 2^18, requests * beams below 2^24)",
+                       fn, requests, beams, vocab, width);
+    return FQ_OK;
+}
+
+} // namespace
+
+extern "C" size_t fq_beam_step_workspace_bytes(int requests, int beams, int vocab, int width)
+{
+    if (check_beams("fq_beam_step_workspace_bytes", requests, beams, vocab, width))
+        return 0;
+    return align_up(fq_beam_scratch_bytes(requests, beams, vocab, width));
+}
+
+extern "C" int fq_beam_step(const void *logits, int64_t ld, const float *scores, const int32_t *done, int eos, int requests, int beams, int vocab, int width,
+                            int32_t *parent, int32_t *token, float *scores_out, int32_t *done_out, const uint64_t *mask, uint64_t *mask_out,
+                            int mask_words, const int32_t *tail, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *fn = "fq_beam_step";
+    if (int rc = check_beams(fn, requests, beams, vocab, width))
+        return rc;
+    if (!logits || !scores || !parent || !token || !scores_out)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
+    if (ld < vocab || ld > 1ll << 32)
+        return fq_fail(FQ_ERR_SHAPE, "%s: ld=%lld for rows of %d", fn, (long long)ld, vocab);
+    if (eos >= vocab || (done && eos < 0))
+        return fq_fail(FQ_ERR_SHAPE, "%s: eos=%d of %d tokens%s", fn, eos, vocab, done ? ", which ended beams go on with" : "");
+    if (mask_out ? mask_words <= 0 || mask_words > FQ_TREE_WORDS : mask || mask_words != 0)
+        return fq_fail(FQ_ERR_SHAPE, "%s: mask_words=%d (1 to %d with mask_out, 0 without, and no mask then)", fn, mask_words, FQ_TREE_WORDS);
+    const size_t need = fq_beam_scratch_bytes(requests, beams, vocab, width);
+    if (!workspace || workspace_bytes < need)
+        return fq_fail(FQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(logits) & 1) || ((reinterpret_cast<uintptr_t>(mask) | reinterpret_cast<uintptr_t>(mask_out)) & 7))
+        return fq_fail(FQ_ERR_ALIGN, "%s: the workspace must be 16-byte aligned, masks 8-byte, logits 2-byte", fn);
+    const size_t in = (size_t)requests * beams, n = (size_t)requests * width;
+    const void *const written[] = {parent, token, scores_out, done_out, mask_out, workspace};
+    const size_t size[] = {n * 4, n * 4, n * 4, n * 4, n * mask_words * 8, need};
+    const void *const read[] = {logits, scores, done, mask, tail};
+    const size_t read_size[] = {((in - 1) * ld + vocab) * 2, in * 4, in * 4, in * mask_words * 8, (size_t)requests * 4};
+    for (int i = 0; i < 6; ++i) {
+        for (int j = 0; j < 5; ++j)
+            if (written[i] && read[j] && overlap(written[i], size[i], read[j], read_size[j]))
+                return fq_fail(FQ_ERR_SHAPE, "%s: an output or the workspace overlaps an input", fn);
+        for (int j = 0; j < i; ++j)
+            if (written[i] && written[j] && overlap(written[i], size[i], written[j], size[j]))
+                return fq_fail(FQ_ERR_SHAPE, "%s: two outputs, or one and the workspace, overlap", fn);
+    }
+    const fq_beam_arrays a{scores, done, tail, parent, token, done_out, scores_out, mask, mask_out, eos, mask_words};
+    return check_hip(fq_launch_beam_step(logits, ld, requests, beams, vocab, width, a, workspace, static_cast<fq_stream>(stream)), "fq_beam_step launch");
+}

@@ -32,9 +32,14 @@ struct Entries {
     decltype(&fq_qk_norm_rope) norm_rope;
     decltype(&fq_attn_paged) attn_paged;
     decltype(&fq_cache_evict) evict;
+    decltype(&fq_paged_plan) plan;
+    decltype(&fq_attn_tree) attn_tree;
+    decltype(&fq_tree_commit) commit;
+    decltype(&fq_beam_step) beam;
 } entry;
 
-PyObject *s_packed, *s_scales, *s_zeros, *s_n, *s_k, *s_bits, *s_struct, *s_positions, *s_slots, *s_q_start, *s_seq_len, *s_table;
+PyObject *s_packed, *s_scales, *s_zeros, *s_n, *s_k, *s_bits, *s_struct, *s_positions, *s_slots, *s_q_start, *s_seq_len, *s_table, *s_held, *s_free_pages, *s_free_count,
+    *s_lacking, *s_mask;
 
 // A contiguous device tensor of plain type, else nullptr.
 const at::Tensor *device_tensor(PyObject *o, at::ScalarType type)
@@ -458,22 +463,189 @@ PyObject *cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- trees of tokens
+// The current device: a launch goes there, whatever device the tensors are on.
+bool is_current(c10::Device dev) { return dev.index() == c10::hip::getCurrentHIPStream().device_index(); }
+
+// An int32 device tensor of this shape on dev, or None where it need not be there.
+bool ints_of(PyObject *o, std::initializer_list<int64_t> dims, c10::Device dev, bool needed, const void **v)
+{
+    return optional(o, at::kInt, dev, v) && (o == Py_None ? !needed : shape_is(&THPVariable_Unpack(o), dims));
+}
+
+// batch, new_tokens, cached, next_position, parents, held_out, free_out, stream
+PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 8, [&](int *rc) {
+        fq_paged_batch b;
+        const at::Tensor *fresh = device_tensor(a[1], at::kInt);
+        void *stream;
+        if (!fresh || !is_current(fresh->device()) || !batch_of(a[0], fresh->device(), &b) || !stream_of(a[7], &stream))
+            return false;
+        const c10::Device dev = fresh->device();
+        const void *nw, *cached, *next, *parents, *held, *held_out, *pages, *count, *count_out, *lacking, *positions, *slots;
+        if (!ints_of(a[1], {b.seqs}, dev, true, &nw) || !ints_of(a[2], {b.seqs}, dev, true, &cached) || !ints_of(a[3], {b.seqs}, dev, false, &next) ||
+            !ints_of(a[4], {b.tokens}, dev, false, &parents) || !ints_of(a[5], {b.seqs}, dev, false, &held_out) ||
+            !ints_of(a[6], {1}, dev, false, &count_out) || !token_ints(a[0], s_held, b.seqs, dev, &held) ||
+            !token_ints(a[0], s_free_pages, b.pages, dev, &pages) || !token_ints(a[0], s_free_count, 1, dev, &count) ||
+            !token_ints(a[0], s_lacking, 1, dev, &lacking) || !token_ints(a[0], s_positions, b.tokens, dev, &positions) ||
+            !token_ints(a[0], s_slots, b.tokens, dev, &slots))
+            return false;
+        void *mask = nullptr;
+        int words = 0;
+        if (parents) {
+            const std::unique_ptr<PyObject, void (*)(PyObject *)> m(PyObject_GetAttr(a[0], s_mask), [](PyObject *o) { Py_XDECREF(o); });
+            if (!m)
+                return false;
+            if (m.get() != Py_None) {
+                const at::Tensor *t = device_tensor(m.get(), at::kLong);
+                if (!shape_is(t, {b.tokens, -1}) || t->device() != dev || t->size(1) < 1 || t->size(1) > FQ_TREE_WORDS)
+                    return false;
+                mask = t->data_ptr();
+                words = (int)t->size(1);
+            }
+        }
+        const auto in = [](const void *p) { return static_cast<const int32_t *>(p); };
+        const auto out = [](const void *p) { return static_cast<int32_t *>(const_cast<void *>(p)); };
+        *rc = without_gil([&] {
+            return entry.plan(&b, in(nw), in(cached), in(next), in(parents), in(held), out(held_out ? held_out : held), out(pages), in(count),
+                              out(count_out ? count_out : count), out(lacking), out(positions), out(slots), static_cast<uint64_t *>(mask), words, stream);
+        });
+        return true;
+    });
+}
+
+PyObject *attn_tree(PyObject *, PyObject *const *a, Py_ssize_t n) // q, batch, mask, k_pages, v_pages, tail, scale, out, lse, workspace, stream
+{
+    return guarded(n, 11, [&](int *rc) {
+        fq_paged_batch b;
+        const at::Tensor *out = device_tensor(a[7], at::kHalf), *mask = device_tensor(a[2], at::kLong),
+                         *ws = a[9] == Py_None ? nullptr : device_tensor(a[9], at::kByte);
+        if (!out || out->dim() != 2 || !mask || (!ws && a[9] != Py_None) || !is_current(out->device()) || !batch_of(a[1], out->device(), &b) || b.tokens == 0)
+            return false;
+        const c10::Device dev = out->device();
+        const int64_t tokens = b.tokens, width = out->size(1);
+        const void *pk, *pv, *lse, *tail;
+        void *stream;
+        float scale;
+        int ldq;
+        const int64_t kv = pools_of(a[3], a[4], b.pages, b.page, dev, &pk, &pv);
+        const at::Tensor *q = half_rows(a[0], tokens, width, &ldq);
+        if (kv == 0 || width % 128 != 0 || width > INT_MAX || out->size(0) != tokens || !q || q->device() != dev || (ws && ws->device() != dev) ||
+            mask->device() != dev || !shape_is(mask, {tokens, -1}) || mask->size(1) < 1 || mask->size(1) > FQ_TREE_WORDS || !float_of(a[6], &scale) ||
+            !ints_of(a[5], {b.seqs}, dev, false, &tail) || !optional(a[8], at::kFloat, dev, &lse) || !stream_of(a[10], &stream) ||
+            (lse && !shape_is(&THPVariable_Unpack(a[8]), {tokens, width / 128})))
+            return false;
+        const void *px = q->data_ptr(), *pm = mask->data_ptr();
+        const int words = (int)mask->size(1);
+        void *po = out->data_ptr(), *pw = ws ? ws->data_ptr() : nullptr;
+        const size_t bytes = ws ? (size_t)ws->numel() : 0;
+        *rc = without_gil([&] {
+            return entry.attn_tree(&b, static_cast<const uint64_t *>(pm), words, static_cast<const int32_t *>(tail), px, ldq, (int)(width / 128), (int)kv, pk, pv,
+                                   scale, po, static_cast<float *>(const_cast<void *>(lse)), pw, bytes, stream);
+        });
+        return !(*rc == FQ_ERR_WORKSPACE && !ws); // none given: the long way makes one
+    });
+}
+
+// batch, k_pages, v_pages, parents, drafted, following, tail, path, accepted, bonus, new_len, stream
+PyObject *tree_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 12, [&](int *rc) {
+        fq_paged_batch b;
+        const at::Tensor *k = device_tensor(a[1], at::kHalf), *v = device_tensor(a[2], at::kHalf), *path = device_tensor(a[7], at::kInt);
+        void *stream;
+        if (!k || !v || !path || k->dim() != 5 || v->sizes() != k->sizes() || v->device() != k->device() || path->device() != k->device() ||
+            !is_current(k->device()) || !batch_of(a[0], k->device(), &b) || !stream_of(a[11], &stream))
+            return false;
+        const c10::Device dev = k->device();
+        const void *parents, *drafted, *following, *tail, *accepted, *bonus, *len;
+        if (!shape_is(k, {-1, b.pages, -1, b.page, 128}) || k->size(0) > INT_MAX || k->size(2) > INT_MAX || !shape_is(path, {b.seqs, -1}) ||
+            path->size(1) < 1 || path->size(1) > INT_MAX || !ints_of(a[3], {b.tokens}, dev, false, &parents) ||
+            !ints_of(a[4], {b.tokens}, dev, false, &drafted) || !ints_of(a[5], {b.tokens}, dev, false, &following) ||
+            !ints_of(a[6], {b.seqs}, dev, false, &tail) || !ints_of(a[8], {b.seqs}, dev, true, &accepted) ||
+            !ints_of(a[9], {b.seqs}, dev, a[3] != Py_None, &bonus) || !ints_of(a[10], {b.seqs}, dev, true, &len) ||
+            (parents != nullptr) != (drafted != nullptr) || (parents != nullptr) != (following != nullptr) || b.tokens == 0)
+            return false;
+        const auto in = [](const void *p) { return static_cast<const int32_t *>(p); };
+        const auto out = [](const void *p) { return static_cast<int32_t *>(const_cast<void *>(p)); };
+        void *pk = k->data_ptr(), *pv = v->data_ptr(), *pp = path->data_ptr();
+        *rc = without_gil([&] {
+            return entry.commit(&b, in(tail), in(parents), in(drafted), in(following), pk, pv, (int)k->size(0), (int)k->size(2), out(pp),
+                                (int)path->size(1), out(accepted), out(bonus), out(len), stream);
+        });
+        return true;
+    });
+}
+
+// logits, scores, width, done, eos, mask, tail, parent, token, scores_out, done_out, mask_out, workspace, stream
+PyObject *beam_step(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 14, [&](int *rc) {
+        const at::Tensor *scores = device_tensor(a[1], at::kFloat), *out = device_tensor(a[9], at::kFloat), *ws = device_tensor(a[12], at::kByte);
+        int width, eos;
+        void *stream;
+        if (!scores || scores->dim() != 2 || !out || !ws || !is_current(scores->device()) || !int_of(a[2], &width) || !int_of(a[4], &eos) ||
+            !stream_of(a[13], &stream) || !THPVariable_CheckExact(a[0]))
+            return false;
+        const c10::Device dev = scores->device();
+        const at::Tensor &x = THPVariable_Unpack(a[0]);
+        const int64_t requests = scores->size(0), beams = scores->size(1);
+        if (requests < 1 || beams < 1 || requests > INT_MAX || beams > 64 || !x.is_cuda() || x.device() != dev || x.scalar_type() != at::kHalf || x.dim() != 2 ||
+            x.size(0) != requests * beams || x.size(1) < 2 || x.size(1) > INT_MAX || x.stride(1) != 1 || x.stride(0) < 0 || out->device() != dev ||
+            ws->device() != dev || !shape_is(out, {requests, width}))
+            return false;
+        const int64_t ld = x.size(0) > 1 ? x.stride(0) : x.size(1);
+        const void *done, *tail, *parent, *token, *done_out, *mask, *mask_out;
+        if (!ints_of(a[3], {requests, beams}, dev, false, &done) || !ints_of(a[6], {requests}, dev, false, &tail) ||
+            !ints_of(a[7], {requests, width}, dev, true, &parent) || !ints_of(a[8], {requests, width}, dev, true, &token) ||
+            !ints_of(a[10], {requests, width}, dev, done || eos >= 0, &done_out) || !optional(a[5], at::kLong, dev, &mask) ||
+            !optional(a[11], at::kLong, dev, &mask_out) || (mask && !mask_out))
+            return false;
+        int64_t words = 0;
+        if (mask_out) {
+            const at::Tensor &m = THPVariable_Unpack(a[11]);
+            if (!shape_is(&m, {requests, width, -1}))
+                return false;
+            words = m.size(2);
+            if (words < 1 || words > FQ_TREE_WORDS || (mask && !shape_is(&THPVariable_Unpack(a[5]), {requests, beams, words})))
+                return false;
+        }
+        const auto in = [](const void *p) { return static_cast<const int32_t *>(p); };
+        const auto ints = [](const void *p) { return static_cast<int32_t *>(const_cast<void *>(p)); };
+        const void *px = x.data_ptr();
+        const float *ps = static_cast<const float *>(scores->data_ptr());
+        float *po = static_cast<float *>(out->data_ptr());
+        void *pw = ws->data_ptr();
+        const size_t bytes = (size_t)ws->numel();
+        *rc = without_gil([&] {
+            return entry.beam(px, ld, ps, in(done), eos, (int)requests, (int)beams, (int)x.size(1), width, ints(parent), ints(token), po, ints(done_out),
+                              static_cast<const uint64_t *>(mask), static_cast<uint64_t *>(const_cast<void *>(mask_out)), (int)words, in(tail), pw, bytes,
+                              stream);
+        });
+        return true;
+    });
+}
+
 PyObject *bind(PyObject *, PyObject *args) // addresses of the entry points, in the order of Entries
 {
-    unsigned long long p[9];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8]))
+    unsigned long long p[13];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12]))
         return nullptr;
     entry = Entries{reinterpret_cast<decltype(entry.qlinear)>(p[0]),  reinterpret_cast<decltype(entry.mixed)>(p[1]),
                     reinterpret_cast<decltype(entry.dense)>(p[2]),    reinterpret_cast<decltype(entry.head_nll)>(p[3]),
                     reinterpret_cast<decltype(entry.token_nll)>(p[4]), reinterpret_cast<decltype(entry.logit_l2)>(p[5]),
                     reinterpret_cast<decltype(entry.norm_rope)>(p[6]), reinterpret_cast<decltype(entry.attn_paged)>(p[7]),
-                    reinterpret_cast<decltype(entry.evict)>(p[8])};
+                    reinterpret_cast<decltype(entry.evict)>(p[8]), reinterpret_cast<decltype(entry.plan)>(p[9]),
+                    reinterpret_cast<decltype(entry.attn_tree)>(p[10]), reinterpret_cast<decltype(entry.commit)>(p[11]),
+                    reinterpret_cast<decltype(entry.beam)>(p[12])};
     Py_RETURN_NONE;
 }
 
 #define FQ_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FQ_FAST(qlinear),   FQ_FAST(mixed),    FQ_FAST(dense_f16), FQ_FAST(head_nll),
-                         FQ_FAST(token_nll), FQ_FAST(logit_l2), FQ_FAST(qk_norm_rope), FQ_FAST(attn_paged), FQ_FAST(cache_evict), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FQ_FAST(token_nll), FQ_FAST(logit_l2), FQ_FAST(qk_norm_rope), FQ_FAST(attn_paged), FQ_FAST(cache_evict),
+                         FQ_FAST(paged_plan), FQ_FAST(attn_tree), FQ_FAST(tree_commit), FQ_FAST(beam_step), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
@@ -492,6 +664,11 @@ PyMODINIT_FUNC PyInit__bind()
     s_q_start = PyUnicode_InternFromString("q_start");
     s_seq_len = PyUnicode_InternFromString("seq_len");
     s_table = PyUnicode_InternFromString("table");
+    s_held = PyUnicode_InternFromString("held");
+    s_free_pages = PyUnicode_InternFromString("free_pages");
+    s_free_count = PyUnicode_InternFromString("free_count");
+    s_lacking = PyUnicode_InternFromString("lacking");
+    s_mask = PyUnicode_InternFromString("mask");
     PyObject *m = PyModule_Create(&module);
     if (m && PyModule_AddStringConstant(m, "torch_version", FQ_TORCH_VERSION) != 0) { // tensors are read by this version's layout
         Py_DECREF(m);

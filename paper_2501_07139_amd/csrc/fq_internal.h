@@ -111,7 +111,32 @@ int fq_launch_qk_norm_rope(const void *q, int ldq, const void *k, int ldk, const
 void fq_attn_paged_plan(const fq_paged_batch &b, int heads, int kv_heads, int *rows, int *splits, int *chunk);
 size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights);
 int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int heads, int kv_heads, const void *k, const void *v, float scale,
-                         void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st);
+                         void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st,
+                         const uint64_t *mask = nullptr, int mask_words = 0, const int32_t *tail = nullptr); // mask: of fq_attn_tree, without weights
+// Trees of tokens (fq_tree.hip, fq_beam.hip).
+struct fq_plan_arrays { // of fq_paged_plan, as they are named there
+    const int32_t *new_tokens, *cached, *next_position, *parents, *held;
+    int32_t *held_out, *free_pages;
+    const int32_t *free_count;
+    int32_t *free_out, *lacking, *positions, *slots;
+    uint64_t *mask;
+    int mask_words;
+};
+int fq_launch_paged_plan(const fq_paged_batch &b, const fq_plan_arrays &a, fq_stream st);
+int fq_launch_tree_commit(const fq_paged_batch &b, const int32_t *tail, const int32_t *parents, const int32_t *drafted, const int32_t *following,
+                          void *k_pages, void *v_pages, int layers, int kv_heads, int32_t *path, int path_stride, int32_t *accepted, int32_t *bonus,
+                          int32_t *new_len, fq_stream st);
+struct fq_beam_arrays { // of fq_beam_step, as they are named there
+    const float *scores;
+    const int32_t *done, *tail;
+    int32_t *parent, *token, *done_out;
+    float *scores_out;
+    const uint64_t *mask;
+    uint64_t *mask_out;
+    int eos, mask_words;
+};
+size_t fq_beam_scratch_bytes(int requests, int beams, int vocab, int width);
+int fq_launch_beam_step(const void *logits, long long ld, int requests, int beams, int vocab, int width, const fq_beam_arrays &a, void *workspace, fq_stream st);
 int fq_launch_cache_evict(const fq_paged_batch &batch, const void *k, const void *v, int kv_heads, const float *weights, int weights_stride, int keep,
                           int recent, const int32_t *dst_table, int dst_stride, int dst_pages, void *k_out, void *v_out, int32_t *kept,
                           int32_t *new_len, float *weights_out, int weights_out_stride, fq_stream st);

@@ -13,6 +13,10 @@
 // rounding, and below it at most 2^-40 or 2^-32 of the largest, however many positions one row's reference spans (as they stood, terms below 2^-25 were lost
 // from the product and kept in the sum: a row whose many positions have 2^-23 of the largest each was off by a fifth).
 // V^T comes from row-major values through the transposing LDS read.
+//
+// With TREE the kernels are those of fq_attn_tree: the last `tail` positions of a sequence are nodes of a tree (drafted tokens, or the steps of
+// several beams), and token i sees all positions ahead of them and of the nodes those whose bits its mask has.  Nothing else differs: what
+// is shared by all rows is read once for all of them, and the masks are looked at in the tiles that the tail reaches into only.
 #include "fq_paged.h"
 
 namespace {
@@ -30,7 +34,24 @@ struct PagedAttnArgs {
     float *scores;            // [tokens][heads][scores_stride]: scaled scores of sequences of few rows; [parts][seqs][kv_heads][..]: parts of column sums
     float scale;              // times log2(e): scores are powers of 2
     int scores_stride, parts, part_rows, ldq, heads, kv_heads, group, splits, chunk, tiles, weights_stride, packed;
+    const uint64_t *mask; // TREE: [tokens][mask_words], bit j of word w: node 64 w + j of the tail
+    const int *tail;      // TREE: [seqs], or NULL: the tokens of the call
+    int mask_words;
 };
+
+// Positions ahead of the tail of a sequence.
+__device__ __forceinline__ int ahead_of_tail(const PagedAttnArgs &p, const SeqRange &s, int b)
+{
+    return s.len - min(max(p.tail ? p.tail[b] : s.n, 0), s.len);
+}
+
+// 64 bits of a mask from bit `at` on, which may be negative: ahead of the mask everything is seen, behind its words nothing.
+__device__ __forceinline__ uint64_t mask_window(const uint64_t *row, int words, int at)
+{
+    const int w = at >> 6, shift = at & 63;
+    const uint64_t lo = w < 0 ? ~0ull : w < words ? row[w] : 0, hi = w < -1 ? ~0ull : w + 1 < words ? row[w + 1] : 0;
+    return shift ? lo >> shift | hi << (64 - shift) : lo;
+}
 
 // A tile of rows of one sequence and key/value head.
 struct RowTile {
@@ -39,7 +60,7 @@ struct RowTile {
 };
 
 // Tile `tile` of TR rows, counted over the sequences; rows < 0 where there is none.  Every wavefront scans the sequences' tile counts.
-template <int TR>
+template <int TR, bool TREE>
 __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile)
 {
     const int lane = threadIdx.x & 63;
@@ -64,7 +85,7 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile)
             r.s = seq_range(p.s, r.b);
             r.rows = r.s.n * p.group;
             const int last = min(r.row0 + TR, r.rows) - 1;
-            r.seen = max(min(r.s.len - r.s.n + last / p.group + 1, r.s.len), 0);
+            r.seen = TREE ? r.s.len : max(min(r.s.len - r.s.n + last / p.group + 1, r.s.len), 0);
             return r;
         }
         base += __builtin_amdgcn_readlane(upto, 63);
@@ -149,7 +170,7 @@ __device__ __forceinline__ bool find_split(const PagedAttnArgs &p, int job, int 
     return false;
 }
 
-template <bool SCORES>
+template <bool SCORES, bool TREE = false>
 __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
 {
     // values of a step: 32 rows of 16 chunks of eight, chunk ch of row r at ch ^ 2 (r % 8), so that the transposing read of sixteen rows by
@@ -171,7 +192,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         return;
     const int col = lane & 15, g = lane >> 4;
     const int token = min(col, rows - 1) / p.group, head = kvh * p.group + min(col, rows - 1) - token * p.group;
-    const int seen = len - n + token + 1, all_seen = len - n + 1; // positions this lane's row sees; ... that every row sees; may be negative
+    // positions this lane's row sees; ... that every row sees; may be negative.  TREE: both are the positions ahead of the tail
+    const int base = TREE ? ahead_of_tail(p, SeqRange{first, n, len}, b) : 0;
+    const int seen = TREE ? base : len - n + token + 1, all_seen = TREE ? base : len - n + 1;
+    const uint64_t *const mask = TREE ? p.mask + (size_t)(first + token) * p.mask_words : nullptr;
 
     h8 qb[4];
     {
@@ -220,11 +244,15 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         }
         uint32_t not_finite = 0; // rows of the step, bit 16 i + 4 s + g, with values that not every row sees and that are not finite
         if (t0 + 32 > min(all_seen, end)) { // uniform; rows that nobody sees may hold anything, and 0 * NaN is NaN
+            const uint32_t bits = TREE ? (uint32_t)(mask_window(mask, p.mask_words, t0 - base) >> (4 * g)) : 0;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    st[i][v] = t0 + 16 * i + 4 * g + v < min(seen, end) ? st[i][v] : -INFINITY;
+                    if constexpr (TREE)
+                        st[i][v] = t0 + 16 * i + 4 * g + v < end && (bits >> (16 * i + v) & 1) ? st[i][v] : -INFINITY;
+                    else
+                        st[i][v] = t0 + 16 * i + 4 * g + v < min(seen, end) ? st[i][v] : -INFINITY;
                     if (t0 + 16 * i + 4 * v + g >= end)
                         vv[i][v] = h8{};
                     if (all_seen < end) { // a chunk's own positions: out of the product, and added for the rows that see them (below)
@@ -285,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_few_kernel(PagedAttnArgs p)
         __builtin_amdgcn_wave_barrier();
         for (; not_finite; not_finite &= not_finite - 1) {
             const int t = t0 + __builtin_ctz(not_finite);
-            if (t >= seen)
+            if (TREE ? !(mask_window(mask, p.mask_words, t - base) & 1) : t >= seen)
                 continue;
             const _Float16 *v = p.v + pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, b, t) * PD + 4 * g;
 #pragma unroll
@@ -375,7 +403,7 @@ __device__ __forceinline__ float other_half(float x, float (*f)(float, float))
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 
-template <int KS, bool WHOLE>
+template <int KS, bool WHOLE, bool TREE = false>
 __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p)
 {
     constexpr int TR = tile_rows_of(KS), KB = 2 / KS; // KB: blocks of 32 positions that a wavefront has of a tile
@@ -391,7 +419,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     const int jobs = (int)gridDim.x, half = (jobs + 1) >> 1, bidx = (int)blockIdx.x;
     const int job = bidx < half || jobs * (int)gridDim.y > 512 ? bidx : jobs - 1 - (bidx - half);
     const int kvh = job % p.kv_heads, split = blockIdx.y;
-    const RowTile tile = find_tile<TR>(p, p.tiles - 1 - job / p.kv_heads);
+    const RowTile tile = find_tile<TR, TREE>(p, p.tiles - 1 - job / p.kv_heads);
     if (tile.rows < 0)
         return;
     const int begin = split * p.chunk, end = min(tile.seen, begin + p.chunk);
@@ -402,10 +430,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     const int kpart = wave % KS, qpart = wave / KS;
     const int row0 = tile.row0 + 32 * qpart; // first row of the wavefront
     const int row = row0 + col, rowc = min(row, tile.rows - 1), token = rowc / p.group, head = kvh * p.group + rowc - token * p.group;
-    const int older = tile.s.len - tile.s.n;                       // positions ahead of the tokens; may be negative
-    const int seen = min(older + token + 1, tile.s.len);           // positions this lane's row sees
-    const int all_seen = older + min(row0, tile.rows - 1) / p.group + 1; // ... that every row of the wavefront sees
-    const int any_seen = older + min(row0 + 31, tile.rows - 1) / p.group + 1;
+    const int older = TREE ? ahead_of_tail(p, tile.s, tile.b) : tile.s.len - tile.s.n; // positions ahead of the tokens (may be negative) or of the tail
+    const int seen = min(older + token + 1, tile.s.len);                               // positions this lane's row sees (not with TREE)
+    const int all_seen = TREE ? older : older + min(row0, tile.rows - 1) / p.group + 1; // ... that every row of the wavefront sees
+    const int any_seen = TREE ? tile.s.len : older + min(row0 + 31, tile.rows - 1) / p.group + 1;
+    const uint64_t *const mask = TREE ? p.mask + (size_t)(tile.s.first + token) * p.mask_words : nullptr;
 
     h8 qb[8];
     {
@@ -443,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     auto store_block = [&](h8 *Vdst, int i) { Vdst[256 * i + vdst] = vreg[i]; };
     // A weight of zero takes nothing from a position, but the matrix product has 0 * inf = NaN.  In tiles that reach behind the first row's last
     // position, values that are not finite are therefore zeros in LDS, and rows that see them get them added (below).
-    const int every = older + tile.row0 / p.group + 1; // positions that every row of the tile sees
+    const int every = TREE ? older : older + tile.row0 / p.group + 1; // positions that every row of the tile sees
     auto clear_not_finite = [&](h8 *Vdst, int jt, unsigned short *flags) {
         if (begin + KT * jt + KT <= every)
             return;
@@ -513,12 +542,23 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
                 }
             }
             if (!PLAIN && (first + 32 * KB > all_seen || first + 32 * KB > end)) { // uniform per wavefront
-                const int limit = min(seen, end) - first - 4 * h;
+                if constexpr (TREE) {
+                    uint64_t bits = mask_window(mask, p.mask_words, first - older);
+                    bits &= end - first < 64 ? (1ull << (end - first)) - 1 : ~0ull; // first < end
+                    bits >>= 4 * h;
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
+                    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        st[kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) < limit ? st[kb][v] : -INFINITY;
+                        for (int v = 0; v < 16; ++v)
+                            st[kb][v] = (uint32_t)(bits >> (32 * kb)) >> (8 * (v >> 2) + (v & 3)) & 1 ? st[kb][v] : -INFINITY;
+                } else {
+                    const int limit = min(seen, end) - first - 4 * h;
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            st[kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) < limit ? st[kb][v] : -INFINITY;
+                }
             }
             float top = st[0][0];
 #pragma unroll
@@ -571,7 +611,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
                 for (; bits; bits &= bits - 1) {
                     const int b = __builtin_ctzll(bits);
                     const int r = 16 * ((b & 15) >> 2) + 4 * (b >> 4) + (b & 3), t = begin + KT * jt + r;
-                    if (r / (32 * KB) != kpart || t >= seen)
+                    if (r / (32 * KB) != kpart || (TREE ? t >= end || !(mask_window(mask, p.mask_words, t - older) & 1) : t >= seen))
                         continue;
                     const _Float16 *v = p.v + pool_row(p.s.table, p.s.table_stride, p.s.page_log2, p.s.pages, p.kv_heads, kvh, tile.b, t) * PD + 4 * h;
 #pragma unroll
@@ -666,7 +706,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
 // Joins the splits of a row.  WAVES wavefronts each, which deal the splits among them; a wavefront takes 64 of its own at a time: a lane has one's
 // maximum and sum, then two dimensions of the outputs, eight loads at a time (those are what a row waits for: a token over 100003 positions, 196
 // splits of 32 rows, 9.5 us with four wavefronts, 6.2 with sixteen; 4.6 for up to eight splits, which is the launch and two loads in turn).  Rows of tiles that one split has served are done already.
-template <int WAVES>
+template <int WAVES, bool TREE = false>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_kernel(PagedAttnArgs p, int tile_rows)
 {
     __shared__ float sums[WAVES][PD + 2];
@@ -681,9 +721,9 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_ker
         return;
     const int row = token * p.group + head % p.group;
     const int last = min((row / tile_rows + 1) * tile_rows, s.n * p.group) - 1;
-    if (s.len - s.n + last / p.group + 1 <= p.chunk)
+    if ((TREE ? s.len : s.len - s.n + last / p.group + 1) <= p.chunk)
         return;
-    const int live = (max(s.len - s.n + token + 1, 0) + p.chunk - 1) / p.chunk;
+    const int live = ((TREE ? s.len : max(s.len - s.n + token + 1, 0)) + p.chunk - 1) / p.chunk;
     const size_t stride = (size_t)p.s.tokens * p.heads;
     const f2 *ml = reinterpret_cast<const f2 *>(p.part_ml) + item, *o = reinterpret_cast<const f2 *>(p.part_o) + (size_t)item * (PD / 2) + lane;
     float mx = -INFINITY, l = 0.f, a0 = 0.f, a1 = 0.f;
@@ -1152,7 +1192,8 @@ size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_he
 }
 
 int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int heads, int kv_heads, const void *k, const void *v, float scale,
-                         void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st)
+                         void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st,
+                         const uint64_t *mask, int mask_words, const int32_t *tail)
 {
     const AttnPlan s = plan_attn(b, heads, kv_heads, weights_out != nullptr);
     float *ws = static_cast<float *>(workspace);
@@ -1180,12 +1221,26 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     a.chunk = s.chunk;
     a.tiles = s.tiles;
     a.weights_stride = weights_stride;
+    a.mask = mask;
+    a.mask_words = mask_words;
+    a.tail = tail;
+    const bool tree = mask != nullptr;
     const bool joined = weights_out && s.rows == FEW && s.splits > 1 && s.splits <= 8; // with the column sums
     if (b.tokens > 0) {
         const long long jobs = (long long)s.tiles * kv_heads;
         a.packed = s.rows == FEW && b.seqs > 1 && s.splits > 1 && jobs * s.splits > 768 && jobs * s.splits < 1 << 24; // more than are resident together
         const dim3 grid((unsigned)(jobs * (a.packed ? s.splits : 1)), a.packed ? 1 : s.splits);
-        if (s.rows == FEW && weights_out)
+        if (s.rows == FEW && tree)
+            hipLaunchKernelGGL((attn_paged_few_kernel<false, true>), grid, dim3(256), 0, st, a);
+        else if (s.rows == 64 && b.page >= KT && tree)
+            hipLaunchKernelGGL((attn_paged_tile_kernel<2, true, true>), grid, dim3(256), 0, st, a);
+        else if (s.rows == 64 && tree)
+            hipLaunchKernelGGL((attn_paged_tile_kernel<2, false, true>), grid, dim3(256), 0, st, a);
+        else if (b.page >= KT && tree)
+            hipLaunchKernelGGL((attn_paged_tile_kernel<1, true, true>), grid, dim3(256), 0, st, a);
+        else if (tree)
+            hipLaunchKernelGGL((attn_paged_tile_kernel<1, false, true>), grid, dim3(256), 0, st, a);
+        else if (s.rows == FEW && weights_out)
             hipLaunchKernelGGL(attn_paged_few_kernel<true>, grid, dim3(256), 0, st, a);
         else if (s.rows == FEW)
             hipLaunchKernelGGL(attn_paged_few_kernel<false>, grid, dim3(256), 0, st, a);
@@ -1204,11 +1259,11 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
             const size_t items = (size_t)b.tokens * heads;
             // more than a wavefront takes at once; more than one of its turns (a grid has less than 2^32 threads)
             if (s.splits > 64 && items < 1 << 22)
-                hipLaunchKernelGGL(attn_paged_merge_kernel<16>, dim3((unsigned)items), dim3(1024), 0, st, a, s.rows);
+                hipLaunchKernelGGL((tree ? attn_paged_merge_kernel<16, true> : attn_paged_merge_kernel<16>), dim3((unsigned)items), dim3(1024), 0, st, a, s.rows);
             else if (s.splits > 8 && items < 1 << 24)
-                hipLaunchKernelGGL(attn_paged_merge_kernel<4>, dim3((unsigned)items), dim3(256), 0, st, a, s.rows);
+                hipLaunchKernelGGL((tree ? attn_paged_merge_kernel<4, true> : attn_paged_merge_kernel<4>), dim3((unsigned)items), dim3(256), 0, st, a, s.rows);
             else
-                hipLaunchKernelGGL(attn_paged_merge_kernel<1>, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
+                hipLaunchKernelGGL((tree ? attn_paged_merge_kernel<1, true> : attn_paged_merge_kernel<1>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
             if ((rc = (int)hipGetLastError()) != 0)
                 return rc;
         }

@@ -1,0 +1,360 @@
+// Trees of tokens over the paged cache, what is integers: page tables, slots and masks of a batch from request lengths (fq_paged_plan), and
+// the accepting of a drafted tree with the move of its rows in the cache (fq_tree_commit).
+#include "fq_paged.h"
+
+namespace {
+
+// ------------------------------------------------------------------ plan
+// From lengths to the arrays of a batch.  With f pages on the stack of free ones, r_b pages given back by sequence b and t_b taken:
+//   stack'  = stack ++ pages of closed sequences, in order;    page j that sequence b takes = stack'[f + R - 1 - (t_0 + .. + t_b-1 + j)],
+// so that everything is a prefix sum over the sequences and then work on items (pages, tokens) that find their sequence by the sums.  One
+// workgroup does the sums, and the items too where they are few: such a call is the latency of a launch and of a few loads that wait for
+// each other.  Many tokens are left to a second launch with a workgroup for 1024 of a sequence.
+constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
+constexpr int PLAN_TOKENS = 8192;      // that the first launch does itself
+constexpr int TREE_NODES = 64 * 64;    // of a sequence: FQ_TREE_WORDS words of 64
+constexpr int SUM_CAP = 1 << 29;       // sums stay there: min(a + b, cap) is as good as + for sums of what is not negative
+
+struct PlanArgs {
+    int *q_start, *seq_len, *table;
+    fq_plan_arrays a;
+    int seqs, tokens, max_q, max_len, table_stride, page_log2, pages;
+};
+
+__device__ __forceinline__ int capped(int a, int b) { return min(a + b, SUM_CAP); }
+
+// Inclusive sums over the workgroup; the same scratch may be used again behind a barrier.
+__device__ __forceinline__ int block_sums(int x, int *scratch)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(x, o, 64);
+        x = lane >= o ? capped(x, v) : x;
+    }
+    if (lane == 63)
+        scratch[wave] = x;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < PLAN_WAVES; ++w)
+        before = w < wave ? capped(before, scratch[w]) : before;
+    return capped(x, before);
+}
+
+// The first of `count` entries of rising sums that is above k; k is below the last one.
+__device__ __forceinline__ int find_above(const int *upto, int count, int k)
+{
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (upto[mid] > k)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    return lo;
+}
+
+// Page and place of position t of sequence b, as a slot; -1 where it has no page.
+__device__ __forceinline__ int slot_of(const PlanArgs &p, int b, int t)
+{
+    const int pg = p.table[(size_t)b * p.table_stride + min(t >> p.page_log2, p.table_stride - 1)];
+    return pg < 0 || pg >= p.pages ? -1 : (pg << p.page_log2) | (t & ((1 << p.page_log2) - 1));
+}
+
+// Word `word` of the mask of node i, and its depth: up the parents, which lie ahead of their children, so that the walk ends.
+__device__ __forceinline__ uint64_t ancestors(const int *parents, int i, int word, int *depth)
+{
+    uint64_t bits = 0;
+    int up = 0;
+    for (int at = i;;) {
+        bits |= at >> 6 == word ? 1ull << (at & 63) : 0ull;
+        const int q = parents[at];
+        if (q < 0 || q >= at)
+            break;
+        at = q;
+        ++up;
+    }
+    *depth = up;
+    return bits;
+}
+
+// Rows behind the last sequence's.
+__device__ __forceinline__ void clear_rows(const PlanArgs &p, int from, int first, int step)
+{
+    for (int m = from + first; m < p.tokens; m += step) {
+        p.a.positions[m] = 0;
+        p.a.slots[m] = -1;
+        for (int w = 0; w < p.a.mask_words; ++w)
+            p.a.mask[(size_t)m * p.a.mask_words + w] = 0;
+    }
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanArgs p, int with_tokens)
+{
+    __shared__ int scratch[2][PLAN_WAVES];
+    __shared__ int upto[PLAN_THREADS], item_at[PLAN_THREADS], held_of[PLAN_THREADS], ahead[PLAN_THREADS], next[PLAN_THREADS];
+    __shared__ int parents[PLAN_TOKENS];
+    const int tid = threadIdx.x;
+    const int capacity = min((long long)p.max_len, (long long)p.table_stride << p.page_log2);
+    const int free0 = min(max(p.a.free_count[0], 0), p.pages);
+
+    // what closed sequences give back
+    int back = 0;
+    for (int c0 = 0; c0 < p.seqs; c0 += PLAN_THREADS) {
+        const int b = c0 + tid;
+        const int r = b < p.seqs && p.a.new_tokens[b] < 0 ? min(max(p.a.held[b], 0), p.table_stride) : 0;
+        const int sum = block_sums(r, scratch[0]);
+        upto[tid] = sum;
+        __syncthreads();
+        const int total = upto[PLAN_THREADS - 1];
+        for (int k = tid; k < total; k += PLAN_THREADS) {
+            const int s = find_above(upto, PLAN_THREADS, k), j = k - (s > 0 ? upto[s - 1] : 0);
+            if (free0 + back + k < p.pages)
+                p.a.free_pages[free0 + back + k] = p.table[(size_t)(c0 + s) * p.table_stride + j];
+        }
+        back = capped(back, total);
+        __syncthreads();
+    }
+    const int have = min(free0 + min(back, p.pages), p.pages);
+
+    int tokens = 0, taken = 0;
+    for (int c0 = 0; c0 < p.seqs; c0 += PLAN_THREADS) {
+        const int b = c0 + tid;
+        int n = 0, before = 0, held = 0, position = 0;
+        bool open = false;
+        if (b < p.seqs) {
+            const int want = p.a.new_tokens[b];
+            open = want >= 0;
+            before = min(max(p.a.cached[b], 0), capacity);
+            held = min(max(p.a.held[b], 0), p.table_stride);
+            position = p.a.next_position ? p.a.next_position[b] : before;
+            n = min(min(max(want, 0), p.max_q), capacity - before);
+        }
+        const int end = min(capped(tokens, block_sums(n, scratch[0])), p.tokens);
+        upto[tid] = end;
+        held_of[tid] = held;
+        ahead[tid] = before;
+        next[tid] = position;
+        __syncthreads();
+        const int first = tid > 0 ? upto[tid - 1] : tokens, all_tokens = upto[PLAN_THREADS - 1];
+        n = end - first;
+        const int len = open ? before + n : 0;
+        const int need = open ? max(((len + (1 << p.page_log2) - 1) >> p.page_log2) - held, 0) : 0;
+        const int need_upto = block_sums(need, scratch[1]), mine = capped(taken, need_upto - need);
+        item_at[tid] = need_upto;
+        if (b < p.seqs) {
+            p.q_start[b] = first;
+            p.seq_len[b] = len;
+            p.a.held_out[b] = open ? held + min(max(have - mine, 0), need) : 0;
+        }
+        __syncthreads();
+        const int pages = item_at[PLAN_THREADS - 1];
+        for (int k = tid; k < pages; k += PLAN_THREADS) {
+            const int s = find_above(item_at, PLAN_THREADS, k), j = k - (s > 0 ? item_at[s - 1] : 0), at = have - 1 - capped(taken, k);
+            if (held_of[s] + j < p.table_stride)
+                p.table[(size_t)(c0 + s) * p.table_stride + held_of[s] + j] = at >= 0 ? p.a.free_pages[at] : -1;
+        }
+        if (with_tokens) {
+            const int count = all_tokens - tokens;
+            if (p.a.parents)
+                for (int k = tid; k < count; k += PLAN_THREADS)
+                    parents[k] = p.a.parents[tokens + k];
+            __syncthreads();
+            const int words = p.a.mask_words > 1 ? p.a.mask_words : 1;
+            for (int k = tid; k < count * words; k += PLAN_THREADS) {
+                const int m = words > 1 ? k / words : k, word = k - m * words;
+                const int s = find_above(upto, PLAN_THREADS, tokens + m), first_of = s > 0 ? upto[s - 1] : tokens, i = tokens + m - first_of;
+                int depth = i;
+                if (p.a.parents) {
+                    const uint64_t bits = ancestors(parents + (first_of - tokens), i, word, &depth);
+                    if (p.a.mask_words)
+                        p.a.mask[(size_t)(tokens + m) * p.a.mask_words + word] = bits;
+                }
+                if (word == 0) {
+                    p.a.positions[tokens + m] = next[s] + depth;
+                    p.a.slots[tokens + m] = slot_of(p, c0 + s, ahead[s] + i);
+                }
+            }
+        }
+        tokens = all_tokens;
+        taken = capped(taken, pages);
+        __syncthreads();
+    }
+    if (tid == 0) {
+        p.q_start[p.seqs] = tokens;
+        p.a.free_out[0] = max(have - taken, 0);
+        p.a.lacking[0] = max(taken - have, 0);
+    }
+    if (with_tokens)
+        clear_rows(p, tokens, tid, PLAN_THREADS);
+}
+
+// The tokens of many: a workgroup for 1024 tokens of a sequence, or for all nodes of a tree; the last one for what is behind the tokens.
+__global__ __launch_bounds__(256) void plan_tokens_kernel(PlanArgs p)
+{
+    __shared__ int parents[TREE_NODES];
+    const int b = blockIdx.x, tid = threadIdx.x;
+    if (b == p.seqs) {
+        clear_rows(p, p.q_start[p.seqs], blockIdx.y * 256 + tid, gridDim.y * 256);
+        return;
+    }
+    const int first = p.q_start[b], n = p.q_start[b + 1] - first, older = p.seq_len[b] - n;
+    const int position = p.a.next_position ? p.a.next_position[b] : older;
+    if (!p.a.parents) {
+        for (int i = blockIdx.y * 1024 + tid; i < min(n, (int)blockIdx.y * 1024 + 1024); i += 256) {
+            p.a.positions[first + i] = position + i;
+            p.a.slots[first + i] = slot_of(p, b, older + i);
+        }
+        return;
+    }
+    for (int i = tid; i < n; i += 256)
+        parents[i] = p.a.parents[first + i];
+    __syncthreads();
+    const int words = p.a.mask_words > 1 ? p.a.mask_words : 1;
+    for (int k = tid; k < n * words; k += 256) {
+        const int i = words > 1 ? k / words : k, word = k - i * words;
+        int depth;
+        const uint64_t bits = ancestors(parents, i, word, &depth);
+        if (p.a.mask_words)
+            p.a.mask[(size_t)(first + i) * p.a.mask_words + word] = bits;
+        if (word == 0) {
+            p.a.positions[first + i] = position + depth;
+            p.a.slots[first + i] = slot_of(p, b, older + i);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ commit
+// A wavefront for one sequence, layer, head and one of keys and values: it finds the path itself (all of them do, at the same time: 64 nodes a
+// step, a ballot for the children) and moves the rows, sixteen at a time, loads ahead of stores.  A path rises, so node path[k] is at least k: what a
+// turn reads lies at or behind what it writes first, and no later turn reads what an earlier one wrote.  No other wavefront has its rows.
+struct CommitArgs {
+    PagedSeqs s;
+    const int *tail, *parents, *drafted, *following;
+    _Float16 *k, *v;
+    int *path, *accepted, *bonus, *new_len;
+    int layers, kv_heads, path_stride;
+};
+
+// Row of a position in the pools of one layer, or -1 where its page is none.
+__device__ __forceinline__ long long commit_row(const CommitArgs &p, int b, int kvh, int t)
+{
+    const int pg = p.s.table[(size_t)b * p.s.table_stride + min(t >> p.s.page_log2, p.s.table_stride - 1)];
+    return pg < 0 || pg >= p.s.pages ? -1 : (((long long)pg * p.kv_heads + kvh) << p.s.page_log2) | (t & ((1 << p.s.page_log2) - 1));
+}
+
+__global__ __launch_bounds__(64) void commit_kernel(CommitArgs p)
+{
+    const int b = blockIdx.y, lane = threadIdx.x;
+    const int values = blockIdx.x & 1, at = blockIdx.x >> 1, kvh = at % p.kv_heads, layer = at / p.kv_heads;
+    const SeqRange s = seq_range(p.s, b);
+    const bool walk = p.parents != nullptr, writes = blockIdx.x == 0;
+    const int tail = min(max(p.tail ? p.tail[b] : s.n, 0), s.len), base = s.len - tail;
+    int *const path_out = p.path + (size_t)b * p.path_stride;
+    const int nodes = min(s.n, tail);
+    const int most = walk ? min(nodes, p.path_stride) : min(min(max(p.accepted[b], 0), p.path_stride), tail);
+    _Float16 *const pool = (values ? p.v : p.k) + ((((size_t)layer * p.s.pages * p.kv_heads) << p.s.page_log2)) * PD;
+
+    // the first 64 nodes stay in registers
+    const int node = min(lane, max(nodes, 1) - 1);
+    int parent0 = -2, drafted0 = 0, next0 = 0;
+    if (walk && nodes > 0) {
+        parent0 = p.parents[s.first + node];
+        drafted0 = p.drafted[s.first + node];
+        next0 = p.following[s.first + node];
+    }
+    int cur = 0, next_token = -1;
+    bool more = most > 0;
+    int k0 = 0;
+    while (k0 < most && more) {
+        // up to 64 of the path, lane k has path[k0 + k]
+        int mine = -1, count = 0;
+        if (walk) {
+            while (count < 64 && k0 + count < most && more) {
+                mine = lane == count ? cur : mine;
+                ++count;
+                next_token = cur < 64 ? __builtin_amdgcn_readlane(next0, cur) : p.following[s.first + cur];
+                int child = -1;
+                for (int c0 = cur & ~63; c0 < nodes && child < 0; c0 += 64) {
+                    bool is;
+                    if (c0 == 0)
+                        is = lane < nodes && lane > cur && parent0 == cur && drafted0 == next_token;
+                    else
+                        is = c0 + lane < nodes && c0 + lane > cur && p.parents[s.first + c0 + lane] == cur && p.drafted[s.first + c0 + lane] == next_token;
+                    const unsigned long long found = __builtin_amdgcn_ballot_w64(is);
+                    child = found ? c0 + __builtin_ctzll(found) : -1;
+                }
+                more = child >= 0;
+                cur = more ? child : cur;
+            }
+        } else {
+            count = min(64, most - k0);
+            mine = lane < count ? min(max(path_out[k0 + lane], k0 + lane), tail - 1) : -1;
+        }
+        if (walk && writes && lane < count)
+            path_out[k0 + lane] = mine;
+        // sixteen lanes a row
+        for (int r0 = 0; r0 < count; r0 += 16) {
+            h8 rows[4];
+            long long to[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = r0 + 4 * i + (lane >> 4), from_node = __shfl(mine, k & 63, 64);
+                const bool moved = k < count && from_node != k0 + k;
+                const long long from = moved ? commit_row(p, b, kvh, base + from_node) : -1;
+                to[i] = moved && from >= 0 ? commit_row(p, b, kvh, base + k0 + k) : -1;
+                rows[i] = h8{};
+                if (to[i] >= 0)
+                    rows[i] = *reinterpret_cast<const h8 *>(pool + from * PD + 8 * (lane & 15));
+            }
+            __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0); // every load of the turn is back before its first store
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (to[i] >= 0)
+                    *reinterpret_cast<h8 *>(pool + to[i] * PD + 8 * (lane & 15)) = rows[i];
+        }
+        k0 += count;
+    }
+    if (!writes)
+        return;
+    if (walk) {
+        for (int k = k0 + lane; k < p.path_stride; k += 64)
+            path_out[k] = -1;
+        if (lane == 0) {
+            p.accepted[b] = k0;
+            if (p.bonus)
+                p.bonus[b] = next_token;
+        }
+    }
+    if (lane == 0)
+        p.new_len[b] = base + k0;
+}
+
+} // namespace
+
+int fq_launch_paged_plan(const fq_paged_batch &b, const fq_plan_arrays &a, fq_stream st)
+{
+    const PagedSeqs s = paged_seqs(b);
+    PlanArgs p{const_cast<int *>(b.q_start), const_cast<int *>(b.seq_len), const_cast<int *>(b.table), a, b.seqs, b.tokens, b.max_q, b.max_len,
+               b.table_stride, s.page_log2, b.pages};
+    const int with_tokens = (long long)b.tokens * (a.mask_words > 1 ? a.mask_words : 1) <= PLAN_TOKENS;
+    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p, with_tokens);
+    int rc = (int)hipGetLastError();
+    if (rc != 0 || with_tokens)
+        return rc;
+    hipLaunchKernelGGL(plan_tokens_kernel, dim3(b.seqs + 1, a.parents ? 1 : (b.max_q + 1023) / 1024), dim3(256), 0, st, p);
+    return (int)hipGetLastError();
+}
+
+int fq_launch_tree_commit(const fq_paged_batch &b, const int32_t *tail, const int32_t *parents, const int32_t *drafted, const int32_t *following,
+                          void *k_pages, void *v_pages, int layers, int kv_heads, int32_t *path, int path_stride, int32_t *accepted, int32_t *bonus,
+                          int32_t *new_len, fq_stream st)
+{
+    CommitArgs p{paged_seqs(b), tail, parents, drafted, following, static_cast<_Float16 *>(k_pages), static_cast<_Float16 *>(v_pages), path, accepted,
+                 bonus, new_len, layers, kv_heads, path_stride};
+    hipLaunchKernelGGL(commit_kernel, dim3(2 * layers * kv_heads, b.seqs), dim3(64), 0, st, p);
+    return (int)hipGetLastError();
+}
