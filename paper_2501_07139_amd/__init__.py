@@ -939,7 +939,7 @@ def fq_paged_plan(batch: PagedBatch, new_tokens, cached, next_position=None, par
         _ints(t, shape, what)
     _ints(next_position, (n,), "next_position")
     _ints(parents, (batch.tokens,), "parents")
-    mask = batch.mask if parents is not None else None
+    mask = batch.mask if parents is not None and batch.tokens else None
     words = 0 if mask is None else _masks(mask, (batch.tokens,), "mask")
     _same_device("fq_paged_plan", batch.device, new_tokens, cached, next_position, parents, held_out, free_out, batch.positions, batch.slots, batch.held,
                  batch.free_pages, batch.free_count, batch.lacking, mask)
@@ -1027,6 +1027,8 @@ def fq_tree_commit(batch: PagedBatch, k_pages, v_pages, parents=None, drafted=No
         _ints(t, (batch.seqs,), what)
     _same_device("fq_tree_commit", batch.device, k_pages, v_pages, parents, drafted, following, tail, path, accepted, bonus, new_len)
     _on_current("fq_tree_commit", batch.device)
+    if walk and not batch.tokens:  # nothing of them is read, but that they are there says what is to be done
+        parents = drafted = following = batch.q_start
     _check(_lib.fq_tree_commit(batch.struct, _dp(tail), _dp(parents), _dp(drafted), _dp(following), _dp(k_pages), _dp(v_pages),
                                k_pages.shape[0] if k_pages.dim() == 5 else 1, k_pages.shape[-3], _dp(path), path.shape[1], _dp(accepted), _dp(bonus),
                                _dp(new_len), _stream(stream)))

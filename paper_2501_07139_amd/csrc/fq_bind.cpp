@@ -493,7 +493,7 @@ PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n)
             return false;
         void *mask = nullptr;
         int words = 0;
-        if (parents) {
+        if (parents && b.tokens > 0) {
             const std::unique_ptr<PyObject, void (*)(PyObject *)> m(PyObject_GetAttr(a[0], s_mask), [](PyObject *o) { Py_XDECREF(o); });
             if (!m)
                 return false;

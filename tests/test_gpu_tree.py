@@ -407,6 +407,18 @@ def test_commit_without_pages_and_with_bad_paths_stays_inside(fq, torch):
     assert torch.equal(k[[0, 2, 4]], before[[0, 2, 4]])
 
 
+def test_calls_without_tokens(fq, torch):
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    b = fq.PagedBatch.reserve(2, 0, 0, 64, 16, 9, mask_words=1)
+    fq.fq_paged_plan(b, ints(0, 3), ints(20, 5), parents=none)
+    assert b.q_start.tolist() == [0, 0, 0] and b.seq_len.tolist() == [20, 5] and b.held.tolist() == [2, 1] and b.free_count.item() == 6
+    pool = torch.zeros((1, 9, 2, 16, 128), dtype=torch.float16, device="cuda")
+    assert fq.fq_attn_tree(torch.zeros((0, 256), dtype=torch.float16, device="cuda"), b, b.mask, pool[0], pool[0].clone()).shape == (0, 256)
+    path, accepted, bonus, new_len = fq.fq_tree_commit(b, pool, pool.clone(), none, none, none)
+    assert path.tolist() == [[-1], [-1]] and accepted.tolist() == [0, 0] and bonus.tolist() == [-1, -1] and new_len.tolist() == [20, 5]
+
+
 # ------------------------------------------------------------------ beams
 def beam_check(fq, torch, rng, logits, scores, width, done=None, eos=-1, words=0, tail=None, rows=None):
     requests, beams = scores.shape
