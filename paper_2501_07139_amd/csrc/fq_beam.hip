@@ -6,9 +6,9 @@
 // of them the wrong way round.  That costs little here: a multiply-add of 64 bits issues as fast as one of 32.
 //
 // Two launches.  A workgroup of the first has a part of a row in registers, read once: its maximum, its sum of exponentials, and its `width` best logits
-// in order.  They are found without sorting: every thread has the largest of its own values; the width-th of these is a bound that at least
-// `width` values reach and that at most `width` threads have values above, so few are left, and each of them counts those ahead of it.  A
-// workgroup of the second has a request: lse of its beams from the parts, and the best of the parts' lists by the same count over their heads.
+// in order.  They are found without sorting: the width-th of the threads' largest is a bound that at least `width` values reach, in at most
+// `width` threads, so few are left, and each of them counts those ahead of it.  A workgroup of the second has a request: lse of its beams from the
+// parts, and the best of the parts' lists by the same count over their heads.
 #include "fq_device.h"
 #include "fq_internal.h"
 
@@ -35,36 +35,25 @@ struct BeamArgs {
 // Whether anything goes on from a beam: not from one that isn't there (-inf) or is not a number.
 __device__ __forceinline__ bool alive(float score) { return score > -INFINITY; }
 
-// exp of x <= 0 in 64 bits: 2^k exp(r), |r| <= ln 2 / 2, by the series up to r^11 (the rest is below 1e-14).
-__device__ __forceinline__ double exp_down(double x)
+// exp of x <= 0 in 64 bits: 2^(i / 64) exp(r), |r| <= ln 2 / 128, by the series up to r^4 (the rest is below 4e-14).  `rough` is x to fp32's
+// precision, which is what i is taken from; table: 2^(k / 64), k < 64.  Both at least -700.
+__device__ __forceinline__ double exp_down(double x, float rough, const double *table)
 {
-    x = fmax(x, -700.0); // 1e-304 for what is below; 2^k stays a normal number
-    const double k = __builtin_rint(x * 1.4426950408889634074);
-    const double r = fma(k, -1.9082149292705877e-10, fma(k, -0.69314718036912381649, x)); // ln 2 in two parts, the first of 32 bits: exact
-    double e = 1.0 / 39916800;
-    e = fma(e, r, 1.0 / 3628800);
-    e = fma(e, r, 1.0 / 362880);
-    e = fma(e, r, 1.0 / 40320);
-    e = fma(e, r, 1.0 / 5040);
-    e = fma(e, r, 1.0 / 720);
-    e = fma(e, r, 1.0 / 120);
-    e = fma(e, r, 1.0 / 24);
-    e = fma(e, r, 1.0 / 6);
+    const float i = __builtin_rintf(rough * 92.332482616893656f); // 64 / ln 2
+    const double r = fma((double)i, -0.010830424696249145, x);   // ln 2 / 64, whose error is below 1e-18 and i below 2^17
+    const int n = (int)i;
+    double e = fma(r, 1.0 / 24, 1.0 / 6);
     e = fma(e, r, 0.5);
     e = fma(e, r, 1.0);
     e = fma(e, r, 1.0);
-    return e * __builtin_bit_cast(double, (uint64_t)(1023 + (int)k) << 52);
+    return e * __builtin_ldexp(table[n & 63], n >> 6);
 }
 
-// fp16 as whole numbers in the same order: NaN above all, both zeros alike, 0 for what is no candidate (-inf).
-__device__ __forceinline__ uint32_t order_of(uint32_t bits)
+// fp16 (neither NaN nor -0) as whole numbers in the same order; 0 for what is no candidate (-inf).
+__device__ __forceinline__ uint32_t order_of(_Float16 x)
 {
-    const uint32_t size = bits & 0x7fff;
-    if (size > 0x7c00)
-        return 0xffff;
-    if (bits == 0xfc00)
-        return 0;
-    return bits & 0x8000 ? (size == 0 ? 0x8000 : 0xffff - bits) : bits | 0x8000;
+    const uint32_t bits = __builtin_bit_cast(unsigned short, x);
+    return bits == 0xfc00 ? 0 : bits & 0x8000 ? 0xffff - bits : bits | 0x8000;
 }
 __device__ __forceinline__ float value_of(uint32_t order) // of a candidate
 {
@@ -78,20 +67,23 @@ struct __attribute__((packed, aligned(2))) LooseChunk {
     u4v bits;
 };
 
-// CHUNKS: 16-byte pieces of a row that a thread has.
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// CHUNKS: 16-byte pieces of a row that a thread has.  Chunks are numbered along the row, so a chunk whose largest value is smaller, or as large and
+// the chunk further on, has nothing ahead of the other's: the order of chunks by (largest value, number) bounds that of their values.
 template <int CHUNKS>
 __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
 {
     __shared__ __align__(16) uint32_t tops[BEAM_THREADS];
     __shared__ uint32_t list[BEAM_MOST * CHUNKS * 8];
-    __shared__ uint32_t wave_top[4], bound;
-    __shared__ double wave_sum[4];
+    __shared__ double table[64], wave_sum[4];
     __shared__ int listed;
     const int row = blockIdx.x / p.parts, part = blockIdx.x - row * p.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (!alive(p.a.scores[row]) || (p.a.done && p.a.done[row] != 0))
+    const bool goes_on = alive(p.a.scores[row]) && !(p.a.done && p.a.done[row] != 0); // uniform
+    if (CHUNKS > 1 && !goes_on) // where there are few rows, what is read for nothing costs less than to wait for the score first
         return;
     const _Float16 *const x = p.logits + (size_t)row * p.ld;
-    uint32_t mine[CHUNKS * 8], top = 0;
+    h8 mine[CHUNKS];
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int at = 8 * ((part * CHUNKS + c) * BEAM_THREADS + tid); // of its first value in the row
@@ -109,59 +101,90 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
             }
             bits = u4v{d[0], d[1], d[2], d[3]};
         }
-        const uint32_t d[4] = {bits.x, bits.y, bits.z, bits.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t order = order_of(d[e >> 1] >> (16 * (e & 1)) & 0xffff);
-            mine[8 * c + e] = order ? order << 16 | (0xffff - (8 * (c * BEAM_THREADS + tid) + e)) : 0;
-            top = max(top, mine[8 * c + e]);
-        }
+        mine[c] = __builtin_bit_cast(h8, bits);
     }
+    if (CHUNKS == 1 && !goes_on)
+        return;
+    if (tid < 64)
+        table[tid] = exp2((double)tid / 64);
+    if (tid == 0)
+        listed = 0;
+    uint32_t order[CHUNKS], top = 0;
+    us2 sizes = {0, 0};
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const u4v bits = __builtin_bit_cast(u4v, mine[c]) & 0x7fff7fffu;
+        const uint32_t d[4] = {bits.x, bits.y, bits.z, bits.w};
+        h2 high = {(_Float16)-INFINITY, (_Float16)-INFINITY};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sizes = __builtin_elementwise_max(sizes, __builtin_bit_cast(us2, d[e]));
+            const h2 y = h2{mine[c][2 * e], mine[c][2 * e + 1]} + h2{(_Float16)0.f, (_Float16)0.f}; // -0 is 0
+            mine[c][2 * e] = y[0];
+            mine[c][2 * e + 1] = y[1];
+            high = __builtin_elementwise_max(high, y);
+        }
+        const uint32_t o = order_of(__builtin_elementwise_max(high[0], high[1]));
+        order[c] = o ? o << 16 | (0xffff - (c * BEAM_THREADS + tid)) : 0;
+        top = max(top, order[c]);
+    }
+    if (max(sizes[0], sizes[1]) > 0x7c00) // a NaN
+        top = 0xffffffffu;
     tops[tid] = top;
-    uint32_t all = top;
+    __syncthreads();
+    const u4v four = *reinterpret_cast<const u4v *>(&tops[4 * lane]); // every wavefront has them all
+    uint32_t all = max(max(four.x, four.y), max(four.z, four.w));
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         all = max(all, (uint32_t)__shfl_xor((int)all, o, 64));
-    if (lane == 0)
-        wave_top[wave] = all;
-    if (tid == 0)
-        listed = 0;
-    __syncthreads();
-    all = max(max(wave_top[0], wave_top[1]), max(wave_top[2], wave_top[3]));
     BeamPart *const out = p.parts_out + (size_t)row * p.parts + part;
     if (all == 0 || all >> 16 >= 0xfc00) { // nothing but -inf, or a NaN or +inf (uniform)
         if (tid == 0)
             *out = BeamPart{all == 0 ? 0.0 : (double)NAN, all == 0 ? -INFINITY : 0.f, 0};
         return;
     }
-    const float high = value_of(all >> 16);
+    // The width-th largest, bit by bit: the largest bound that `width` of them reach.  The lower half is 0xfc00 at least where there is an upper one.
+    uint32_t least = 0;
+    const auto reach = [&](uint32_t b) {
+        return (int)(__popcll(__builtin_amdgcn_ballot_w64(four.x >= b)) + __popcll(__builtin_amdgcn_ballot_w64(four.y >= b)) +
+                     __popcll(__builtin_amdgcn_ballot_w64(four.z >= b)) + __popcll(__builtin_amdgcn_ballot_w64(four.w >= b)));
+    };
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit > 0x8000; bit >>= 1)
+        least = reach(least | bit) >= p.width ? least | bit : least;
+    if (least) {
+        least |= 0xfc00;
+#pragma unroll 1
+        for (uint32_t bit = 0x200; bit; bit >>= 1)
+            least = reach(least | bit) >= p.width ? least | bit : least;
+    }
+    least = max(least, 1u);
+    if (top >= least) { // at most `width` threads: all of theirs fit the list
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (order[c] >= least) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t o = order_of(mine[c][e]);
+                    if (o && o >= least >> 16)
+                        list[atomicAdd(&listed, 1)] = o << 16 | (0xffff - (8 * (c * BEAM_THREADS + tid) + e));
+                }
+            }
+    }
+    const float high = value_of(all >> 16), low = high - 700.f;
     double sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < CHUNKS * 8; ++e)
-        sum += mine[e] ? exp_down((double)value_of(mine[e] >> 16) - (double)high) : 0.0;
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float l = fmaxf((float)mine[c][e], low);
+            sum += exp_down((double)l - (double)high, l - high, table);
+        }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         sum += __shfl_xor(sum, o, 64);
     if (lane == 0)
         wave_sum[wave] = sum;
-    // how many threads' largest are ahead of this one's
-    int ahead = 0;
-#pragma unroll 8
-    for (int i = 0; i < BEAM_THREADS; i += 4) {
-        const u4v t = *reinterpret_cast<const u4v *>(&tops[i]);
-        ahead += (t.x > top || (t.x == top && i < tid)) + (t.y > top || (t.y == top && i + 1 < tid)) + (t.z > top || (t.z == top && i + 2 < tid)) +
-                 (t.w > top || (t.w == top && i + 3 < tid));
-    }
-    if (ahead == p.width - 1)
-        bound = max(top, 1u);
-    __syncthreads();
-    const uint32_t least = bound;
-    if (top >= least) {
-#pragma unroll
-        for (int e = 0; e < CHUNKS * 8; ++e)
-            if (mine[e] >= least)
-                list[atomicAdd(&listed, 1)] = mine[e];
-    }
     __syncthreads();
     const int count = listed;
     uint32_t *const to = p.candidates + ((size_t)row * p.parts + part) * p.width;
@@ -187,64 +210,105 @@ __device__ __forceinline__ double value_of(uint64_t order)
     return __builtin_bit_cast(double, order >> 63 ? order & ~(1ull << 63) : ~order);
 }
 
+// Everything that the call has left in memory is asked for at once, as far as registers hold it: the parts, PER entries of lists and a word
+// of masks a thread.  Entries beyond those are read once the lists that matter are known.
+template <int PER>
 __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, int part_values)
 {
-    __shared__ uint64_t heads[BEAM_LISTS], keys[BEAM_MOST * BEAM_MOST];
+    __shared__ uint64_t heads[BEAM_LISTS], keys[BEAM_MOST * BEAM_MOST], masks[BEAM_THREADS];
     __shared__ uint32_t index[BEAM_MOST * BEAM_MOST];
-    __shared__ double offset[BEAM_MOST]; // score - lse
+    __shared__ double offset[BEAM_MOST], table[64]; // score - lse
+    __shared__ float scores[BEAM_MOST];
     __shared__ int parent[BEAM_MOST], ended[BEAM_MOST], chosen[BEAM_MOST];
+    __shared__ unsigned char counts[BEAM_LISTS];
     __shared__ uint64_t bound;
     __shared__ int listed, found;
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row0 = r * p.beams, lists = p.beams * p.parts;
-    for (int b = wave; b < p.beams; b += BEAM_THREADS / 64) {
-        const float score = p.a.scores[row0 + b];
-        const bool over = p.a.done && p.a.done[row0 + b] != 0;
-        double at = NAN;
-        if (over) {
-            at = score;
-        } else if (alive(score)) {
-            const BeamPart *const parts = p.parts_out + (size_t)(row0 + b) * p.parts;
-            float high = -INFINITY;
-            for (int i = lane; i < p.parts; i += 64)
-                high = fmaxf(high, parts[i].max);
+    double *const sums = reinterpret_cast<double *>(heads);  // of the parts, until the heads are known
+    float *const highs = reinterpret_cast<float *>(index);
+    const int r = blockIdx.x, tid = threadIdx.x;
+    const int row0 = r * p.beams, lists = p.beams * p.parts, entries = lists * p.width, mask_entries = p.beams * p.a.mask_words;
+    const BeamPart *const parts = p.parts_out + (size_t)row0 * p.parts;
+    const uint32_t *const candidates = p.candidates + (size_t)row0 * p.parts * p.width;
+    uint32_t held[PER];
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1)
-                high = fmaxf(high, __shfl_xor(high, o, 64));
-            double sum = 0.0;
-            for (int i = lane; i < p.parts; i += 64)
-                sum += parts[i].max == -INFINITY ? 0.0 : parts[i].sum * exp_down((double)parts[i].max - (double)high);
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1)
-                sum += __shfl_xor(sum, o, 64);
-            at = sum > 0.0 ? (double)score - ((double)high + log(sum)) : (double)NAN;
-        }
-        if (lane == 0) {
-            offset[b] = at;
-            ended[b] = over;
-        }
+    for (int k = 0; k < PER; ++k)
+        held[k] = candidates[min(tid + BEAM_THREADS * k, entries - 1)];
+    const bool masks_here = p.a.mask && mask_entries <= BEAM_THREADS;
+    if (masks_here && tid < mask_entries)
+        masks[tid] = p.a.mask[(size_t)row0 * p.a.mask_words + tid];
+    const int tail = p.a.mask_out && p.a.tail ? p.a.tail[r] : 0;
+    for (int i = tid; i < lists; i += BEAM_THREADS) { // of beams that nobody has looked at, anything
+        const BeamPart part = parts[i];
+        sums[i] = part.sum;
+        highs[i] = part.max;
+        counts[i] = (unsigned char)part.count;
     }
+    if (tid < p.beams) {
+        scores[tid] = p.a.scores[row0 + tid];
+        ended[tid] = p.a.done && p.a.done[row0 + tid] != 0;
+    }
+    if (tid < 64)
+        table[tid] = exp2((double)tid / 64);
     if (tid == 0) {
         bound = 1;
         listed = found = 0;
     }
     __syncthreads();
-    // the order of entry j of a list, 0 where it has none that counts
-    const auto entry = [&](int b, int part, int j, int *token) -> uint64_t {
-        const double at = offset[b];
-        if (ended[b]) {
-            *token = p.a.eos;
-            return part == 0 && j == 0 && at > -INFINITY ? order_of(at) : 0;
+    for (int i = tid; i < lists; i += BEAM_THREADS) { // every part's sum as of the beam's maximum
+        const int first = i / p.parts * p.parts;
+        float high = -INFINITY;
+        for (int j = 0; j < p.parts; ++j)
+            high = fmaxf(high, highs[first + j]);
+        const float l = fmaxf(highs[i], high - 700.f);
+        sums[i] = highs[i] == -INFINITY ? 0.0 : sums[i] * exp_down((double)l - (double)high, l - high, table);
+    }
+    __syncthreads();
+    if (tid < p.beams) {
+        double at = NAN;
+        if (ended[tid]) {
+            at = scores[tid];
+        } else if (alive(scores[tid])) {
+            double sum = 0.0;
+            float high = -INFINITY;
+            for (int j = 0; j < p.parts; ++j) {
+                sum += sums[tid * p.parts + j];
+                high = fmaxf(high, highs[tid * p.parts + j]);
+            }
+            at = sum > 0.0 ? (double)scores[tid] - ((double)high + log(sum)) : (double)NAN;
         }
-        if (!(at > -INFINITY) || j >= p.parts_out[(size_t)(row0 + b) * p.parts + part].count)
-            return 0;
-        const uint32_t c = p.candidates[((size_t)(row0 + b) * p.parts + part) * p.width + j];
-        *token = part * part_values + (int)(0xffff - (c & 0xffff));
-        return order_of(at + (double)value_of(c >> 16));
+        offset[tid] = at;
+    }
+    __syncthreads();
+    // The order of entry j of list l, 0 where it has none that counts, and its index; c: what the list has there.
+    const auto entry = [&](int l, int j, uint32_t c, uint32_t *at) -> uint64_t {
+        const int b = l / p.parts, part = l - b * p.parts;
+        const double off = offset[b];
+        if (ended[b]) {
+            *at = (uint32_t)b * p.vocab + p.a.eos;
+            return part == 0 && j == 0 && off > -INFINITY ? order_of(off) : 0;
+        }
+        *at = (uint32_t)b * p.vocab + part * part_values + (0xffff - (c & 0xffff));
+        return off > -INFINITY && j < counts[l] ? order_of(off + (double)value_of(c >> 16)) : 0;
     };
-    int token;
-    for (int i = tid; i < lists; i += BEAM_THREADS)
-        heads[i] = entry(i / p.parts, i % p.parts, 0, &token);
+    const bool all_held = entries <= PER * BEAM_THREADS;
+    uint64_t held_key[PER];
+    uint32_t held_at[PER];
+    if (all_held) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int i = tid + BEAM_THREADS * k, l = i / p.width, j = i - l * p.width;
+            held_key[k] = 0;
+            if (i < entries) {
+                held_key[k] = entry(l, j, held[k], &held_at[k]);
+                if (j == 0)
+                    heads[l] = held_key[k];
+            }
+        }
+    } else {
+        uint32_t at;
+        for (int l = tid; l < lists; l += BEAM_THREADS)
+            heads[l] = entry(l, 0, candidates[(size_t)l * p.width], &at);
+    }
     __syncthreads();
     // Lists whose heads are among the `width` first: no other list has any of the best, and of these what the last of the heads is not ahead of.
     for (int i = tid; i < lists; i += BEAM_THREADS) {
@@ -252,22 +316,34 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
         if (head == 0)
             continue;
         int ahead = 0;
+#pragma unroll 4
         for (int j = 0; j < lists; ++j)
             ahead += heads[j] > head || (heads[j] == head && j < i);
-        if (ahead < p.width)
+        if (ahead < p.width) {
             chosen[ahead] = i;
+            atomicMax(&found, ahead + 1);
+        }
         if (ahead == p.width - 1)
             bound = head;
-        atomicMax(&found, min(ahead + 1, p.width));
     }
     __syncthreads();
-    for (int i = tid; i < found * p.width; i += BEAM_THREADS) { // at most 64 lists of 64 entries
-        const int l = chosen[i / p.width], b = l / p.parts;
-        const uint64_t key = entry(b, l - b * p.parts, i % p.width, &token);
+    const auto take = [&](uint64_t key, uint32_t at) {
         if (key >= bound) {
             const int to = atomicAdd(&listed, 1);
             keys[to] = key;
-            index[to] = (uint32_t)b * p.vocab + token;
+            index[to] = at;
+        }
+    };
+    if (all_held) { // at most PER * 256 of them
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            take(held_key[k], held_at[k]);
+    } else { // at most 64 lists of 64 entries
+        for (int i = tid; i < found * p.width; i += BEAM_THREADS) {
+            const int n = i / p.width, l = chosen[n], j = i - n * p.width;
+            uint32_t at;
+            const uint64_t key = entry(l, j, candidates[(size_t)l * p.width + j], &at);
+            take(key, at);
         }
     }
     __syncthreads();
@@ -277,6 +353,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
         int at = i; // places behind those that are found are empty
         if (i < count) {
             at = 0;
+#pragma unroll 4
             for (int j = 0; j < count; ++j)
                 at += keys[j] > keys[i] || (keys[j] == keys[i] && index[j] < index[i]);
         }
@@ -293,13 +370,17 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
     if (!p.a.mask_out)
         return;
     __syncthreads();
-    const int tail = p.a.tail ? p.a.tail[r] : 0;
     for (int i = tid; i < p.width * p.a.mask_words; i += BEAM_THREADS) {
         const int j = i / p.a.mask_words, w = i - j * p.a.mask_words, b = parent[j];
         const long long own = (long long)tail + j;
         uint64_t bits = 0;
-        if (b >= 0)
-            bits = (p.a.mask ? p.a.mask[((size_t)row0 + b) * p.a.mask_words + w] : 0) | (own >= 0 && own >> 6 == w ? 1ull << (own & 63) : 0ull);
+        if (b >= 0) {
+            bits = own >= 0 && own >> 6 == w ? 1ull << (own & 63) : 0ull;
+            if (masks_here)
+                bits |= masks[b * p.a.mask_words + w];
+            else if (p.a.mask)
+                bits |= p.a.mask[((size_t)row0 + b) * p.a.mask_words + w];
+        }
         p.a.mask_out[out * p.a.mask_words + i] = bits;
     }
 }
@@ -339,6 +420,6 @@ int fq_launch_beam_step(const void *logits, long long ld, int requests, int beam
     const int rc = (int)hipGetLastError();
     if (rc != 0)
         return rc;
-    hipLaunchKernelGGL(beam_merge_kernel, dim3(requests), dim3(BEAM_THREADS), 0, st, p, 8 * BEAM_THREADS * s.chunks);
+    hipLaunchKernelGGL(beam_merge_kernel<4>, dim3(requests), dim3(BEAM_THREADS), 0, st, p, 8 * BEAM_THREADS * s.chunks);
     return (int)hipGetLastError();
 }
