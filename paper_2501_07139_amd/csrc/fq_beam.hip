@@ -17,9 +17,11 @@ namespace {
 constexpr int BEAM_THREADS = 256, BEAM_MOST = 64; // most beams, and most of them that go on
 constexpr int BEAM_LISTS = BEAM_MOST * 32;        // of a request: parts of 8192 values of up to 2^18
 
+constexpr int BEAM_NONE = -(1 << 20); // below the power of two of any logit
+
 struct BeamPart {
-    double sum; // of exp(logit - max); NaN where a logit is NaN or +inf
-    float max;  // -inf where there is none above
+    double sum; // of exp(logit) 2^-scale; NaN where a logit is NaN or +inf
+    int scale;  // BEAM_NONE where there is none above -inf
     int count;  // of its list
 };
 
@@ -35,18 +37,22 @@ struct BeamArgs {
 // Whether anything goes on from a beam: not from one that isn't there (-inf) or is not a number.
 __device__ __forceinline__ bool alive(float score) { return score > -INFINITY; }
 
-// exp of x <= 0 in 64 bits: 2^(i / 64) exp(r), |r| <= ln 2 / 128, by the series up to r^4 (the rest is below 4e-14).  `rough` is x to fp32's
-// precision, which is what i is taken from; table: 2^(k / 64), k < 64.  Both at least -700.
-__device__ __forceinline__ double exp_down(double x, float rough, const double *table)
+// exp(x) 2^-scale in 64 bits, 2^(i / 256) exp(r) with |r| <= ln 2 / 512, by the series up to r^3 (the rest is below 2e-13 of it); table: 2^(k / 256).  i comes
+// from the sum with 1.5 * 2^52, whose lowest bits it is then.  |x| < 2^17, and x / ln 2 - scale at least -1020.
+constexpr int EXP_TABLE = 256;
+
+__device__ __forceinline__ double exp_scaled(double x, int scale, const double *table)
 {
-    const float i = __builtin_rintf(rough * 92.332482616893656f); // 64 / ln 2
-    const double r = fma((double)i, -0.010830424696249145, x);   // ln 2 / 64, whose error is below 1e-18 and i below 2^17
-    const int n = (int)i;
-    double e = fma(r, 1.0 / 24, 1.0 / 6);
-    e = fma(e, r, 0.5);
+    constexpr double SHIFT = 6755399441055744.0;
+    const double shifted = fma(x, 369.32993046757464, SHIFT);           // 256 / ln 2
+    const double r = fma(shifted - SHIFT, -0.0027076061740622863, x);   // ln 2 / 256, whose error is below 3e-19, times i
+    const int i = (int)(uint32_t)__builtin_bit_cast(uint64_t, shifted); // mod 2^32
+    double e = fma(r, 1.0 / 6, 0.5);
     e = fma(e, r, 1.0);
     e = fma(e, r, 1.0);
-    return e * __builtin_ldexp(table[n & 63], n >> 6);
+    const uint64_t t = __builtin_bit_cast(uint64_t, table[i & (EXP_TABLE - 1)]);
+    const uint32_t high = (uint32_t)(t >> 32) + (((uint32_t)(i >> 8) - (uint32_t)scale) << 20);
+    return e * __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)t);
 }
 
 // fp16 (neither NaN nor -0) as whole numbers in the same order; 0 for what is no candidate (-inf).
@@ -76,7 +82,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
 {
     __shared__ __align__(16) uint32_t tops[BEAM_THREADS];
     __shared__ uint32_t list[BEAM_MOST * CHUNKS * 8];
-    __shared__ double table[64], wave_sum[4];
+    __shared__ double table[EXP_TABLE], wave_sum[4];
+    __shared__ uint32_t bound;
     __shared__ int listed;
     const int row = blockIdx.x / p.parts, part = blockIdx.x - row * p.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool goes_on = alive(p.a.scores[row]) && !(p.a.done && p.a.done[row] != 0); // uniform
@@ -105,8 +112,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
     }
     if (CHUNKS == 1 && !goes_on)
         return;
-    if (tid < 64)
-        table[tid] = exp2((double)tid / 64);
+    table[tid] = exp2((double)tid / EXP_TABLE);
     if (tid == 0)
         listed = 0;
     uint32_t order[CHUNKS], top = 0;
@@ -140,26 +146,45 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
     BeamPart *const out = p.parts_out + (size_t)row * p.parts + part;
     if (all == 0 || all >> 16 >= 0xfc00) { // nothing but -inf, or a NaN or +inf (uniform)
         if (tid == 0)
-            *out = BeamPart{all == 0 ? 0.0 : (double)NAN, all == 0 ? -INFINITY : 0.f, 0};
+            *out = BeamPart{all == 0 ? 0.0 : (double)NAN, all == 0 ? BEAM_NONE : 0, 0};
         return;
     }
-    // The width-th largest, bit by bit: the largest bound that `width` of them reach.  The lower half is 0xfc00 at least where there is an upper one.
-    uint32_t least = 0;
-    const auto reach = [&](uint32_t b) {
-        return (int)(__popcll(__builtin_amdgcn_ballot_w64(four.x >= b)) + __popcll(__builtin_amdgcn_ballot_w64(four.y >= b)) +
-                     __popcll(__builtin_amdgcn_ballot_w64(four.z >= b)) + __popcll(__builtin_amdgcn_ballot_w64(four.w >= b)));
-    };
+    if (wave == 0) {
+        // The width-th largest, bit by bit: the largest bound that `width` of them reach.  Their lower half is 0xfc00 at least; it matters only where
+        // ties would be more than the list holds.
+        uint32_t least = 0;
+        const auto reach = [&](uint32_t b) {
+            return (int)(__popcll(__builtin_amdgcn_ballot_w64(four.x >= b)) + __popcll(__builtin_amdgcn_ballot_w64(four.y >= b)) +
+                         __popcll(__builtin_amdgcn_ballot_w64(four.z >= b)) + __popcll(__builtin_amdgcn_ballot_w64(four.w >= b)));
+        };
 #pragma unroll 1
-    for (uint32_t bit = 1u << 31; bit > 0x8000; bit >>= 1)
-        least = reach(least | bit) >= p.width ? least | bit : least;
-    if (least) {
-        least |= 0xfc00;
-#pragma unroll 1
-        for (uint32_t bit = 0x200; bit; bit >>= 1)
+        for (uint32_t bit = 1u << 31; bit > 0x8000; bit >>= 1)
             least = reach(least | bit) >= p.width ? least | bit : least;
+        if (least && reach(least) > BEAM_MOST) {
+            least |= 0xfc00;
+#pragma unroll 1
+            for (uint32_t bit = 0x200; bit; bit >>= 1)
+                least = reach(least | bit) >= p.width ? least | bit : least;
+        }
+        if (lane == 0)
+            bound = max(least, 1u);
     }
-    least = max(least, 1u);
-    if (top >= least) { // at most `width` threads: all of theirs fit the list
+    const float high = value_of(all >> 16), low = high - 700.f;
+    const int scale = (int)rintf(high * 1.44269504f); // sums as of 2^scale, near exp(high)
+    double sum = 0.0;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sum += exp_scaled((double)fmaxf((float)mine[c][e], low), scale, table);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        sum += __shfl_xor(sum, o, 64);
+    if (lane == 0)
+        wave_sum[wave] = sum;
+    __syncthreads();
+    const uint32_t least = bound;
+    if (top >= least) { // at most 64 threads: all of theirs fit the list
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
             if (order[c] >= least) {
@@ -171,20 +196,6 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
                 }
             }
     }
-    const float high = value_of(all >> 16), low = high - 700.f;
-    double sum = 0.0;
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float l = fmaxf((float)mine[c][e], low);
-            sum += exp_down((double)l - (double)high, l - high, table);
-        }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        sum += __shfl_xor(sum, o, 64);
-    if (lane == 0)
-        wave_sum[wave] = sum;
     __syncthreads();
     const int count = listed;
     uint32_t *const to = p.candidates + ((size_t)row * p.parts + part) * p.width;
@@ -196,7 +207,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
             to[before] = list[i];
     }
     if (tid == 0)
-        *out = BeamPart{wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3], high, min(count, p.width)};
+        *out = BeamPart{wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3], scale, min(count, p.width)};
 }
 
 // 64 bits in the order of their values; 0 is below all numbers.
@@ -210,22 +221,31 @@ __device__ __forceinline__ double value_of(uint64_t order)
     return __builtin_bit_cast(double, order >> 63 ? order & ~(1ull << 63) : ~order);
 }
 
+// i / d for i * d < 2^32, with 2^32 / d rounded up.
+__device__ __forceinline__ int quotient(int i, uint32_t inverse) { return inverse ? (int)__umulhi((uint32_t)i, inverse) : i; }
+
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane)
+{
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane), lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+    return (uint64_t)hi << 32 | lo;
+}
+
 // Everything that the call has left in memory is asked for at once, as far as registers hold it: the parts, PER entries of lists and a word
 // of masks a thread.  Entries beyond those are read once the lists that matter are known.
 template <int PER>
-__global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, int part_values)
+__global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, int part_values, uint32_t per_width, uint32_t per_parts)
 {
     __shared__ uint64_t heads[BEAM_LISTS], keys[BEAM_MOST * BEAM_MOST], masks[BEAM_THREADS];
     __shared__ uint32_t index[BEAM_MOST * BEAM_MOST];
-    __shared__ double offset[BEAM_MOST], table[64]; // score - lse
+    __shared__ double offset[BEAM_MOST]; // score - lse
     __shared__ float scores[BEAM_MOST];
-    __shared__ int parent[BEAM_MOST], ended[BEAM_MOST], chosen[BEAM_MOST];
+    __shared__ int parent[BEAM_MOST], ended[BEAM_MOST], chosen[BEAM_MOST], before[64];
     __shared__ unsigned char counts[BEAM_LISTS];
     __shared__ uint64_t bound;
     __shared__ int listed, found;
     double *const sums = reinterpret_cast<double *>(heads);  // of the parts, until the heads are known
-    float *const highs = reinterpret_cast<float *>(index);
-    const int r = blockIdx.x, tid = threadIdx.x;
+    int *const scales = reinterpret_cast<int *>(index);
+    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row0 = r * p.beams, lists = p.beams * p.parts, entries = lists * p.width, mask_entries = p.beams * p.a.mask_words;
     const BeamPart *const parts = p.parts_out + (size_t)row0 * p.parts;
     const uint32_t *const candidates = p.candidates + (size_t)row0 * p.parts * p.width;
@@ -240,7 +260,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
     for (int i = tid; i < lists; i += BEAM_THREADS) { // of beams that nobody has looked at, anything
         const BeamPart part = parts[i];
         sums[i] = part.sum;
-        highs[i] = part.max;
+        scales[i] = part.scale;
         counts[i] = (unsigned char)part.count;
     }
     if (tid < p.beams) {
@@ -248,19 +268,10 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
         ended[tid] = p.a.done && p.a.done[row0 + tid] != 0;
     }
     if (tid < 64)
-        table[tid] = exp2((double)tid / 64);
+        before[tid] = 0;
     if (tid == 0) {
         bound = 1;
         listed = found = 0;
-    }
-    __syncthreads();
-    for (int i = tid; i < lists; i += BEAM_THREADS) { // every part's sum as of the beam's maximum
-        const int first = i / p.parts * p.parts;
-        float high = -INFINITY;
-        for (int j = 0; j < p.parts; ++j)
-            high = fmaxf(high, highs[first + j]);
-        const float l = fmaxf(highs[i], high - 700.f);
-        sums[i] = highs[i] == -INFINITY ? 0.0 : sums[i] * exp_down((double)l - (double)high, l - high, table);
     }
     __syncthreads();
     if (tid < p.beams) {
@@ -269,19 +280,20 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
             at = scores[tid];
         } else if (alive(scores[tid])) {
             double sum = 0.0;
-            float high = -INFINITY;
-            for (int j = 0; j < p.parts; ++j) {
-                sum += sums[tid * p.parts + j];
-                high = fmaxf(high, highs[tid * p.parts + j]);
-            }
-            at = sum > 0.0 ? (double)scores[tid] - ((double)high + log(sum)) : (double)NAN;
+            int scale = BEAM_NONE;
+            for (int j = 0; j < p.parts; ++j)
+                scale = max(scale, scales[tid * p.parts + j]);
+#pragma unroll 4
+            for (int j = 0; j < p.parts; ++j)
+                sum += ldexp(sums[tid * p.parts + j], scales[tid * p.parts + j] - scale);
+            at = sum > 0.0 ? (double)scores[tid] - ((double)scale * 0.69314718055994530942 + log(sum)) : (double)NAN;
         }
         offset[tid] = at;
     }
     __syncthreads();
     // The order of entry j of list l, 0 where it has none that counts, and its index; c: what the list has there.
     const auto entry = [&](int l, int j, uint32_t c, uint32_t *at) -> uint64_t {
-        const int b = l / p.parts, part = l - b * p.parts;
+        const int b = quotient(l, per_parts), part = l - b * p.parts;
         const double off = offset[b];
         if (ended[b]) {
             *at = (uint32_t)b * p.vocab + p.a.eos;
@@ -296,7 +308,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
     if (all_held) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const int i = tid + BEAM_THREADS * k, l = i / p.width, j = i - l * p.width;
+            const int i = tid + BEAM_THREADS * k, l = quotient(i, per_width), j = i - l * p.width;
             held_key[k] = 0;
             if (i < entries) {
                 held_key[k] = entry(l, j, held[k], &held_at[k]);
@@ -311,20 +323,32 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
     }
     __syncthreads();
     // Lists whose heads are among the `width` first: no other list has any of the best, and of these what the last of the heads is not ahead of.
-    for (int i = tid; i < lists; i += BEAM_THREADS) {
-        const uint64_t head = heads[i];
-        if (head == 0)
-            continue;
-        int ahead = 0;
-#pragma unroll 4
-        for (int j = 0; j < lists; ++j)
-            ahead += heads[j] > head || (heads[j] == head && j < i);
-        if (ahead < p.width) {
+    const auto head_is = [&](uint64_t head, int i, int ahead) {
+        if (ahead < p.width && head != 0) {
             chosen[ahead] = i;
-            atomicMax(&found, ahead + 1);
+            if (!all_held)
+                atomicMax(&found, ahead + 1);
+            if (ahead == p.width - 1)
+                bound = head;
         }
-        if (ahead == p.width - 1)
-            bound = head;
+    };
+    if (lists <= 64) { // a lane has one of them, and each in turn is compared with all
+        const uint64_t head = lane < lists ? heads[lane] : 0;
+        for (int i = wave; i < lists; i += BEAM_THREADS / 64) {
+            const uint64_t mine = lane_of(head, i);
+            const int ahead = __popcll(__builtin_amdgcn_ballot_w64(head > mine)) + __popcll(__builtin_amdgcn_ballot_w64(head == mine && lane < i));
+            if (lane == 0)
+                head_is(mine, i, ahead);
+        }
+    } else {
+        for (int i = tid; i < lists; i += BEAM_THREADS) {
+            const uint64_t head = heads[i];
+            int ahead = 0;
+#pragma unroll 4
+            for (int j = 0; j < lists; ++j)
+                ahead += heads[j] > head || (heads[j] == head && j < i);
+            head_is(head, i, ahead);
+        }
     }
     __syncthreads();
     const auto take = [&](uint64_t key, uint32_t at) {
@@ -340,7 +364,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
             take(held_key[k], held_at[k]);
     } else { // at most 64 lists of 64 entries
         for (int i = tid; i < found * p.width; i += BEAM_THREADS) {
-            const int n = i / p.width, l = chosen[n], j = i - n * p.width;
+            const int n = quotient(i, per_width), l = chosen[n], j = i - n * p.width;
             uint32_t at;
             const uint64_t key = entry(l, j, candidates[(size_t)l * p.width + j], &at);
             take(key, at);
@@ -349,13 +373,28 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
     __syncthreads();
     const int count = listed;
     const size_t out = (size_t)r * p.width;
-    for (int i = tid; i < max(count, p.width); i += BEAM_THREADS) {
+    const int turns = max(count, p.width);
+    if (turns <= 64) { // a lane has one each, and a wavefront compares a quarter of them with all
+        int few = 0;
+        const uint64_t key = lane < count ? keys[lane] : 0;
+        const uint32_t place = lane < count ? index[lane] : 0xffffffffu;
+        for (int j = wave; j < count; j += BEAM_THREADS / 64) {
+            const uint64_t other = lane_of(key, j);
+            few += other > key || (other == key && (uint32_t)__builtin_amdgcn_readlane((int)place, j) < place);
+        }
+        atomicAdd(&before[lane], few);
+        __syncthreads();
+    }
+    for (int i = tid; i < turns; i += BEAM_THREADS) {
         int at = i; // places behind those that are found are empty
         if (i < count) {
             at = 0;
+            if (turns <= 64)
+                at = before[i];
+            else
 #pragma unroll 4
-            for (int j = 0; j < count; ++j)
-                at += keys[j] > keys[i] || (keys[j] == keys[i] && index[j] < index[i]);
+                for (int j = 0; j < count; ++j)
+                    at += keys[j] > keys[i] || (keys[j] == keys[i] && index[j] < index[i]);
         }
         if (at >= p.width)
             continue;
@@ -384,6 +423,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
         p.a.mask_out[out * p.a.mask_words + i] = bits;
     }
 }
+
+uint32_t inverse(int d) { return d > 1 ? (uint32_t)(((1ull << 32) + d - 1) / d) : 0; } // for quotient()
 
 // Small parts where there are few rows: a part is read by one workgroup, and 512 of them fill the chip.
 struct BeamPlan {
@@ -420,6 +461,7 @@ int fq_launch_beam_step(const void *logits, long long ld, int requests, int beam
     const int rc = (int)hipGetLastError();
     if (rc != 0)
         return rc;
-    hipLaunchKernelGGL(beam_merge_kernel<4>, dim3(requests), dim3(BEAM_THREADS), 0, st, p, 8 * BEAM_THREADS * s.chunks);
+    hipLaunchKernelGGL(beam_merge_kernel<4>, dim3(requests), dim3(BEAM_THREADS), 0, st, p, 8 * BEAM_THREADS * s.chunks,
+                       inverse(width), inverse(s.parts));
     return (int)hipGetLastError();
 }
