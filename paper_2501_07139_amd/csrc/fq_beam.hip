@@ -31,28 +31,39 @@ struct BeamArgs {
     fq_beam_arrays a;
     BeamPart *parts_out;  // [rows][parts]
     uint32_t *candidates; // [rows][parts][width]: order of the value, 65535 - place in the part
-    int requests, beams, vocab, width, parts;
+    int requests, beams, vocab, width, parts, part_chunks;
 };
 
 // Whether anything goes on from a beam: not from one that isn't there (-inf) or is not a number.
 __device__ __forceinline__ bool alive(float score) { return score > -INFINITY; }
 
-// exp(x) 2^-scale in 64 bits, 2^(i / 256) exp(r) with |r| <= ln 2 / 512, by the series up to r^3 (the rest is below 2e-13 of it); table: 2^(k / 256).  i comes
-// from the sum with 1.5 * 2^52, whose lowest bits it is then.  |x| < 2^17, and x / ln 2 - scale at least -1020.
+// exp(x) 2^-scale in 64 bits, as 2^(i / 256) exp(r) with |r| <= ln 2 / 512, by the series up to r^3 (the rest is below 2e-13 of it).  i - 256 scale comes from the sum
+// with `shift`, 1.5 * 2^52 - 256 scale, whose lowest bits it is then.  table: entry k has 2^(k / 256), less k << 12 in its upper word, so that adding i << 12 there
+// leaves the power of two alone.  |x| < 2^17, and x / ln 2 - scale at least -1020.
 constexpr int EXP_TABLE = 256;
 
-__device__ __forceinline__ double exp_scaled(double x, int scale, const double *table)
+__device__ __forceinline__ u2v exp_entry(int k)
 {
-    constexpr double SHIFT = 6755399441055744.0;
-    const double shifted = fma(x, 369.32993046757464, SHIFT);           // 256 / ln 2
-    const double r = fma(shifted - SHIFT, -0.0027076061740622863, x);   // ln 2 / 256, whose error is below 3e-19, times i
-    const int i = (int)(uint32_t)__builtin_bit_cast(uint64_t, shifted); // mod 2^32
-    double e = fma(r, 1.0 / 6, 0.5);
+    const u2v e = __builtin_bit_cast(u2v, exp2((double)k / EXP_TABLE));
+    return u2v{e.x, e.y - ((uint32_t)k << 12)};
+}
+struct ExpTerms {
+    double shift, steps, step, sixth; // 1.5 * 2^52 - 256 scale; 256 / ln 2; -ln 2 / 256, whose error is below 3e-19, times i
+    __device__ explicit ExpTerms(int scale) : shift(6755399441055744.0 - 256.0 * scale), steps(369.32993046757464), step(-0.0027076061740622863), sixth(1.0 / 6)
+    {
+        asm("" : "+v"(shift), "+v"(steps), "+v"(step), "+v"(sixth)); // in registers: moved there for every use otherwise
+    }
+};
+__device__ __forceinline__ double add_exp(double sum, double x, const ExpTerms &c, const u2v *table)
+{
+    const double shifted = fma(x, c.steps, c.shift);
+    const double r = fma(shifted - c.shift, c.step, x);
+    const uint32_t i = (uint32_t)__builtin_bit_cast(uint64_t, shifted);
+    double e = fma(r, c.sixth, 0.5);
     e = fma(e, r, 1.0);
     e = fma(e, r, 1.0);
-    const uint64_t t = __builtin_bit_cast(uint64_t, table[i & (EXP_TABLE - 1)]);
-    const uint32_t high = (uint32_t)(t >> 32) + (((uint32_t)(i >> 8) - (uint32_t)scale) << 20);
-    return e * __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)t);
+    const u2v t = table[i & (EXP_TABLE - 1)];
+    return fma(e, __builtin_bit_cast(double, u2v{t.x, t.y + (i << 12)}), sum);
 }
 
 // fp16 (neither NaN nor -0) as whole numbers in the same order; 0 for what is no candidate (-inf).
@@ -78,11 +89,12 @@ typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 // CHUNKS: 16-byte pieces of a row that a thread has.  Chunks are numbered along the row, so a chunk whose largest value is smaller, or as large and
 // the chunk further on, has nothing ahead of the other's: the order of chunks by (largest value, number) bounds that of their values.
 template <int CHUNKS>
-__global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
+__global__ __launch_bounds__(BEAM_THREADS, CHUNKS == 8 ? 6 : 8) void beam_rows_kernel(BeamArgs p)
 {
     __shared__ __align__(16) uint32_t tops[BEAM_THREADS];
     __shared__ uint32_t list[BEAM_MOST * CHUNKS * 8];
-    __shared__ double table[EXP_TABLE], wave_sum[4];
+    __shared__ u2v table[EXP_TABLE];
+    __shared__ double wave_sum[4];
     __shared__ uint32_t bound;
     __shared__ int listed;
     const int row = blockIdx.x / p.parts, part = blockIdx.x - row * p.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -93,9 +105,10 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
     h8 mine[CHUNKS];
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const int at = 8 * ((part * CHUNKS + c) * BEAM_THREADS + tid); // of its first value in the row
+        const int chunk = c * BEAM_THREADS + tid, at = 8 * (part * p.part_chunks + chunk); // its first value's place in the row
         u4v bits = {0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u};
-        if (at + 8 <= p.vocab) {
+        if (chunk >= p.part_chunks) {
+        } else if (at + 8 <= p.vocab) {
             bits = reinterpret_cast<const LooseChunk *>(x + at)->bits;
         } else if (at < p.vocab) { // the end of a row, value by value: nothing is read behind it
             uint32_t d[4];
@@ -112,7 +125,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
     }
     if (CHUNKS == 1 && !goes_on)
         return;
-    table[tid] = exp2((double)tid / EXP_TABLE);
+    table[tid] = exp_entry(tid);
     if (tid == 0)
         listed = 0;
     uint32_t order[CHUNKS], top = 0;
@@ -150,7 +163,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
         return;
     }
     if (wave == 0) {
-        // The width-th largest, bit by bit: the largest bound that `width` of them reach.  Their lower half is 0xfc00 at least; it matters only where
+        // The width-th largest, bit by bit: the largest bound that `width` of them reach.  Their lower half is 0xf800 at least; it matters only where
         // ties would be more than the list holds.
         uint32_t least = 0;
         const auto reach = [&](uint32_t b) {
@@ -161,22 +174,24 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(BeamArgs p)
         for (uint32_t bit = 1u << 31; bit > 0x8000; bit >>= 1)
             least = reach(least | bit) >= p.width ? least | bit : least;
         if (least && reach(least) > BEAM_MOST) {
-            least |= 0xfc00;
+            least |= 0xf800;
 #pragma unroll 1
-            for (uint32_t bit = 0x200; bit; bit >>= 1)
+            for (uint32_t bit = 0x400; bit; bit >>= 1)
                 least = reach(least | bit) >= p.width ? least | bit : least;
         }
         if (lane == 0)
             bound = max(least, 1u);
     }
-    const float high = value_of(all >> 16), low = high - 700.f;
+    const float high = value_of(all >> 16);
     const int scale = (int)rintf(high * 1.44269504f); // sums as of 2^scale, near exp(high)
+    const ExpTerms terms(scale);
+    const float low = high - 700.f; // -inf and what else is below counts as exp(-700) of the largest
     double sum = 0.0;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            sum += exp_scaled((double)fmaxf((float)mine[c][e], low), scale, table);
+            sum = add_exp(sum, (double)fmaxf((float)mine[c][e], low), terms, table);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         sum += __shfl_xor(sum, o, 64);
@@ -224,28 +239,52 @@ __device__ __forceinline__ double value_of(uint64_t order)
 // i / d for i * d < 2^32, with 2^32 / d rounded up.
 __device__ __forceinline__ int quotient(int i, uint32_t inverse) { return inverse ? (int)__umulhi((uint32_t)i, inverse) : i; }
 
-__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane)
+// How many of up to 64 Q keys in LDS are ahead of each, added to ahead[]: a lane has Q of them, a wavefront compares a quarter of all with those.  Of equal
+// ones the lower index[] is ahead, or the lower place without one.
+template <int Q>
+__device__ __forceinline__ void count_ahead(const uint64_t *keys, const uint32_t *index, int count, int *ahead)
 {
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane), lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
-    return (uint64_t)hi << 32 | lo;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint64_t key[Q];
+    uint32_t place[Q];
+    int found[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int i = lane + 64 * q, at = min(i, max(count - 1, 0));
+        key[q] = keys[at];
+        place[q] = index ? index[at] : (uint32_t)i;
+        found[q] = 0;
+    }
+#pragma unroll 2
+    for (int j = wave; j < count; j += BEAM_THREADS / 64) {
+        const uint64_t other = keys[j];
+        const uint32_t other_place = index ? index[j] : (uint32_t)j;
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            found[q] += other > key[q] || (other == key[q] && other_place < place[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+        if (lane + 64 * q < count)
+            atomicAdd(&ahead[lane + 64 * q], found[q]);
 }
 
 // Everything that the call has left in memory is asked for at once, as far as registers hold it: the parts, PER entries of lists and a word
 // of masks a thread.  Entries beyond those are read once the lists that matter are known.
 template <int PER>
-__global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, int part_values, uint32_t per_width, uint32_t per_parts)
+__global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, uint32_t per_width, uint32_t per_parts)
 {
     __shared__ uint64_t heads[BEAM_LISTS], keys[BEAM_MOST * BEAM_MOST], masks[BEAM_THREADS];
     __shared__ uint32_t index[BEAM_MOST * BEAM_MOST];
     __shared__ double offset[BEAM_MOST]; // score - lse
     __shared__ float scores[BEAM_MOST];
-    __shared__ int parent[BEAM_MOST], ended[BEAM_MOST], chosen[BEAM_MOST], before[64];
+    __shared__ int parent[BEAM_MOST], ended[BEAM_MOST], chosen[BEAM_MOST], ahead_of[2][BEAM_THREADS]; // heads; what is left of the entries
     __shared__ unsigned char counts[BEAM_LISTS];
     __shared__ uint64_t bound;
     __shared__ int listed, found;
     double *const sums = reinterpret_cast<double *>(heads);  // of the parts, until the heads are known
     int *const scales = reinterpret_cast<int *>(index);
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = blockIdx.x, tid = threadIdx.x;
     const int row0 = r * p.beams, lists = p.beams * p.parts, entries = lists * p.width, mask_entries = p.beams * p.a.mask_words;
     const BeamPart *const parts = p.parts_out + (size_t)row0 * p.parts;
     const uint32_t *const candidates = p.candidates + (size_t)row0 * p.parts * p.width;
@@ -267,8 +306,7 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
         scores[tid] = p.a.scores[row0 + tid];
         ended[tid] = p.a.done && p.a.done[row0 + tid] != 0;
     }
-    if (tid < 64)
-        before[tid] = 0;
+    ahead_of[0][tid] = ahead_of[1][tid] = 0;
     if (tid == 0) {
         bound = 1;
         listed = found = 0;
@@ -299,10 +337,11 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
             *at = (uint32_t)b * p.vocab + p.a.eos;
             return part == 0 && j == 0 && off > -INFINITY ? order_of(off) : 0;
         }
-        *at = (uint32_t)b * p.vocab + part * part_values + (0xffff - (c & 0xffff));
+        *at = (uint32_t)b * p.vocab + part * p.part_chunks * 8 + (0xffff - (c & 0xffff));
         return off > -INFINITY && j < counts[l] ? order_of(off + (double)value_of(c >> 16)) : 0;
     };
     const bool all_held = entries <= PER * BEAM_THREADS;
+    const int firsts = all_held ? max(min(64 / lists, p.width), 1) : 1, firsts_all = lists * firsts; // entries of a list that the bound is taken from
     uint64_t held_key[PER];
     uint32_t held_at[PER];
     if (all_held) {
@@ -312,8 +351,8 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
             held_key[k] = 0;
             if (i < entries) {
                 held_key[k] = entry(l, j, held[k], &held_at[k]);
-                if (j == 0)
-                    heads[l] = held_key[k];
+                if (j < firsts)
+                    heads[l * firsts + j] = held_key[k];
             }
         }
     } else {
@@ -322,32 +361,34 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
             heads[l] = entry(l, 0, candidates[(size_t)l * p.width], &at);
     }
     __syncthreads();
-    // Lists whose heads are among the `width` first: no other list has any of the best, and of these what the last of the heads is not ahead of.
-    const auto head_is = [&](uint64_t head, int i, int ahead) {
+    // The width-th of the heads bounds what is among the best; and no list whose head is not among the `width` first has any of them.
+    const auto head_is = [&](int i, int ahead) {
+        const uint64_t head = heads[i];
         if (ahead < p.width && head != 0) {
-            chosen[ahead] = i;
-            if (!all_held)
+            if (!all_held) {
+                chosen[ahead] = i;
                 atomicMax(&found, ahead + 1);
+            }
             if (ahead == p.width - 1)
                 bound = head;
         }
     };
-    if (lists <= 64) { // a lane has one of them, and each in turn is compared with all
-        const uint64_t head = lane < lists ? heads[lane] : 0;
-        for (int i = wave; i < lists; i += BEAM_THREADS / 64) {
-            const uint64_t mine = lane_of(head, i);
-            const int ahead = __popcll(__builtin_amdgcn_ballot_w64(head > mine)) + __popcll(__builtin_amdgcn_ballot_w64(head == mine && lane < i));
-            if (lane == 0)
-                head_is(mine, i, ahead);
-        }
+    if (firsts_all <= BEAM_THREADS) {
+        if (firsts_all <= 64)
+            count_ahead<1>(heads, nullptr, firsts_all, ahead_of[0]);
+        else
+            count_ahead<4>(heads, nullptr, firsts_all, ahead_of[0]);
+        __syncthreads();
+        if (tid < firsts_all)
+            head_is(tid, ahead_of[0][tid]);
     } else {
-        for (int i = tid; i < lists; i += BEAM_THREADS) {
+        for (int i = tid; i < firsts_all; i += BEAM_THREADS) {
             const uint64_t head = heads[i];
             int ahead = 0;
 #pragma unroll 4
-            for (int j = 0; j < lists; ++j)
+            for (int j = 0; j < firsts_all; ++j)
                 ahead += heads[j] > head || (heads[j] == head && j < i);
-            head_is(head, i, ahead);
+            head_is(i, ahead);
         }
     }
     __syncthreads();
@@ -373,24 +414,19 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
     __syncthreads();
     const int count = listed;
     const size_t out = (size_t)r * p.width;
-    const int turns = max(count, p.width);
-    if (turns <= 64) { // a lane has one each, and a wavefront compares a quarter of them with all
-        int few = 0;
-        const uint64_t key = lane < count ? keys[lane] : 0;
-        const uint32_t place = lane < count ? index[lane] : 0xffffffffu;
-        for (int j = wave; j < count; j += BEAM_THREADS / 64) {
-            const uint64_t other = lane_of(key, j);
-            few += other > key || (other == key && (uint32_t)__builtin_amdgcn_readlane((int)place, j) < place);
-        }
-        atomicAdd(&before[lane], few);
+    if (count <= BEAM_THREADS) {
+        if (count <= 64)
+            count_ahead<1>(keys, index, count, ahead_of[1]);
+        else
+            count_ahead<4>(keys, index, count, ahead_of[1]);
         __syncthreads();
     }
-    for (int i = tid; i < turns; i += BEAM_THREADS) {
+    for (int i = tid; i < max(count, p.width); i += BEAM_THREADS) {
         int at = i; // places behind those that are found are empty
         if (i < count) {
             at = 0;
-            if (turns <= 64)
-                at = before[i];
+            if (count <= BEAM_THREADS)
+                at = ahead_of[1][i];
             else
 #pragma unroll 4
                 for (int j = 0; j < count; ++j)
@@ -426,19 +462,24 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, in
 
 uint32_t inverse(int d) { return d > 1 ? (uint32_t)(((1ull << 32) + d - 1) / d) : 0; } // for quotient()
 
-// Small parts where there are few rows: a part is read by one workgroup, and 512 of them fill the chip.
+// The largest parts of which there are enough to fill the chip (what a workgroup does once costs as much as 16 values a thread), and no more of
+// them than a request's lists may be.
 struct BeamPlan {
-    int chunks, parts;
+    int chunks, parts, part_chunks;
     size_t end;
 };
 
 BeamPlan plan_beam(int requests, int beams, int vocab, int width)
 {
     const long long rows = (long long)requests * beams;
-    const auto parts = [&](int chunks) { return (vocab + 8 * BEAM_THREADS * chunks - 1) / (8 * BEAM_THREADS * chunks); };
+    const int all = (vocab + 7) / 8;
+    const auto parts = [&](int chunks) { return (all + BEAM_THREADS * chunks - 1) / (BEAM_THREADS * chunks); };
     BeamPlan s;
-    s.chunks = rows * parts(1) <= 512 ? 1 : 4;
+    s.chunks = 8;
+    while (s.chunks > 1 && rows * parts(s.chunks) < 1200 && beams * parts(s.chunks / 2) <= BEAM_LISTS)
+        s.chunks /= 2;
     s.parts = parts(s.chunks);
+    s.part_chunks = (all + s.parts - 1) / s.parts;
     s.end = (size_t)rows * s.parts * (sizeof(BeamPart) + sizeof(uint32_t) * width);
     return s;
 }
@@ -452,16 +493,13 @@ int fq_launch_beam_step(const void *logits, long long ld, int requests, int beam
     const BeamPlan s = plan_beam(requests, beams, vocab, width);
     const size_t rows = (size_t)requests * beams;
     BeamArgs p{static_cast<const _Float16 *>(logits), ld, a, static_cast<BeamPart *>(workspace),
-               reinterpret_cast<uint32_t *>(static_cast<BeamPart *>(workspace) + rows * s.parts), requests, beams, vocab, width, s.parts};
+               reinterpret_cast<uint32_t *>(static_cast<BeamPart *>(workspace) + rows * s.parts), requests, beams, vocab, width, s.parts, s.part_chunks};
     const dim3 grid((unsigned)(rows * s.parts));
-    if (s.chunks == 1)
-        hipLaunchKernelGGL(beam_rows_kernel<1>, grid, dim3(BEAM_THREADS), 0, st, p);
-    else
-        hipLaunchKernelGGL(beam_rows_kernel<4>, grid, dim3(BEAM_THREADS), 0, st, p);
+    const auto kernel = s.chunks == 1 ? beam_rows_kernel<1> : s.chunks == 2 ? beam_rows_kernel<2> : s.chunks == 4 ? beam_rows_kernel<4> : beam_rows_kernel<8>;
+    hipLaunchKernelGGL(kernel, grid, dim3(BEAM_THREADS), 0, st, p);
     const int rc = (int)hipGetLastError();
     if (rc != 0)
         return rc;
-    hipLaunchKernelGGL(beam_merge_kernel<4>, dim3(requests), dim3(BEAM_THREADS), 0, st, p, 8 * BEAM_THREADS * s.chunks,
-                       inverse(width), inverse(s.parts));
+    hipLaunchKernelGGL(beam_merge_kernel<4>, dim3(requests), dim3(BEAM_THREADS), 0, st, p, inverse(width), inverse(s.parts));
     return (int)hipGetLastError();
 }
