@@ -42,11 +42,23 @@ __device__ __forceinline__ bool alive(float score) { return score > -INFINITY; }
 // leaves the power of two alone.  |x| < 2^17, and x / ln 2 - scale at least -1020.
 constexpr int EXP_TABLE = 256;
 
-__device__ __forceinline__ u2v exp_entry(int k)
+struct ExpTable {
+    double entry[EXP_TABLE];
+};
+constexpr ExpTable exp_entries()
 {
-    const u2v e = __builtin_bit_cast(u2v, exp2((double)k / EXP_TABLE));
-    return u2v{e.x, e.y - ((uint32_t)k << 12)};
+    ExpTable t{};
+    for (int k = 0; k < EXP_TABLE; ++k) {
+        const double x = k * 0.0027076061740622863;
+        double sum = 1.0;
+        for (int n = 22; n > 0; --n) // the series of exp from its end
+            sum = 1.0 + sum * x / n;
+        t.entry[k] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, sum) - ((uint64_t)k << 44));
+    }
+    return t;
 }
+__device__ constexpr ExpTable exp_table = exp_entries();
+
 struct ExpTerms {
     double shift, steps, step, sixth; // 1.5 * 2^52 - 256 scale; 256 / ln 2; -ln 2 / 256, whose error is below 3e-19, times i
     __device__ explicit ExpTerms(int scale) : shift(6755399441055744.0 - 256.0 * scale), steps(369.32993046757464), step(-0.0027076061740622863), sixth(1.0 / 6)
@@ -66,11 +78,14 @@ __device__ __forceinline__ double add_exp(double sum, double x, const ExpTerms &
     return fma(e, __builtin_bit_cast(double, u2v{t.x, t.y + (i << 12)}), sum);
 }
 
-// fp16 (neither NaN nor -0) as whole numbers in the same order; 0 for what is no candidate (-inf).
+// fp16 as whole numbers in the same order, both zeros alike; ORDER_LEAST and above are candidates, -inf is below, +inf and what of NaN is positive from
+// ORDER_INF on.
+constexpr uint32_t ORDER_LEAST = 0x400, ORDER_INF = 0xfc00;
+
 __device__ __forceinline__ uint32_t order_of(_Float16 x)
 {
-    const uint32_t bits = __builtin_bit_cast(unsigned short, x);
-    return bits == 0xfc00 ? 0 : bits & 0x8000 ? 0xffff - bits : bits | 0x8000;
+    const uint32_t bits = __builtin_bit_cast(unsigned short, x), order = bits ^ (bits & 0x8000 ? 0xffff : 0x8000);
+    return order == 0x7fff ? 0x8000 : order;
 }
 __device__ __forceinline__ float value_of(uint32_t order) // of a candidate
 {
@@ -84,12 +99,10 @@ struct __attribute__((packed, aligned(2))) LooseChunk {
     u4v bits;
 };
 
-typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-
 // CHUNKS: 16-byte pieces of a row that a thread has.  Chunks are numbered along the row, so a chunk whose largest value is smaller, or as large and
 // the chunk further on, has nothing ahead of the other's: the order of chunks by (largest value, number) bounds that of their values.
 template <int CHUNKS>
-__global__ __launch_bounds__(BEAM_THREADS, CHUNKS == 8 ? 6 : 8) void beam_rows_kernel(BeamArgs p)
+__global__ __launch_bounds__(BEAM_THREADS, 8) void beam_rows_kernel(BeamArgs p)
 {
     __shared__ __align__(16) uint32_t tops[BEAM_THREADS];
     __shared__ uint32_t list[BEAM_MOST * CHUNKS * 8];
@@ -125,30 +138,20 @@ __global__ __launch_bounds__(BEAM_THREADS, CHUNKS == 8 ? 6 : 8) void beam_rows_k
     }
     if (CHUNKS == 1 && !goes_on)
         return;
-    table[tid] = exp_entry(tid);
+    table[tid] = __builtin_bit_cast(u2v, exp_table.entry[tid]);
     if (tid == 0)
         listed = 0;
     uint32_t order[CHUNKS], top = 0;
-    us2 sizes = {0, 0};
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        const u4v bits = __builtin_bit_cast(u4v, mine[c]) & 0x7fff7fffu;
-        const uint32_t d[4] = {bits.x, bits.y, bits.z, bits.w};
-        h2 high = {(_Float16)-INFINITY, (_Float16)-INFINITY};
+        h2 high = {mine[c][0], mine[c][1]};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sizes = __builtin_elementwise_max(sizes, __builtin_bit_cast(us2, d[e]));
-            const h2 y = h2{mine[c][2 * e], mine[c][2 * e + 1]} + h2{(_Float16)0.f, (_Float16)0.f}; // -0 is 0
-            mine[c][2 * e] = y[0];
-            mine[c][2 * e + 1] = y[1];
-            high = __builtin_elementwise_max(high, y);
-        }
-        const uint32_t o = order_of(__builtin_elementwise_max(high[0], high[1]));
-        order[c] = o ? o << 16 | (0xffff - (c * BEAM_THREADS + tid)) : 0;
+        for (int e = 1; e < 4; ++e)
+            high = __builtin_elementwise_maximum(high, h2{mine[c][2 * e], mine[c][2 * e + 1]}); // NaN where there is one
+        const _Float16 h = __builtin_elementwise_maximum(high[0], high[1]);
+        order[c] = (h != h ? 0xffff : order_of(h)) << 16 | (0xffff - (c * BEAM_THREADS + tid));
         top = max(top, order[c]);
     }
-    if (max(sizes[0], sizes[1]) > 0x7c00) // a NaN
-        top = 0xffffffffu;
     tops[tid] = top;
     __syncthreads();
     const u4v four = *reinterpret_cast<const u4v *>(&tops[4 * lane]); // every wavefront has them all
@@ -157,13 +160,14 @@ __global__ __launch_bounds__(BEAM_THREADS, CHUNKS == 8 ? 6 : 8) void beam_rows_k
     for (int o = 32; o > 0; o >>= 1)
         all = max(all, (uint32_t)__shfl_xor((int)all, o, 64));
     BeamPart *const out = p.parts_out + (size_t)row * p.parts + part;
-    if (all == 0 || all >> 16 >= 0xfc00) { // nothing but -inf, or a NaN or +inf (uniform)
+    const bool none = all >> 16 < ORDER_LEAST;
+    if (none || all >> 16 >= ORDER_INF) { // nothing but -inf, or a NaN or +inf (uniform)
         if (tid == 0)
-            *out = BeamPart{all == 0 ? 0.0 : (double)NAN, all == 0 ? BEAM_NONE : 0, 0};
+            *out = BeamPart{none ? 0.0 : (double)NAN, none ? BEAM_NONE : 0, 0};
         return;
     }
     if (wave == 0) {
-        // The width-th largest, bit by bit: the largest bound that `width` of them reach.  Their lower half is 0xf800 at least; it matters only where
+        // The width-th largest, bit by bit: the largest bound that `width` of them reach.  Their lower half is 0xfc00 at least; it matters only where
         // ties would be more than the list holds.
         uint32_t least = 0;
         const auto reach = [&](uint32_t b) {
@@ -173,14 +177,14 @@ __global__ __launch_bounds__(BEAM_THREADS, CHUNKS == 8 ? 6 : 8) void beam_rows_k
 #pragma unroll 1
         for (uint32_t bit = 1u << 31; bit > 0x8000; bit >>= 1)
             least = reach(least | bit) >= p.width ? least | bit : least;
-        if (least && reach(least) > BEAM_MOST) {
-            least |= 0xf800;
+        if (least >= ORDER_LEAST << 16 && reach(least) > BEAM_MOST) {
+            least |= 0xfc00;
 #pragma unroll 1
-            for (uint32_t bit = 0x400; bit; bit >>= 1)
+            for (uint32_t bit = 0x200; bit; bit >>= 1)
                 least = reach(least | bit) >= p.width ? least | bit : least;
         }
         if (lane == 0)
-            bound = max(least, 1u);
+            bound = max(least, ORDER_LEAST << 16);
     }
     const float high = value_of(all >> 16);
     const int scale = (int)rintf(high * 1.44269504f); // sums as of 2^scale, near exp(high)
@@ -206,7 +210,7 @@ __global__ __launch_bounds__(BEAM_THREADS, CHUNKS == 8 ? 6 : 8) void beam_rows_k
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t o = order_of(mine[c][e]);
-                    if (o && o >= least >> 16)
+                    if (o >= least >> 16)
                         list[atomicAdd(&listed, 1)] = o << 16 | (0xffff - (8 * (c * BEAM_THREADS + tid) + e));
                 }
             }
@@ -462,8 +466,9 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, ui
 
 uint32_t inverse(int d) { return d > 1 ? (uint32_t)(((1ull << 32) + d - 1) / d) : 0; } // for quotient()
 
-// The largest parts of which there are enough to fill the chip (what a workgroup does once costs as much as 16 values a thread), and no more of
-// them than a request's lists may be.
+// The largest parts of which there are enough to fill the chip, and no more of them than a request's lists may be: what a workgroup does once costs as
+// much as 16 values a thread (37 requests of 5 beams, one of them live, 32000 tokens: parts of 2048 values 7.7 us, 4096 7.2; 61 of 12: 8192 values
+// 24.0, 16384 25.7, as their workgroups wait for memory all at once).
 struct BeamPlan {
     int chunks, parts, part_chunks;
     size_t end;
@@ -475,7 +480,7 @@ BeamPlan plan_beam(int requests, int beams, int vocab, int width)
     const int all = (vocab + 7) / 8;
     const auto parts = [&](int chunks) { return (all + BEAM_THREADS * chunks - 1) / (BEAM_THREADS * chunks); };
     BeamPlan s;
-    s.chunks = 8;
+    s.chunks = 4;
     while (s.chunks > 1 && rows * parts(s.chunks) < 1200 && beams * parts(s.chunks / 2) <= BEAM_LISTS)
         s.chunks /= 2;
     s.parts = parts(s.chunks);
@@ -495,7 +500,7 @@ int fq_launch_beam_step(const void *logits, long long ld, int requests, int beam
     BeamArgs p{static_cast<const _Float16 *>(logits), ld, a, static_cast<BeamPart *>(workspace),
                reinterpret_cast<uint32_t *>(static_cast<BeamPart *>(workspace) + rows * s.parts), requests, beams, vocab, width, s.parts, s.part_chunks};
     const dim3 grid((unsigned)(rows * s.parts));
-    const auto kernel = s.chunks == 1 ? beam_rows_kernel<1> : s.chunks == 2 ? beam_rows_kernel<2> : s.chunks == 4 ? beam_rows_kernel<4> : beam_rows_kernel<8>;
+    const auto kernel = s.chunks == 1 ? beam_rows_kernel<1> : s.chunks == 2 ? beam_rows_kernel<2> : beam_rows_kernel<4>;
     hipLaunchKernelGGL(kernel, grid, dim3(BEAM_THREADS), 0, st, p);
     const int rc = (int)hipGetLastError();
     if (rc != 0)
