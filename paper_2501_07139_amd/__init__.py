@@ -132,8 +132,10 @@ def _load_bind():
                       "`python paper_2501_07139_amd/build.py` builds it", RuntimeWarning, stacklevel=2)
         return None
     names = ("fq_qlinear_tile", "fq_qlinear_mixed", "fq_dense_f16", "fq_head_nll", "fq_token_nll", "fq_logit_l2", "fq_qk_norm_rope",
-             "fq_attn_paged", "fq_cache_evict", "fq_paged_plan", "fq_attn_tree", "fq_tree_commit", "fq_beam_step")
+             "fq_attn_paged", "fq_cache_evict")
     _bind.bind(*(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
+    names = ("fq_paged_plan", "fq_attn_tree", "fq_tree_commit", "fq_beam_step")
+    _bind.bind_trees(*(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
     return _bind
 
 

@@ -627,25 +627,41 @@ PyObject *beam_step(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-PyObject *bind(PyObject *, PyObject *args) // addresses of the entry points, in the order of Entries
+// Addresses of the entry points, in the order of Entries: the first nine, and those over trees of tokens.
+PyObject *bind(PyObject *, PyObject *args)
 {
-    unsigned long long p[13];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10], &p[11], &p[12]))
+    unsigned long long p[9];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8]))
         return nullptr;
-    entry = Entries{reinterpret_cast<decltype(entry.qlinear)>(p[0]),  reinterpret_cast<decltype(entry.mixed)>(p[1]),
-                    reinterpret_cast<decltype(entry.dense)>(p[2]),    reinterpret_cast<decltype(entry.head_nll)>(p[3]),
-                    reinterpret_cast<decltype(entry.token_nll)>(p[4]), reinterpret_cast<decltype(entry.logit_l2)>(p[5]),
-                    reinterpret_cast<decltype(entry.norm_rope)>(p[6]), reinterpret_cast<decltype(entry.attn_paged)>(p[7]),
-                    reinterpret_cast<decltype(entry.evict)>(p[8]), reinterpret_cast<decltype(entry.plan)>(p[9]),
-                    reinterpret_cast<decltype(entry.attn_tree)>(p[10]), reinterpret_cast<decltype(entry.commit)>(p[11]),
-                    reinterpret_cast<decltype(entry.beam)>(p[12])};
+    entry.qlinear = reinterpret_cast<decltype(entry.qlinear)>(p[0]);
+    entry.mixed = reinterpret_cast<decltype(entry.mixed)>(p[1]);
+    entry.dense = reinterpret_cast<decltype(entry.dense)>(p[2]);
+    entry.head_nll = reinterpret_cast<decltype(entry.head_nll)>(p[3]);
+    entry.token_nll = reinterpret_cast<decltype(entry.token_nll)>(p[4]);
+    entry.logit_l2 = reinterpret_cast<decltype(entry.logit_l2)>(p[5]);
+    entry.norm_rope = reinterpret_cast<decltype(entry.norm_rope)>(p[6]);
+    entry.attn_paged = reinterpret_cast<decltype(entry.attn_paged)>(p[7]);
+    entry.evict = reinterpret_cast<decltype(entry.evict)>(p[8]);
+    Py_RETURN_NONE;
+}
+
+PyObject *bind_trees(PyObject *, PyObject *args)
+{
+    unsigned long long p[4];
+    if (!PyArg_ParseTuple(args, "KKKK", &p[0], &p[1], &p[2], &p[3]))
+        return nullptr;
+    entry.plan = reinterpret_cast<decltype(entry.plan)>(p[0]);
+    entry.attn_tree = reinterpret_cast<decltype(entry.attn_tree)>(p[1]);
+    entry.commit = reinterpret_cast<decltype(entry.commit)>(p[2]);
+    entry.beam = reinterpret_cast<decltype(entry.beam)>(p[3]);
     Py_RETURN_NONE;
 }
 
 #define FQ_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FQ_FAST(qlinear),   FQ_FAST(mixed),    FQ_FAST(dense_f16), FQ_FAST(head_nll),
                          FQ_FAST(token_nll), FQ_FAST(logit_l2), FQ_FAST(qk_norm_rope), FQ_FAST(attn_paged), FQ_FAST(cache_evict),
-                         FQ_FAST(paged_plan), FQ_FAST(attn_tree), FQ_FAST(tree_commit), FQ_FAST(beam_step), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FQ_FAST(paged_plan), FQ_FAST(attn_tree), FQ_FAST(tree_commit), FQ_FAST(beam_step), {"bind", bind, METH_VARARGS, nullptr},
+                         {"bind_trees", bind_trees, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
