@@ -227,37 +227,37 @@ __global__ __launch_bounds__(256) void plan_tokens_kernel(PlanArgs p)
 }
 
 // ------------------------------------------------------------------ commit
-// A wavefront for one sequence, layer, head and one of keys and values: it finds the path itself (all of them do, at the same time: 64 nodes a
-// step, a ballot for the children) and moves the rows, sixteen at a time, loads ahead of stores.  A path rises, so node path[k] is at least k: what a
-// turn reads lies at or behind what it writes first, and no later turn reads what an earlier one wrote.  No other wavefront has its rows.
+// A workgroup for one sequence, layer and two or eight heads.  Every wavefront finds the path itself (64 nodes a step, a ballot for the children: a barrier
+// would cost as much) and takes every fourth of the items, an item being a row of the path for one head of keys or values, sixteen lanes wide.  Thirty-two items
+// a turn, loads ahead of stores, rows in rising order for each head.  A path rises, so node path[k] is at least k: what a turn reads lies at or behind what it
+// writes, and no later turn reads what an earlier one wrote.  No other wavefront has its heads.  Bound by the chain of loads for one sequence
+// (lengths, nodes and pages, rows), by starting workgroups and the rows' way for many (29 sequences, 32 layers of 8 heads, 26 MB: a wavefront for each head of
+// keys and of values 15.6 us).
+constexpr int COMMIT_ITEMS = 32; // of a turn
+
 struct CommitArgs {
     PagedSeqs s;
     const int *tail, *parents, *drafted, *following;
     _Float16 *k, *v;
     int *path, *accepted, *bonus, *new_len;
-    int layers, kv_heads, path_stride;
+    int layers, kv_heads, path_stride, group_heads, head_groups;
 };
 
-// Row of a position in the pools of one layer, or -1 where its page is none.
-__device__ __forceinline__ long long commit_row(const CommitArgs &p, int b, int kvh, int t)
+__global__ __launch_bounds__(256) void commit_kernel(CommitArgs p)
 {
-    const int pg = p.s.table[(size_t)b * p.s.table_stride + min(t >> p.s.page_log2, p.s.table_stride - 1)];
-    return pg < 0 || pg >= p.s.pages ? -1 : (((long long)pg * p.kv_heads + kvh) << p.s.page_log2) | (t & ((1 << p.s.page_log2) - 1));
-}
-
-__global__ __launch_bounds__(64) void commit_kernel(CommitArgs p)
-{
-    const int b = blockIdx.y, lane = threadIdx.x;
-    const int values = blockIdx.x & 1, at = blockIdx.x >> 1, kvh = at % p.kv_heads, layer = at / p.kv_heads;
+    const int b = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int layer = blockIdx.x / p.head_groups, head0 = (blockIdx.x - layer * p.head_groups) * p.group_heads, heads = min(p.kv_heads - head0, p.group_heads);
     const SeqRange s = seq_range(p.s, b);
-    const bool walk = p.parents != nullptr, writes = blockIdx.x == 0;
-    const int tail = min(max(p.tail ? p.tail[b] : s.n, 0), s.len), base = s.len - tail;
+    const bool walk = p.parents != nullptr, writes = blockIdx.x == 0 && wave == 0;
+    const int tail = min(max(p.tail ? p.tail[b] : s.n, 0), s.len), base = s.len - tail, nodes = min(s.n, tail);
     int *const path_out = p.path + (size_t)b * p.path_stride;
-    const int nodes = min(s.n, tail);
     const int most = walk ? min(nodes, p.path_stride) : min(min(max(p.accepted[b], 0), p.path_stride), tail);
-    _Float16 *const pool = (values ? p.v : p.k) + ((((size_t)layer * p.s.pages * p.kv_heads) << p.s.page_log2)) * PD;
+    const size_t layer_at = (((size_t)layer * p.s.pages * p.kv_heads) << p.s.page_log2) * PD;
 
-    // the first 64 nodes stay in registers
+    // asked for together: the pages from the tail's first on, a lane each, and the first 64 nodes
+    const int page0 = base >> p.s.page_log2;
+    const int *const table = p.s.table + (size_t)b * p.s.table_stride;
+    const int pages = table[min(page0 + lane, p.s.table_stride - 1)];
     const int node = min(lane, max(nodes, 1) - 1);
     int parent0 = -2, drafted0 = 0, next0 = 0;
     if (walk && nodes > 0) {
@@ -265,9 +265,14 @@ __global__ __launch_bounds__(64) void commit_kernel(CommitArgs p)
         drafted0 = p.drafted[s.first + node];
         next0 = p.following[s.first + node];
     }
-    int cur = 0, next_token = -1;
+    // Row of a position in the pools of one layer, or -1 where its page is none.
+    const auto row_of = [&](int kvh, int t) -> long long {
+        const int at = (t >> p.s.page_log2) - page0, held = __shfl(pages, at & 63, 64); // every lane takes part
+        const int pg = at < 64 ? held : table[min(page0 + at, p.s.table_stride - 1)];
+        return pg < 0 || pg >= p.s.pages ? -1 : (((long long)pg * p.kv_heads + kvh) << p.s.page_log2) | (t & ((1 << p.s.page_log2) - 1));
+    };
+    int cur = 0, next_token = -1, k0 = 0;
     bool more = most > 0;
-    int k0 = 0;
     while (k0 < most && more) {
         // up to 64 of the path, lane k has path[k0 + k]
         int mine = -1, count = 0;
@@ -295,26 +300,35 @@ __global__ __launch_bounds__(64) void commit_kernel(CommitArgs p)
         }
         if (walk && writes && lane < count)
             path_out[k0 + lane] = mine;
-        // sixteen lanes a row
-        for (int r0 = 0; r0 < count; r0 += 16) {
-            h8 rows[4];
-            long long to[4];
+        // Rows that stay where they are need nothing; those are the first ones of the whole path, if any.
+        const int still = k0 + count - 1 == __builtin_amdgcn_readlane(mine, count - 1) ? count
+                                                                                     : __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < count && mine != k0 + lane));
+        // Items: rows of the path in order, for each of the wavefront's pools (keys and values of a head are two) in turn.
+        const int rows = count - still, items = rows * ((2 * heads - wave + 3) / 4);
+        const uint32_t inverse = rows > 1 ? 0xffffffffu / (uint32_t)rows + 1 : 0; // 2^32 / rows rounded up: item / rows, both small
+        for (int i0 = 0; i0 < items; i0 += COMMIT_ITEMS) {
+            h8 moved[COMMIT_ITEMS / 4];
+            _Float16 *to[COMMIT_ITEMS / 4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = r0 + 4 * i + (lane >> 4), from_node = __shfl(mine, k & 63, 64);
-                const bool moved = k < count && from_node != k0 + k;
-                const long long from = moved ? commit_row(p, b, kvh, base + from_node) : -1;
-                to[i] = moved && from >= 0 ? commit_row(p, b, kvh, base + k0 + k) : -1;
-                rows[i] = h8{};
-                if (to[i] >= 0)
-                    rows[i] = *reinterpret_cast<const h8 *>(pool + from * PD + 8 * (lane & 15));
+            for (int i = 0; i < COMMIT_ITEMS / 4; ++i) {
+                to[i] = nullptr;
+                if (i0 + 4 * i >= items) // uniform
+                    continue;
+                const int item = min(i0 + 4 * i + (lane >> 4), items - 1), set = inverse ? (int)__umulhi((uint32_t)item, inverse) : item;
+                const int k = still + item - set * rows, which = wave + 4 * set, kvh = head0 + (which >> 1);
+                const long long from = row_of(kvh, base + __shfl(mine, k, 64)), at = row_of(kvh, base + k0 + k);
+                _Float16 *const pool = (which & 1 ? p.v : p.k) + layer_at + 8 * (lane & 15);
+                to[i] = i0 + 4 * i + (lane >> 4) < items && from >= 0 && at >= 0 ? pool + at * PD : nullptr;
+                moved[i] = h8{};
+                if (to[i])
+                    moved[i] = *reinterpret_cast<const h8 *>(pool + from * PD);
             }
             __builtin_amdgcn_s_waitcnt(FQ_WAIT_VMCNT0); // every load of the turn is back before its first store
             asm volatile("" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (to[i] >= 0)
-                    *reinterpret_cast<h8 *>(pool + to[i] * PD + 8 * (lane & 15)) = rows[i];
+            for (int i = 0; i < COMMIT_ITEMS / 4; ++i)
+                if (to[i])
+                    *reinterpret_cast<h8 *>(to[i]) = moved[i];
         }
         k0 += count;
     }
@@ -353,8 +367,10 @@ int fq_launch_tree_commit(const fq_paged_batch &b, const int32_t *tail, const in
                           void *k_pages, void *v_pages, int layers, int kv_heads, int32_t *path, int path_stride, int32_t *accepted, int32_t *bonus,
                           int32_t *new_len, fq_stream st)
 {
+    // few workgroups: two heads each, so that a wavefront has one pool (one sequence, four layers of eight heads: 4.9 -> 4.0 us)
+    const int group_heads = (long long)layers * ((kv_heads + 7) / 8) * b.seqs >= 256 ? 8 : 2;
     CommitArgs p{paged_seqs(b), tail, parents, drafted, following, static_cast<_Float16 *>(k_pages), static_cast<_Float16 *>(v_pages), path, accepted,
-                 bonus, new_len, layers, kv_heads, path_stride};
-    hipLaunchKernelGGL(commit_kernel, dim3(2 * layers * kv_heads, b.seqs), dim3(64), 0, st, p);
+                 bonus, new_len, layers, kv_heads, path_stride, group_heads, (kv_heads + group_heads - 1) / group_heads};
+    hipLaunchKernelGGL(commit_kernel, dim3(layers * p.head_groups, b.seqs), dim3(256), 0, st, p);
     return (int)hipGetLastError();
 }
