@@ -998,7 +998,7 @@ extern "C" size_t fq_attn_tree_workspace_bytes(const fq_paged_batch *batch, int 
     const char *fn = "fq_attn_tree_workspace_bytes";
     if (check_batch(fn, batch, n_kv_heads) || check_heads(fn, batch->tokens, n_heads, n_kv_heads))
         return 0;
-    return align_up(fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, false));
+    return align_up(fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, false, true));
 }
 
 extern "C" int fq_attn_tree(const fq_paged_batch *batch, const uint64_t *mask, int mask_words, const int32_t *tail, const void *q, int ldq, int n_heads,
@@ -1018,7 +1018,7 @@ extern "C" int fq_attn_tree(const fq_paged_batch *batch, const uint64_t *mask, i
         return fq_fail(FQ_ERR_SHAPE, "%s: ldq=%d (at least the row, a multiple of 8)", fn, ldq);
     if (!(scale > 0.f) || scale > 1e30f)
         return fq_fail(FQ_ERR_SHAPE, "%s: scale=%g (must be positive and finite)", fn, scale);
-    const size_t need = fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, false);
+    const size_t need = fq_attn_paged_scratch_bytes(*batch, n_heads, n_kv_heads, false, true);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fq_fail(FQ_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(mask) & 7))

@@ -60,17 +60,24 @@ struct RowTile {
 };
 
 // Tile `tile` of TR rows, counted over the sequences; rows < 0 where there is none.  Every wavefront scans the sequences' tile counts.
+// TREE with p.packed: item `tile` of the splits of all tiles, a sequence's splits in turn and in each the tiles, which read the same positions; *split takes
+// its number.
 template <int TR, bool TREE>
-__device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile)
+__device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile, int *split)
 {
+    const bool packed = TREE && p.packed;
     const int lane = threadIdx.x & 63;
     RowTile r;
     r.rows = -1;
     int base = 0;
     for (int i = 0; i < p.s.seqs; i += 64) {
         int count = 0;
-        if (i + lane < p.s.seqs)
-            count = (seq_range(p.s, i + lane).n * p.group + TR - 1) / TR;
+        if (i + lane < p.s.seqs) {
+            const SeqRange s = seq_range(p.s, i + lane);
+            count = (s.n * p.group + TR - 1) / TR;
+            if (packed)
+                count *= max((s.len + p.chunk - 1) / p.chunk, 1);
+        }
         int upto = count; // inclusive sums over the lanes
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -81,9 +88,15 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile)
         if (behind) {
             const int at = __builtin_ctzll(behind);
             r.b = i + at;
-            r.row0 = (tile - base - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(count, at))) * TR;
+            int mine = tile - base - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(count, at));
             r.s = seq_range(p.s, r.b);
             r.rows = r.s.n * p.group;
+            if (packed) {
+                const int tiles = (r.rows + TR - 1) / TR;
+                *split = mine / tiles;
+                mine -= *split * tiles;
+            }
+            r.row0 = mine * TR;
             const int last = min(r.row0 + TR, r.rows) - 1;
             r.seen = TREE ? r.s.len : max(min(r.s.len - r.s.n + last / p.group + 1, r.s.len), 0);
             return r;
@@ -417,9 +430,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
 
     // Longest tiles first; where all workgroups are resident together, two a CU, dealt from both ends: b and b + half share a CU.
     const int jobs = (int)gridDim.x, half = (jobs + 1) >> 1, bidx = (int)blockIdx.x;
-    const int job = bidx < half || jobs * (int)gridDim.y > 512 ? bidx : jobs - 1 - (bidx - half);
-    const int kvh = job % p.kv_heads, split = blockIdx.y;
-    const RowTile tile = find_tile<TR, TREE>(p, p.tiles - 1 - job / p.kv_heads);
+    const int job = bidx < half || jobs * (int)gridDim.y > 512 || (TREE && p.packed) ? bidx : jobs - 1 - (bidx - half);
+    const int kvh = job % p.kv_heads;
+    int split = blockIdx.y;
+    const RowTile tile = find_tile<TR, TREE>(p, TREE && p.packed ? job / p.kv_heads : p.tiles - 1 - job / p.kv_heads, &split);
     if (tile.rows < 0)
         return;
     const int begin = split * p.chunk, end = min(tile.seen, begin + p.chunk);
@@ -435,6 +449,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     const int all_seen = TREE ? older : older + min(row0, tile.rows - 1) / p.group + 1; // ... that every row of the wavefront sees
     const int any_seen = TREE ? tile.s.len : older + min(row0 + 31, tile.rows - 1) / p.group + 1;
     const uint64_t *const mask = TREE ? p.mask + (size_t)(tile.s.first + token) * p.mask_words : nullptr;
+    // A wavefront without rows copies its share of the tiles and leaves the rest of the CU to others: trees have few rows, and the last tile of most is not full.
+    const bool idle = TREE && row0 >= tile.rows;
 
     h8 qb[8];
     {
@@ -525,7 +541,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
         const char *const Kcur = reinterpret_cast<const char *>(PAR ? Ks1 : Ks0), *const Vcur = reinterpret_cast<const char *>(PAR ? Vs1 : Vs0);
         h8 *const Knext = PAR ? Ks0 : Ks1, *const Vnext = PAR ? Vs0 : Vs1;
         const int first = begin + KT * jt + 32 * KB * kpart; // first position of the wavefront's part
-        if (PLAIN || first < min(any_seen, end)) {
+        if (!idle && (PLAIN || first < min(any_seen, end))) {
             // the next tile's copies go out between the products: issued in a row they wait for each other
             f16v st[KB];
 #pragma unroll
@@ -706,7 +722,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
 // Joins the splits of a row.  WAVES wavefronts each, which deal the splits among them; a wavefront takes 64 of its own at a time: a lane has one's
 // maximum and sum, then two dimensions of the outputs, eight loads at a time (those are what a row waits for: a token over 100003 positions, 196
 // splits of 32 rows, 9.5 us with four wavefronts, 6.2 with sixteen; 4.6 for up to eight splits, which is the launch and two loads in turn).  Rows of tiles that one split has served are done already.
-template <int WAVES, bool TREE = false>
+template <int WAVES>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_kernel(PagedAttnArgs p, int tile_rows)
 {
     __shared__ float sums[WAVES][PD + 2];
@@ -721,9 +737,9 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_ker
         return;
     const int row = token * p.group + head % p.group;
     const int last = min((row / tile_rows + 1) * tile_rows, s.n * p.group) - 1;
-    if ((TREE ? s.len : s.len - s.n + last / p.group + 1) <= p.chunk)
+    if (s.len - s.n + last / p.group + 1 <= p.chunk)
         return;
-    const int live = ((TREE ? s.len : max(s.len - s.n + token + 1, 0)) + p.chunk - 1) / p.chunk;
+    const int live = (max(s.len - s.n + token + 1, 0) + p.chunk - 1) / p.chunk;
     const size_t stride = (size_t)p.s.tokens * p.heads;
     const f2 *ml = reinterpret_cast<const f2 *>(p.part_ml) + item, *o = reinterpret_cast<const f2 *>(p.part_o) + (size_t)item * (PD / 2) + lane;
     float mx = -INFINITY, l = 0.f, a0 = 0.f, a1 = 0.f;
@@ -788,6 +804,108 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_ker
     *reinterpret_cast<h2 *>(p.out + (size_t)item * PD + 2 * lane) = h2{(_Float16)(a0 * inv), (_Float16)(a1 * inv)};
     if (lane == 0 && p.lse)
         p.lse[item] = (mx + log2f(l)) * LN2;
+}
+
+// The same for trees, whose rows have all splits of their sequence.  Half a wavefront has four dimensions a lane and asks for all it needs of eight splits at
+// once.  A workgroup has eight heads of a token, one each half wavefront; or with SPREAD, where there are many splits for the jobs, one head, and they deal the
+// splits.  Jobs are counted over the sequences that have several splits, and a grid of 1024 workgroups takes them in turn: to start a workgroup takes an XCD about
+// 20 clocks (704 tokens of 40 heads, 178 of them with up to 4 splits: 10.6 us with a wavefront for each head of each token, 8.7 with a workgroup for each eight).
+template <bool SPREAD>
+__global__ __launch_bounds__(256) void attn_tree_merge_kernel(PagedAttnArgs p)
+{
+    __shared__ f4 sums[8][PD / 4];
+    __shared__ float tops[8], norms[8];
+    const int half = threadIdx.x >> 5, d = threadIdx.x & 31, groups = SPREAD ? p.heads : (p.heads + 7) / 8;
+    const size_t stride = (size_t)p.s.tokens * p.heads;
+    const int lane = threadIdx.x & 63;
+    for (int job = blockIdx.x;; job += gridDim.x) {
+        SeqRange s;
+        int at = -1, base = 0; // of the job in its sequence
+        for (int i = 0; i < p.s.seqs && at < 0; i += 64) {
+            SeqRange mine = {0, 0, 0};
+            if (i + lane < p.s.seqs)
+                mine = seq_range(p.s, i + lane);
+            const int count = mine.len > p.chunk ? mine.n * groups : 0;
+            int upto = count; // inclusive sums over the lanes
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(upto, o, 64);
+                upto += lane >= o ? v : 0;
+            }
+            const unsigned long long behind = __builtin_amdgcn_ballot_w64(base + upto > job);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                at = job - base - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(count, l));
+                s.first = __builtin_amdgcn_readlane(mine.first, l);
+                s.n = __builtin_amdgcn_readlane(mine.n, l);
+                s.len = __builtin_amdgcn_readlane(mine.len, l);
+            }
+            base += __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (at < 0) // no more of them
+            return;
+        const int token = at / groups, part = at - token * groups, m = s.first + token, head = SPREAD ? part : 8 * part + half;
+        if (head >= p.heads)
+            continue;
+        const int live = (s.len + p.chunk - 1) / p.chunk, mine = SPREAD ? max((live - half + 7) / 8, 0) : live; // splits of half a wavefront, every eighth
+        const size_t item = (size_t)m * p.heads + head;
+        const f2 *ml = reinterpret_cast<const f2 *>(p.part_ml) + item;
+        const f4 *o = reinterpret_cast<const f4 *>(p.part_o) + item * (PD / 4) + d;
+        float mx = -INFINITY, l = 0.f;
+        f4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = 0; i0 < mine; i0 += 8) {
+            f2 a[8];
+            f4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { // those past the last one repeat it, with a weight of zero
+                const int split = min(i0 + i, mine - 1) * (SPREAD ? 8 : 1) + (SPREAD ? half : 0);
+                a[i] = ml[split * stride];
+                v[i] = o[split * stride * (PD / 4)];
+            }
+            float top = mx;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                top = fmaxf(top, a[i][0]);
+            const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(mx - ref);
+            mx = top;
+            l *= alpha;
+            acc *= alpha;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < mine) {
+                    const float w = __builtin_amdgcn_exp2f(a[i][0] - ref);
+                    l = fmaf(w, a[i][1], l);
+                    acc += v[i] * w;
+                }
+        }
+        if constexpr (SPREAD) {
+            sums[half][d] = acc;
+            if (d == 0) {
+                tops[half] = mx;
+                norms[half] = l;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                mx = fmaxf(mx, tops[i]);
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            l = 0.f;
+            acc = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = __builtin_amdgcn_exp2f(tops[i] - ref);
+                l = fmaf(w, norms[i], l);
+                acc += sums[i][d] * w;
+            }
+            __syncthreads(); // read ahead of the next turn's
+            if (half != 0)
+                continue;
+        }
+        const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+        *reinterpret_cast<h4 *>(p.out + item * PD + 4 * d) = h4{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv), (_Float16)(acc[3] * inv)};
+        if (d == 0 && p.lse)
+            p.lse[item] = (mx + log2f(l)) * LN2;
+    }
 }
 
 // --------------------------------------------------------------- column sums
@@ -1089,7 +1207,41 @@ struct AttnPlan {
     int scores_stride, parts, part_rows; // of the column sums: parts of the rows, rows of one
 };
 
-AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weights)
+//
+// Trees of more than sixteen rows: an estimate of their own, as their wavefronts without rows are idle and their splits that there are come first.  Rows and
+// positions are those that the caller states, or sequences half as long as the longest; a sequence's last tile is taken to be half full, and a tile costs by 32
+// rows that it has and by itself.  Over 46 calls of 3 to 150 nodes and 20 to 30000 positions its choice takes 2.7 % longer than the best of both heights and up
+// to fifteen lengths (fitted to half of them 3 to 6 % on the others), that for chunks 9 %: 12 sequences of up to 46 nodes of 40 heads, 8 key/value heads
+// and 2539 positions 36 -> 27 us.
+void plan_tree(const fq_paged_batch &b, int heads, int kv_heads, int *rows_out, int *chunk_out)
+{
+    const int group = heads / kv_heads;
+    const bool known = b.positions > 0 && b.pairs > 0;
+    const double tokens = b.tokens, positions = known ? (double)b.positions : b.seqs > 1 ? 0.5 * b.seqs * b.max_len + 1 : b.max_len + 1.0;
+    const double pairs = known ? (double)b.pairs : tokens * positions / b.seqs, seen_rows = pairs * group / positions; // of a sequence, as a position sees them
+    const double items = tokens * heads, slow = b.page < KT ? 1.96 : 1.0; // four pages a tile to look up
+    double best = 0;
+    for (int rows = 64; rows <= 128; rows *= 2)
+        for (int chunk = 128;; chunk += chunk < 768 ? 128 : chunk < 1536 ? 256 : chunk < 2048 ? 512 : chunk) {
+            const int splits = (b.max_len + chunk - 1) / chunk;
+            const double tiles = seen_rows / rows + 0.5 > 1 ? seen_rows / rows + 0.5 : 1, units = seen_rows / 32 + 0.5 > 1 ? seen_rows / 32 + 0.5 : 1;
+            const double length = chunk < b.max_len + KT ? chunk : b.max_len + KT, alone = length / KT * (rows == 64 ? 0.65 : 0.77) * slow;
+            const double together = kv_heads / 256.0 * positions / KT * (tiles * (rows == 64 ? 0.35 : 0.16) + units * 0.43) * slow;
+            const double all = items * splits, longer = pairs * heads / chunk + items, parts = longer < all ? longer : all;
+            const double full = tokens * group / rows + (b.seqs < tokens * group ? b.seqs : tokens * group);
+            const double us = 9.2 + (alone > together ? alone + 0.28 * together : together + 0.28 * alone) + 0.001 * full * kv_heads * splits +
+                              (splits > 1 ? 5.6 + 260e-6 * parts : 0) + (splits > 8 ? 0.7 : 0);
+            if ((best == 0 || us < best) && (splits == 1 || all <= 1 << 20)) {
+                best = us;
+                *rows_out = rows;
+                *chunk_out = chunk;
+            }
+            if (splits <= 1)
+                break;
+        }
+}
+
+AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weights, bool tree = false)
 {
     AttnPlan s;
     const int group = heads / kv_heads;
@@ -1106,6 +1258,9 @@ AttnPlan plan_attn(const fq_paged_batch &b, int heads, int kv_heads, bool weight
         const auto pieces = [&](int chunk) { return jobs * ((b.max_len + chunk - 1) / chunk); };
         const bool one = b.max_len <= (jobs >= 160 ? FEW_CHUNK : jobs >= 128 ? 512 : 384); // no split is longer than FEW_CHUNK
         s.chunk = one ? (b.max_len + 127) / 128 * 128 : pieces(128) <= 384 ? 128 : pieces(256) <= 384 ? 256 : 512;
+    } else if (tree) {
+        plan_tree(b, heads, kv_heads, &s.rows, &s.chunk);
+        s.tiles = (int)tiles(s.rows);
     } else {
         // steps of a tile, all splits together; several sequences are taken to be half as long as the longest where the caller does not say
         const double mean = (b.max_len > b.max_q ? b.max_len - 0.5 * b.max_q : 0.5 * b.max_len) / KT * (b.seqs > 1 ? 0.5 : 1.0) + 0.5;
@@ -1186,16 +1341,16 @@ void fq_attn_paged_plan(const fq_paged_batch &b, int heads, int kv_heads, int *r
     *chunk = s.chunk;
 }
 
-size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights)
+size_t fq_attn_paged_scratch_bytes(const fq_paged_batch &b, int heads, int kv_heads, bool weights, bool tree)
 {
-    return plan_attn(b, heads, kv_heads, weights).end * sizeof(float);
+    return plan_attn(b, heads, kv_heads, weights, tree).end * sizeof(float);
 }
 
 int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int heads, int kv_heads, const void *k, const void *v, float scale,
                          void *out, float *lse, const float *weights, float *weights_out, int weights_stride, void *workspace, fq_stream st,
                          const uint64_t *mask, int mask_words, const int32_t *tail)
 {
-    const AttnPlan s = plan_attn(b, heads, kv_heads, weights_out != nullptr);
+    const AttnPlan s = plan_attn(b, heads, kv_heads, weights_out != nullptr, mask != nullptr);
     float *ws = static_cast<float *>(workspace);
     PagedAttnArgs a;
     a.s = paged_seqs(b);
@@ -1228,7 +1383,8 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
     const bool joined = weights_out && s.rows == FEW && s.splits > 1 && s.splits <= 8; // with the column sums
     if (b.tokens > 0) {
         const long long jobs = (long long)s.tiles * kv_heads;
-        a.packed = s.rows == FEW && b.seqs > 1 && s.splits > 1 && jobs * s.splits > 768 && jobs * s.splits < 1 << 24; // more than are resident together
+        // more than are resident together, and those that there are come first
+        a.packed = tree && s.rows != FEW ? s.splits > 1 && jobs * s.splits < 1 << 24 : s.rows == FEW && b.seqs > 1 && s.splits > 1 && jobs * s.splits > 768 && jobs * s.splits < 1 << 24;
         const dim3 grid((unsigned)(jobs * (a.packed ? s.splits : 1)), a.packed ? 1 : s.splits);
         if (s.rows == FEW && tree)
             hipLaunchKernelGGL((attn_paged_few_kernel<false, true>), grid, dim3(256), 0, st, a);
@@ -1256,14 +1412,18 @@ int fq_launch_attn_paged(const fq_paged_batch &b, const void *q, int ldq, int he
         if (rc != 0)
             return rc;
         if (s.splits > 1 && !joined) {
-            const size_t items = (size_t)b.tokens * heads;
+            const size_t items = (size_t)b.tokens * heads, groups = (size_t)b.tokens * ((heads + 7) / 8);
             // more than a wavefront takes at once; more than one of its turns (a grid has less than 2^32 threads)
-            if (s.splits > 64 && items < 1 << 22)
-                hipLaunchKernelGGL((tree ? attn_paged_merge_kernel<16, true> : attn_paged_merge_kernel<16>), dim3((unsigned)items), dim3(1024), 0, st, a, s.rows);
+            if (tree && (items + 1023) / 1024 * 8 < (size_t)s.splits) // fewer turns over the jobs than over the splits
+                hipLaunchKernelGGL(attn_tree_merge_kernel<true>, dim3((unsigned)(items < 1024 ? items : 1024)), dim3(256), 0, st, a);
+            else if (tree)
+                hipLaunchKernelGGL(attn_tree_merge_kernel<false>, dim3((unsigned)(groups < 1024 ? groups : 1024)), dim3(256), 0, st, a);
+            else if (s.splits > 64 && items < 1 << 22)
+                hipLaunchKernelGGL(attn_paged_merge_kernel<16>, dim3((unsigned)items), dim3(1024), 0, st, a, s.rows);
             else if (s.splits > 8 && items < 1 << 24)
-                hipLaunchKernelGGL((tree ? attn_paged_merge_kernel<4, true> : attn_paged_merge_kernel<4>), dim3((unsigned)items), dim3(256), 0, st, a, s.rows);
+                hipLaunchKernelGGL(attn_paged_merge_kernel<4>, dim3((unsigned)items), dim3(256), 0, st, a, s.rows);
             else
-                hipLaunchKernelGGL((tree ? attn_paged_merge_kernel<1, true> : attn_paged_merge_kernel<1>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
+                hipLaunchKernelGGL(attn_paged_merge_kernel<1>, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a, s.rows);
             if ((rc = (int)hipGetLastError()) != 0)
                 return rc;
         }

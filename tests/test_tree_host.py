@@ -109,7 +109,11 @@ def test_workspaces():
     assert 4 * 64 * 32 * (16 + 4 * 64) <= most < 1 << 28
     assert fq._lib.fq_attn_tree_workspace_bytes(None, 2, 2) == 0
     b = batch(max_len=4000, table_stride=250)
-    assert fq._lib.fq_attn_tree_workspace_bytes(ctypes.byref(b), 2, 2) == fq._lib.fq_attn_paged_workspace_bytes(ctypes.byref(b), 2, 2, 0) > 0
+    assert fq._lib.fq_attn_tree_workspace_bytes(ctypes.byref(b), 2, 2) > 0
+    # whatever the sizes: no more than 2^20 rows' parts, a split covers 128 positions at least
+    for tokens, max_q, max_len, seqs in ((60000, 60000, 1 << 24, 1), (65535, 1, 1 << 24, 65535), (3, 3, 1 << 24, 1), (40, 20, 1, 2), (5000, 1000, 0, 300)):
+        b = batch(tokens=tokens, max_q=max_q, seqs=seqs, max_len=max_len, table_stride=1 << 20)
+        assert fq._lib.fq_attn_tree_workspace_bytes(ctypes.byref(b), 16, 2) <= (1 << 20) * 520 + 256 or max_q == 1
 
 
 def test_reserved_batch():
