@@ -5,15 +5,17 @@
 namespace {
 
 // ------------------------------------------------------------------ plan
-// From lengths to the arrays of a batch.  With f pages on the stack of free ones, r_b pages given back by sequence b and t_b taken:
-//   stack'  = stack ++ pages of closed sequences, in order;    page j that sequence b takes = stack'[f + R - 1 - (t_0 + .. + t_b-1 + j)],
-// so that everything is a prefix sum over the sequences and then work on items (pages, tokens) that find their sequence by the sums.  One
-// workgroup does the sums, and the items too where they are few: such a call is the latency of a launch and of a few loads that wait for
-// each other.  Many tokens are left to a second launch with a workgroup for 1024 of a sequence.
-constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
-constexpr int PLAN_TOKENS = 8192;      // that the first launch does itself
-constexpr int TREE_NODES = 64 * 64;    // of a sequence: FQ_TREE_WORDS words of 64
-constexpr int SUM_CAP = 1 << 29;       // sums stay there: min(a + b, cap) is as good as + for sums of what is not negative
+// From lengths to the arrays of a batch.  With f pages on the stack of free ones, R given back by closed sequences and t_b taken by sequence b:
+//   stack' = stack ++ pages of closed sequences, in order;    page j that sequence b takes = stack'[f + R - 1 - (t_0 + .. + t_(b-1) + j)],
+// so that everything is prefix sums over the sequences and then work on items (pages, tokens) that find their sequence by the sums.  One workgroup does
+// the sums, and the items too where they are few: such a call is a launch and the loads that wait for each other (what the sequences have, then free pages
+// and tables), so all inputs are asked for at once, nothing that is written is read again, and few sequences take a quarter of the threads, whose barriers
+// cost less (7 sequences of a token 5.9 -> 4.3 us, kernel 3.2).  Many tokens are left to a second launch with a workgroup for 1024 of
+// a sequence.
+constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_TOKENS = 8192;   // that the first launch does itself
+constexpr int TREE_NODES = 64 * 64; // of a sequence: FQ_TREE_WORDS words of 64
+constexpr int SUM_CAP = 1 << 29;    // sums stay there: min(a + b, cap) is as good as + for sums of what is not negative
 
 struct PlanArgs {
     int *q_start, *seq_len, *table;
@@ -23,37 +25,47 @@ struct PlanArgs {
 
 __device__ __forceinline__ int capped(int a, int b) { return min(a + b, SUM_CAP); }
 
-// Inclusive sums over the workgroup; the same scratch may be used again behind a barrier.
-__device__ __forceinline__ int block_sums(int x, int *scratch)
+// Inclusive sums of N numbers a thread over the workgroup.
+template <int N, int THREADS>
+__device__ __forceinline__ void block_sums(int (&x)[N], int (&scratch)[N][THREADS / 64])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(x, o, 64);
-        x = lane >= o ? capped(x, v) : x;
-    }
-    if (lane == 63)
-        scratch[wave] = x;
-    __syncthreads();
-    int before = 0;
+    for (int o = 1; o < 64; o <<= 1)
 #pragma unroll
-    for (int w = 0; w < PLAN_WAVES; ++w)
-        before = w < wave ? capped(before, scratch[w]) : before;
-    return capped(x, before);
+        for (int n = 0; n < N; ++n) {
+            const int v = __shfl_up(x[n], o, 64);
+            x[n] = lane >= o ? capped(x[n], v) : x[n];
+        }
+    if (lane == 63)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            scratch[n][wave] = x[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        int before = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w)
+            before = w < wave ? capped(before, scratch[n][w]) : before;
+        x[n] = capped(x[n], before);
+    }
 }
 
-// The first of `count` entries of rising sums that is above k; k is below the last one.
-__device__ __forceinline__ int find_above(const int *upto, int count, int k)
+// The first of `count` entries of rising sums that is above k[i], which is below the last one; several at a time, as each step waits for the one before.
+template <int N>
+__device__ __forceinline__ void find_above(const int *upto, int count, const int (&k)[N], int (&at)[N])
 {
-    int lo = 0, hi = count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (upto[mid] > k)
-            hi = mid;
-        else
-            lo = mid + 1;
-    }
-    return lo;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        at[i] = 0;
+    for (int step = 1 << (31 - __builtin_clz(max(count, 1))); step > 0; step >>= 1) // entries ahead of `at` are not above
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            at[i] += at[i] + step <= count && upto[at[i] + step - 1] <= k[i] ? step : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        at[i] = min(at[i], count - 1);
 }
 
 // Page and place of position t of sequence b, as a slot; -1 where it has no page.
@@ -91,81 +103,134 @@ __device__ __forceinline__ void clear_rows(const PlanArgs &p, int from, int firs
     }
 }
 
-__global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanArgs p, int with_tokens)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void plan_kernel(PlanArgs p, int with_tokens)
 {
-    __shared__ int scratch[2][PLAN_WAVES];
-    __shared__ int upto[PLAN_THREADS], item_at[PLAN_THREADS], held_of[PLAN_THREADS], ahead[PLAN_THREADS], next[PLAN_THREADS];
-    __shared__ int parents[PLAN_TOKENS];
+    constexpr int TOKENS = THREADS == PLAN_THREADS ? PLAN_TOKENS : 1024, AHEAD = TOKENS / THREADS;
+    __shared__ int scratch[2][THREADS / 64], scratch1[1][THREADS / 64];
+    __shared__ int upto[THREADS], taken_upto[THREADS], back_upto[THREADS], held_of[THREADS], ahead[THREADS], next[THREADS];
+    __shared__ int parents[TOKENS];
     const int tid = threadIdx.x;
     const int capacity = min((long long)p.max_len, (long long)p.table_stride << p.page_log2);
     const int free0 = min(max(p.a.free_count[0], 0), p.pages);
+    const bool with_parents = with_tokens && p.a.parents, one_turn = p.seqs <= THREADS;
+    int parent[AHEAD];
+    if (with_parents && one_turn) // of the first tokens, whichever sequences they are of
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            parent[i] = tid + THREADS * i < p.tokens ? p.a.parents[tid + THREADS * i] : 0;
 
-    // what closed sequences give back
-    int back = 0;
-    for (int c0 = 0; c0 < p.seqs; c0 += PLAN_THREADS) {
-        const int b = c0 + tid;
-        const int r = b < p.seqs && p.a.new_tokens[b] < 0 ? min(max(p.a.held[b], 0), p.table_stride) : 0;
-        const int sum = block_sums(r, scratch[0]);
-        upto[tid] = sum;
-        __syncthreads();
-        const int total = upto[PLAN_THREADS - 1];
-        for (int k = tid; k < total; k += PLAN_THREADS) {
-            const int s = find_above(upto, PLAN_THREADS, k), j = k - (s > 0 ? upto[s - 1] : 0);
-            if (free0 + back + k < p.pages)
-                p.a.free_pages[free0 + back + k] = p.table[(size_t)(c0 + s) * p.table_stride + j];
+    // Pages that closed sequences give back go on the stack, from place `from` on.
+    const auto give_back = [&](int c0, int from, int total) {
+        for (int k = tid; k < total; k += THREADS) {
+            const int item[1] = {k};
+            int s[1];
+            find_above(back_upto, THREADS, item, s);
+            const int j = k - (s[0] > 0 ? back_upto[s[0] - 1] : 0);
+            if (from + k < p.pages)
+                p.a.free_pages[from + k] = p.table[(size_t)(c0 + s[0]) * p.table_stride + j];
         }
-        back = capped(back, total);
-        __syncthreads();
-    }
-    const int have = min(free0 + min(back, p.pages), p.pages);
+    };
+    int back = 0; // of all sequences; more than one turn of them: all are looked at ahead of the rest
+    if (!one_turn)
+        for (int c0 = 0; c0 < p.seqs; c0 += THREADS) {
+            const int b = c0 + tid;
+            int sum[1] = {b < p.seqs && p.a.new_tokens[b] < 0 ? min(max(p.a.held[b], 0), p.table_stride) : 0};
+            block_sums<1, THREADS>(sum, scratch1);
+            back_upto[tid] = sum[0];
+            __syncthreads();
+            const int total = back_upto[THREADS - 1];
+            give_back(c0, min(capped(free0, back), p.pages), total);
+            back = capped(back, total);
+            __syncthreads();
+        }
 
     int tokens = 0, taken = 0;
-    for (int c0 = 0; c0 < p.seqs; c0 += PLAN_THREADS) {
-        const int b = c0 + tid;
+    for (int c0 = 0; c0 < p.seqs; c0 += THREADS) {
+        const int b = c0 + tid, seqs = min(p.seqs - c0, THREADS);
         int n = 0, before = 0, held = 0, position = 0;
         bool open = false;
         if (b < p.seqs) {
             const int want = p.a.new_tokens[b];
+            before = p.a.cached[b];
+            held = p.a.held[b];
+            position = p.a.next_position ? p.a.next_position[b] : 0;
             open = want >= 0;
-            before = min(max(p.a.cached[b], 0), capacity);
-            held = min(max(p.a.held[b], 0), p.table_stride);
-            position = p.a.next_position ? p.a.next_position[b] : before;
+            before = min(max(before, 0), capacity);
+            held = min(max(held, 0), p.table_stride);
+            position = p.a.next_position ? position : before;
             n = min(min(max(want, 0), p.max_q), capacity - before);
         }
-        const int end = min(capped(tokens, block_sums(n, scratch[0])), p.tokens);
-        upto[tid] = end;
-        held_of[tid] = held;
-        ahead[tid] = before;
-        next[tid] = position;
-        __syncthreads();
-        const int first = tid > 0 ? upto[tid - 1] : tokens, all_tokens = upto[PLAN_THREADS - 1];
+        int sum[2] = {n, open || b >= p.seqs ? 0 : held};
+        block_sums<2, THREADS>(sum, scratch);
+        const int end = min(capped(tokens, sum[0]), p.tokens), first = min(capped(tokens, sum[0] - n), p.tokens);
         n = end - first;
         const int len = open ? before + n : 0;
         const int need = open ? max(((len + (1 << p.page_log2) - 1) >> p.page_log2) - held, 0) : 0;
-        const int need_upto = block_sums(need, scratch[1]), mine = capped(taken, need_upto - need);
-        item_at[tid] = need_upto;
+        int need_upto[1] = {need};
+        block_sums<1, THREADS>(need_upto, scratch1);
+        upto[tid] = end;
+        taken_upto[tid] = need_upto[0];
+        back_upto[tid] = sum[1];
+        held_of[tid] = held;
+        ahead[tid] = before;
+        next[tid] = position;
+        if (with_parents && one_turn)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                parents[tid + THREADS * i] = parent[i];
+        __syncthreads();
+        const int all_tokens = upto[THREADS - 1], pages = taken_upto[THREADS - 1];
+        if (one_turn && back_upto[THREADS - 1] > 0) {
+            back = back_upto[THREADS - 1];
+            give_back(0, free0, back);
+            __syncthreads();
+        }
+        const int have = min(free0 + min(back, p.pages), p.pages);
         if (b < p.seqs) {
             p.q_start[b] = first;
             p.seq_len[b] = len;
-            p.a.held_out[b] = open ? held + min(max(have - mine, 0), need) : 0;
+            p.a.held_out[b] = open ? held + min(max(have - capped(taken, need_upto[0] - need), 0), need) : 0;
         }
-        __syncthreads();
-        const int pages = item_at[PLAN_THREADS - 1];
-        for (int k = tid; k < pages; k += PLAN_THREADS) {
-            const int s = find_above(item_at, PLAN_THREADS, k), j = k - (s > 0 ? item_at[s - 1] : 0), at = have - 1 - capped(taken, k);
-            if (held_of[s] + j < p.table_stride)
-                p.table[(size_t)(c0 + s) * p.table_stride + held_of[s] + j] = at >= 0 ? p.a.free_pages[at] : -1;
+        for (int k0 = tid; k0 < pages; k0 += 4 * THREADS) {
+            int k[4], s[4], page[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                k[i] = min(k0 + THREADS * i, pages - 1);
+            find_above(taken_upto, seqs, k, s);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = have - 1 - capped(taken, k[i]);
+                page[i] = at >= 0 ? p.a.free_pages[at] : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int column = held_of[s[i]] + k[i] - (s[i] > 0 ? taken_upto[s[i] - 1] : 0);
+                if (k0 + THREADS * i < pages && column < p.table_stride)
+                    p.table[(size_t)(c0 + s[i]) * p.table_stride + column] = page[i];
+            }
         }
         if (with_tokens) {
             const int count = all_tokens - tokens;
-            if (p.a.parents)
-                for (int k = tid; k < count; k += PLAN_THREADS)
+            if (with_parents && !one_turn) {
+                for (int k = tid; k < count; k += THREADS)
                     parents[k] = p.a.parents[tokens + k];
-            __syncthreads();
+                __syncthreads();
+            }
             const int words = p.a.mask_words > 1 ? p.a.mask_words : 1;
-            for (int k = tid; k < count * words; k += PLAN_THREADS) {
+            for (int k = tid; k < count * words; k += THREADS) {
                 const int m = words > 1 ? k / words : k, word = k - m * words;
-                const int s = find_above(upto, PLAN_THREADS, tokens + m), first_of = s > 0 ? upto[s - 1] : tokens, i = tokens + m - first_of;
+                const int item[1] = {tokens + m};
+                int at[1];
+                find_above(upto, seqs, item, at);
+                const int s = at[0], first_of = s > 0 ? upto[s - 1] : tokens, i = tokens + m - first_of;
+                int page = -1, t = 0;
+                if (word == 0) { // its page: one that the sequence had, or the one that it gets above, from where that comes
+                    t = ahead[s] + i;
+                    const int column = t >> p.page_log2, mine = capped(taken, s > 0 ? taken_upto[s - 1] : 0), top = have - 1 - (mine + column - held_of[s]);
+                    const int *from = column < held_of[s] ? p.table + (size_t)(c0 + s) * p.table_stride + column : top >= 0 ? p.a.free_pages + top : nullptr;
+                    page = from ? *from : -1;
+                }
                 int depth = i;
                 if (p.a.parents) {
                     const uint64_t bits = ancestors(parents + (first_of - tokens), i, word, &depth);
@@ -174,21 +239,22 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(PlanArgs p, int with
                 }
                 if (word == 0) {
                     p.a.positions[tokens + m] = next[s] + depth;
-                    p.a.slots[tokens + m] = slot_of(p, c0 + s, ahead[s] + i);
+                    p.a.slots[tokens + m] = page < 0 || page >= p.pages ? -1 : (page << p.page_log2) | (t & ((1 << p.page_log2) - 1));
                 }
             }
         }
         tokens = all_tokens;
         taken = capped(taken, pages);
-        __syncthreads();
-    }
-    if (tid == 0) {
-        p.q_start[p.seqs] = tokens;
-        p.a.free_out[0] = max(have - taken, 0);
-        p.a.lacking[0] = max(taken - have, 0);
+        if (c0 + THREADS >= p.seqs && tid == 0) {
+            p.q_start[p.seqs] = tokens;
+            p.a.free_out[0] = max(have - taken, 0);
+            p.a.lacking[0] = max(taken - have, 0);
+        }
+        if (!one_turn)
+            __syncthreads();
     }
     if (with_tokens)
-        clear_rows(p, tokens, tid, PLAN_THREADS);
+        clear_rows(p, tokens, tid, THREADS);
 }
 
 // The tokens of many: a workgroup for 1024 tokens of a sequence, or for all nodes of a tree; the last one for what is behind the tokens.
@@ -354,8 +420,12 @@ int fq_launch_paged_plan(const fq_paged_batch &b, const fq_plan_arrays &a, fq_st
     const PagedSeqs s = paged_seqs(b);
     PlanArgs p{const_cast<int *>(b.q_start), const_cast<int *>(b.seq_len), const_cast<int *>(b.table), a, b.seqs, b.tokens, b.max_q, b.max_len,
                b.table_stride, s.page_log2, b.pages};
-    const int with_tokens = (long long)b.tokens * (a.mask_words > 1 ? a.mask_words : 1) <= PLAN_TOKENS;
-    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p, with_tokens);
+    const long long rows = (long long)b.tokens * (a.mask_words > 1 ? a.mask_words : 1);
+    const int with_tokens = rows <= (a.parents ? 1024 : PLAN_TOKENS);
+    if (b.seqs <= 256 && (rows <= 1024 || !with_tokens))
+        hipLaunchKernelGGL(plan_kernel<256>, dim3(1), dim3(256), 0, st, p, with_tokens);
+    else
+        hipLaunchKernelGGL(plan_kernel<PLAN_THREADS>, dim3(1), dim3(PLAN_THREADS), 0, st, p, with_tokens);
     int rc = (int)hipGetLastError();
     if (rc != 0 || with_tokens)
         return rc;
