@@ -1211,7 +1211,7 @@ struct AttnPlan {
 // Trees of more than sixteen rows: an estimate of their own, as their wavefronts without rows are idle and their splits that there are come first.  Rows and
 // positions are those that the caller states, or sequences half as long as the longest; a sequence's last tile is taken to be half full, and a tile costs by 32
 // rows that it has and by itself.  Over 46 calls of 3 to 150 nodes and 20 to 30000 positions its choice takes 2.7 % longer than the best of both heights and up
-// to fifteen lengths (fitted to half of them 3 to 6 % on the others), that for chunks 9 %: 12 sequences of up to 46 nodes of 40 heads, 8 key/value heads
+// to fifteen lengths (fitted to half of them 3 to 5 % on the others), that for chunks 9 %: 12 sequences of up to 46 nodes of 40 heads, 8 key/value heads
 // and 2539 positions 36 -> 27 us.
 void plan_tree(const fq_paged_batch &b, int heads, int kv_heads, int *rows_out, int *chunk_out)
 {
@@ -1219,18 +1219,18 @@ void plan_tree(const fq_paged_batch &b, int heads, int kv_heads, int *rows_out, 
     const bool known = b.positions > 0 && b.pairs > 0;
     const double tokens = b.tokens, positions = known ? (double)b.positions : b.seqs > 1 ? 0.5 * b.seqs * b.max_len + 1 : b.max_len + 1.0;
     const double pairs = known ? (double)b.pairs : tokens * positions / b.seqs, seen_rows = pairs * group / positions; // of a sequence, as a position sees them
-    const double items = tokens * heads, slow = b.page < KT ? 1.96 : 1.0; // four pages a tile to look up
+    const double items = tokens * heads, slow = b.page < KT ? 1.2 : 1.0; // four pages a tile to look up
     double best = 0;
     for (int rows = 64; rows <= 128; rows *= 2)
         for (int chunk = 128;; chunk += chunk < 768 ? 128 : chunk < 1536 ? 256 : chunk < 2048 ? 512 : chunk) {
             const int splits = (b.max_len + chunk - 1) / chunk;
             const double tiles = seen_rows / rows + 0.5 > 1 ? seen_rows / rows + 0.5 : 1, units = seen_rows / 32 + 0.5 > 1 ? seen_rows / 32 + 0.5 : 1;
-            const double length = chunk < b.max_len + KT ? chunk : b.max_len + KT, alone = length / KT * (rows == 64 ? 0.65 : 0.77) * slow;
-            const double together = kv_heads / 256.0 * positions / KT * (tiles * (rows == 64 ? 0.35 : 0.16) + units * 0.43) * slow;
+            const double length = chunk < b.max_len + KT ? chunk : b.max_len + KT, alone = length / KT * (rows == 64 ? 0.73 : 0.77) * slow;
+            const double together = kv_heads / 256.0 * positions / KT * (tiles * (rows == 64 ? 0.2 : 0.1) + units * 0.31) * slow;
             const double all = items * splits, longer = pairs * heads / chunk + items, parts = longer < all ? longer : all;
             const double full = tokens * group / rows + (b.seqs < tokens * group ? b.seqs : tokens * group);
-            const double us = 9.2 + (alone > together ? alone + 0.28 * together : together + 0.28 * alone) + 0.001 * full * kv_heads * splits +
-                              (splits > 1 ? 5.6 + 260e-6 * parts : 0) + (splits > 8 ? 0.7 : 0);
+            const double us = 6 + (alone > together ? alone + 0.14 * together : together + 0.14 * alone) + 0.0013 * full * kv_heads * splits +
+                              (splits > 1 ? 3.4 + 210e-6 * parts : 0) + (splits > 8 ? 0.6 : 0);
             if ((best == 0 || us < best) && (splits == 1 || all <= 1 << 20)) {
                 best = us;
                 *rows_out = rows;
