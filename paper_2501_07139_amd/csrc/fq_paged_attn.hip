@@ -57,6 +57,7 @@ __device__ __forceinline__ uint64_t mask_window(const uint64_t *row, int words, 
 struct RowTile {
     SeqRange s;
     int b, row0, rows, seen; // first row, rows of the sequence and head, positions that the tile's last row sees
+    int older;               // positions ahead of the tokens (may be negative), with TREE ahead of the tail
 };
 
 // Tile `tile` of TR rows, counted over the sequences; rows < 0 where there is none.  Every wavefront scans the sequences' tile counts.
@@ -71,9 +72,11 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile, i
     r.rows = -1;
     int base = 0;
     for (int i = 0; i < p.s.seqs; i += 64) {
-        int count = 0;
+        int count = 0, older = 0;
+        SeqRange s = {0, 0, 0};
         if (i + lane < p.s.seqs) {
-            const SeqRange s = seq_range(p.s, i + lane);
+            s = seq_range(p.s, i + lane);
+            older = TREE ? ahead_of_tail(p, s, i + lane) : s.len - s.n;
             count = (s.n * p.group + TR - 1) / TR;
             if (packed)
                 count *= max((s.len + p.chunk - 1) / p.chunk, 1);
@@ -89,7 +92,10 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs &p, int tile, i
             const int at = __builtin_ctzll(behind);
             r.b = i + at;
             int mine = tile - base - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(count, at));
-            r.s = seq_range(p.s, r.b);
+            r.s.first = __builtin_amdgcn_readlane(s.first, at); // not loaded again: a tile waits for fewer loads in turn
+            r.s.n = __builtin_amdgcn_readlane(s.n, at);
+            r.s.len = __builtin_amdgcn_readlane(s.len, at);
+            r.older = __builtin_amdgcn_readlane(older, at);
             r.rows = r.s.n * p.group;
             if (packed) {
                 const int tiles = (r.rows + TR - 1) / TR;
@@ -444,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(PagedAttnArgs p
     const int kpart = wave % KS, qpart = wave / KS;
     const int row0 = tile.row0 + 32 * qpart; // first row of the wavefront
     const int row = row0 + col, rowc = min(row, tile.rows - 1), token = rowc / p.group, head = kvh * p.group + rowc - token * p.group;
-    const int older = TREE ? ahead_of_tail(p, tile.s, tile.b) : tile.s.len - tile.s.n; // positions ahead of the tokens (may be negative) or of the tail
+    const int older = tile.older;
     const int seen = min(older + token + 1, tile.s.len);                               // positions this lane's row sees (not with TREE)
     const int all_seen = TREE ? older : older + min(row0, tile.rows - 1) / p.group + 1; // ... that every row of the wavefront sees
     const int any_seen = TREE ? tile.s.len : older + min(row0 + 31, tile.rows - 1) / p.group + 1;
