@@ -539,7 +539,7 @@ int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void 
  * a token ahead of it, -1 for instance, makes it a root) positions = next_position[b] + its depth, and mask (or NULL), uint64
  * [tokens][mask_words], has its own bit and those of its ancestors; max_q at most 64 mask_words then, and 64 FQ_TREE_WORDS without a mask.  Rows of
  * positions, slots and mask behind the last token: 0, -1, 0.
- * batch: its sizes are the bounds; its arrays q_start, seq_len and table (all columns; those behind what is held are written as pages are
+ * batch: its sizes are the bounds (tokens below 2^28); its arrays q_start, seq_len and table (all columns; those behind what is held are written as pages are
  * taken) are the output.  free_pages int32 [pages], of which the first free_count[0] are free; free_out[0] of them are free afterwards.
  * lacking[0]: pages that the stack did not have; held_out counts those that a sequence has, and the table has -1 for the others.
  * In place: cached may be seq_len, held held_out, free_count free_out; no output may overlap an input or another otherwise.

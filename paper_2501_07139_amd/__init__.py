@@ -717,7 +717,7 @@ class PagedBatch:
         mask_words, `mask` int64 [tokens, mask_words] takes the masks of drafted trees."""
         if page not in PAGE_SIZES or not 0 < pages <= (2 ** 31 - 1) // page:
             raise FqError(-2, f"PagedBatch.reserve: {pages} pages of {page} positions (pages of {PAGE_SIZES}, 2^31 - 1 positions at most)")
-        if not 1 <= seqs <= 65535 or not 0 <= max_q <= tokens <= seqs * max_q or tokens >= 1 << 29 or not 1 <= max_len <= 1 << 24:
+        if not 1 <= seqs <= 65535 or not 0 <= max_q <= tokens <= seqs * max_q or tokens >= 1 << 28 or not 1 <= max_len <= 1 << 24:
             raise FqError(-2, f"PagedBatch.reserve: {seqs} sequences, {tokens} tokens, at most {max_q} of one, {max_len} positions")
         if not 0 <= mask_words <= TREE_WORDS or (mask_words and max_q > 64 * mask_words):
             raise FqError(-2, f"PagedBatch.reserve: {mask_words} words of masks (at most {TREE_WORDS}) for {max_q} tokens of a sequence")

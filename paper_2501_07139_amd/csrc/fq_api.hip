@@ -959,8 +959,8 @@ extern "C" int fq_paged_plan(const fq_paged_batch *batch, const int32_t *new_tok
         return rc;
     if (!new_tokens || !cached || !held || !held_out || !free_pages || !free_count || !free_out || !lacking || (batch->tokens > 0 && (!positions || !slots)))
         return fq_fail(FQ_ERR_NULL, "%s: NULL argument", fn);
-    if (batch->tokens >= 1 << 29)
-        return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d (below 2^29)", fn, batch->tokens);
+    if (batch->tokens >= 1 << 28)
+        return fq_fail(FQ_ERR_SHAPE, "%s: tokens=%d (below 2^28)", fn, batch->tokens);
     if (mask && !parents)
         return fq_fail(FQ_ERR_NULL, "%s: a mask without parents", fn);
     if (mask ? mask_words <= 0 || mask_words > FQ_TREE_WORDS || batch->max_q > 64 * mask_words : mask_words != 0)

@@ -52,20 +52,14 @@ __device__ __forceinline__ void block_sums(int (&x)[N], int (&scratch)[N][THREAD
     }
 }
 
-// The first of `count` entries of rising sums that is above k[i], which is below the last one; several at a time, as each step waits for the one before.
-template <int N>
-__device__ __forceinline__ void find_above(const int *upto, int count, const int (&k)[N], int (&at)[N])
+// The first of `count` entries of rising sums that is above k, which is below the last one.
+__device__ __forceinline__ int find_above(const int *upto, int count, int k)
 {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        at[i] = 0;
+    int at = 0;
+#pragma unroll 1
     for (int step = 1 << (31 - __builtin_clz(max(count, 1))); step > 0; step >>= 1) // entries ahead of `at` are not above
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            at[i] += at[i] + step <= count && upto[at[i] + step - 1] <= k[i] ? step : 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        at[i] = min(at[i], count - 1);
+        at += at + step <= count && upto[at + step - 1] <= k ? step : 0;
+    return min(at, count - 1);
 }
 
 // Page and place of position t of sequence b, as a slot; -1 where it has no page.
@@ -122,13 +116,11 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(PlanArgs p, int with_toke
 
     // Pages that closed sequences give back go on the stack, from place `from` on.
     const auto give_back = [&](int c0, int from, int total) {
+#pragma unroll 1
         for (int k = tid; k < total; k += THREADS) {
-            const int item[1] = {k};
-            int s[1];
-            find_above(back_upto, THREADS, item, s);
-            const int j = k - (s[0] > 0 ? back_upto[s[0] - 1] : 0);
+            const int s = find_above(back_upto, min(p.seqs - c0, THREADS), k), j = k - (s > 0 ? back_upto[s - 1] : 0);
             if (from + k < p.pages)
-                p.a.free_pages[from + k] = p.table[(size_t)(c0 + s[0]) * p.table_stride + j];
+                p.a.free_pages[from + k] = p.table[(size_t)(c0 + s) * p.table_stride + j];
         }
     };
     int back = 0; // of all sequences; more than one turn of them: all are looked at ahead of the rest
@@ -192,23 +184,11 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(PlanArgs p, int with_toke
             p.seq_len[b] = len;
             p.a.held_out[b] = open ? held + min(max(have - capped(taken, need_upto[0] - need), 0), need) : 0;
         }
-        for (int k0 = tid; k0 < pages; k0 += 4 * THREADS) {
-            int k[4], s[4], page[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                k[i] = min(k0 + THREADS * i, pages - 1);
-            find_above(taken_upto, seqs, k, s);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = have - 1 - capped(taken, k[i]);
-                page[i] = at >= 0 ? p.a.free_pages[at] : -1;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int column = held_of[s[i]] + k[i] - (s[i] > 0 ? taken_upto[s[i] - 1] : 0);
-                if (k0 + THREADS * i < pages && column < p.table_stride)
-                    p.table[(size_t)(c0 + s[i]) * p.table_stride + column] = page[i];
-            }
+#pragma unroll 1
+        for (int k = tid; k < pages; k += THREADS) {
+            const int s = find_above(taken_upto, seqs, k), at = have - 1 - capped(taken, k), column = held_of[s] + k - (s > 0 ? taken_upto[s - 1] : 0);
+            if (column < p.table_stride)
+                p.table[(size_t)(c0 + s) * p.table_stride + column] = at >= 0 ? p.a.free_pages[at] : -1;
         }
         if (with_tokens) {
             const int count = all_tokens - tokens;
@@ -218,12 +198,10 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(PlanArgs p, int with_toke
                 __syncthreads();
             }
             const int words = p.a.mask_words > 1 ? p.a.mask_words : 1;
+#pragma unroll 1
             for (int k = tid; k < count * words; k += THREADS) {
                 const int m = words > 1 ? k / words : k, word = k - m * words;
-                const int item[1] = {tokens + m};
-                int at[1];
-                find_above(upto, seqs, item, at);
-                const int s = at[0], first_of = s > 0 ? upto[s - 1] : tokens, i = tokens + m - first_of;
+                const int s = find_above(upto, seqs, tokens + m), first_of = s > 0 ? upto[s - 1] : tokens, i = tokens + m - first_of;
                 int page = -1, t = 0;
                 if (word == 0) { // its page: one that the sequence had, or the one that it gets above, from where that comes
                     t = ahead[s] + i;

@@ -260,7 +260,8 @@ def plan_case(rng, seqs, page, new_max, cached_max, closed, lack=0, tree=False):
     (7, 16, 90, 50, 0, 9, False), (64, 16, 30, 200, 0.2, 40, False), (1500, 16, 3, 60, 0.2, 0, False), (2100, 32, 2, 500, 0.1, 100, False),
     (20, 256, 2000, 3000, 0.1, 0, False), (1100, 16, 40, 300, 0.2, 50, False), (1, 16, 9, 20, 0, 0, True), (6, 16, 64, 90, 0.2, 0, True),
     (50, 64, 33, 300, 0.2, 5, True), (9, 16, 200, 40, 0, 0, True), (300, 16, 50, 40, 0.1, 0, True), (1030, 32, 12, 40, 0.1, 0, True),
-    (3, 16, 1500, 100, 0, 0, True)], ids=str)
+    (3, 16, 1500, 100, 0, 0, True), (2, 64, 30000, 100, 0, 0, False), (3000, 16, 10, 60, 0.3, 50, False), (300, 16, 200, 300, 0.3, 0, False),
+    (5000, 256, 9, 700, 0.2, 700, False)], ids=str)
 def test_plan(fq, torch, seqs, page, new_max, cached_max, closed, lack, tree):
     rng = np.random.default_rng(seqs + page + new_max)
     for given_position in (False, True):

@@ -28,7 +28,7 @@ def plan(b, **c):
     (-1, {"pages": None}, {}), (-1, {"count": None}, {}), (-1, {"count_out": None}, {}), (-1, {"lacking": None}, {}), (-1, {"positions": None}, {}),
     (-1, {"slots": None}, {}), (-1, {"mask": 0x20000, "words": 1}, {}), (-2, {"words": 1}, {}), (-2, {"parents": 0x18000, "mask": 0x20000}, {}),
     (-2, {"parents": 0x18000, "mask": 0x20000, "words": 65}, {}), (-2, {"parents": 0x18000, "mask": 0x20000, "words": 1}, {"tokens": 70, "max_q": 65}),
-    (-2, {"parents": 0x18000}, {"tokens": 5000, "max_q": 4097}), (-2, {}, {"tokens": 1 << 29, "max_q": 1 << 28}), (-2, {}, {"max_q": 2}),
+    (-2, {"parents": 0x18000}, {"tokens": 5000, "max_q": 4097}), (-2, {}, {"tokens": 1 << 28, "max_q": 1 << 27}), (-2, {}, {"max_q": 2}),
     (-2, {}, {"max_len": 129}), (-2, {}, {"page": 24}), (-2, {}, {"seqs": 0}), (-5, {"parents": 0x18000, "mask": 0x20004, "words": 1}, {}),
     (-2, {"next": 0x110000}, {}), (-2, {"new": 0x110004}, {}), (-2, {"cached": 0x110004}, {}), (-2, {"held_out": 0x12004}, {}), (-2, {"positions": 0x17000}, {}),
     (-2, {"lacking": 0x14000}, {}), (-2, {"positions": 0x100004}, {}), (-2, {"parents": 0x16000}, {}), (-2, {"slots": 0x120000 + 60}, {})], ids=str)
