@@ -569,7 +569,7 @@ int fq_attn_tree(const fq_paged_batch *batch, const uint64_t *mask, int mask_wor
  * the path there is -1.  The tail is the tokens of the call then, and `tail` NULL.
  * With none of the three, path and accepted are read (the beam that won, for instance; accepted is cut to path_stride and to the tail, a node
  * below its place in the path is taken for that place, one behind the tail for its last), bonus NULL; tail as in fq_attn_tree.
- * Outputs overlap neither inputs (new_len is not seq_len) nor each other.
+ * Outputs overlap neither inputs (new_len is not seq_len) nor each other.  layers * n_kv_heads * seqs below 2^24.
  */
 int fq_tree_commit(const fq_paged_batch *batch, const int32_t *tail, const int32_t *parents, const int32_t *drafted, const int32_t *following,
                    void *k_pages, void *v_pages, int layers, int n_kv_heads, int32_t *path, int path_stride, int32_t *accepted,
@@ -586,7 +586,7 @@ int fq_tree_commit(const fq_paged_batch *batch, const int32_t *tail, const int32
  * parent, token int32 [requests][width], scores_out fp32, done_out int32 (or NULL): done[parent], or token is eos (eos < 0: no token is).
  * mask_out (or NULL) uint64 [requests][width][mask_words] = mask [requests][beams][mask_words] (NULL: zeros) of the parent, and bit tail[request]
  * (NULL: 0) + place, the node that the beam's token will be: with it the beams are a tree for fq_attn_tree, and nothing of the cache moves.
- * beams and width 1 to 64, vocab up to 2^18, requests * beams below 2^24.  workspace: fq_beam_step_workspace_bytes bytes, 16-byte aligned.
+ * beams and width 1 to 64, vocab up to 2^18, requests * beams * (vocab / 8192, rounded up) below 2^24.  workspace: fq_beam_step_workspace_bytes bytes, 16-byte aligned.
  * Outputs and workspace overlap neither inputs nor each other.
  */
 size_t fq_beam_step_workspace_bytes(int requests, int beams, int vocab, int width);

@@ -1046,8 +1046,8 @@ extern "C" int fq_tree_commit(const fq_paged_batch *batch, const int32_t *tail, 
         return fq_fail(FQ_ERR_NULL, "%s: parents, drafted and following go together", fn);
     if (walk ? tail != nullptr : bonus != nullptr)
         return fq_fail(FQ_ERR_SHAPE, walk ? "%s: the tail of a tree that is checked is the tokens of the call" : "%s: bonus without a tree to check", fn);
-    if (layers <= 0 || layers > 65535 || (long long)layers * n_kv_heads * batch->seqs >= 1 << 25 || path_stride <= 0 || path_stride > 1 << 24)
-        return fq_fail(FQ_ERR_SHAPE, "%s: layers=%d n_kv_heads=%d seqs=%d path_stride=%d (product of the first three below 2^25)", fn, layers, n_kv_heads,
+    if (layers <= 0 || layers > 65535 || (long long)layers * n_kv_heads * batch->seqs >= 1 << 24 || path_stride <= 0 || path_stride > 1 << 24)
+        return fq_fail(FQ_ERR_SHAPE, "%s: layers=%d n_kv_heads=%d seqs=%d path_stride=%d (product of the first three below 2^24)", fn, layers, n_kv_heads,
                        batch->seqs, path_stride);
     if (!aligned16(k_pages) || !aligned16(v_pages))
         return fq_fail(FQ_ERR_ALIGN, "%s: pools must be 16-byte aligned", fn);
@@ -1076,9 +1076,10 @@ namespace {
 
 int check_beams(const char *fn, int requests, int beams, int vocab, int width)
 {
-    if (requests <= 0 || beams <= 0 || beams > 64 || width <= 0 || width > 64 || vocab <= 0 || vocab > 1 << 18 || (long long)requests * beams >= 1 << 24)
-        return fq_fail(FQ_ERR_SHAPE, "%s: requests=%d beams=%d vocab=%d width=%d (beams and width 1 to 64, vocab up to 2^18, requests * beams below 2^24)",
-                       fn, requests, beams, vocab, width);
+    if (requests <= 0 || beams <= 0 || beams > 64 || width <= 0 || width > 64 || vocab <= 0 || vocab > 1 << 18 ||
+        (long long)requests * beams * ((vocab + 8191) / 8192) >= 1 << 24) // a grid has less than 2^32 threads
+        return fq_fail(FQ_ERR_SHAPE, "%s: requests=%d beams=%d vocab=%d width=%d (beams and width 1 to 64, vocab up to 2^18, requests * beams for each 8192 "
+                       "of it below 2^24)", fn, requests, beams, vocab, width);
     return FQ_OK;
 }
 

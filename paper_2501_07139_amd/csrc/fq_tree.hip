@@ -247,10 +247,11 @@ __global__ __launch_bounds__(256) void plan_tokens_kernel(PlanArgs p)
     const int first = p.q_start[b], n = p.q_start[b + 1] - first, older = p.seq_len[b] - n;
     const int position = p.a.next_position ? p.a.next_position[b] : older;
     if (!p.a.parents) {
-        for (int i = blockIdx.y * 1024 + tid; i < min(n, (int)blockIdx.y * 1024 + 1024); i += 256) {
-            p.a.positions[first + i] = position + i;
-            p.a.slots[first + i] = slot_of(p, b, older + i);
-        }
+        for (int i0 = blockIdx.y * 1024; i0 < n; i0 += gridDim.y * 1024)
+            for (int i = i0 + tid; i < min(n, i0 + 1024); i += 256) {
+                p.a.positions[first + i] = position + i;
+                p.a.slots[first + i] = slot_of(p, b, older + i);
+            }
         return;
     }
     for (int i = tid; i < n; i += 256)
@@ -404,10 +405,11 @@ int fq_launch_paged_plan(const fq_paged_batch &b, const fq_plan_arrays &a, fq_st
         hipLaunchKernelGGL(plan_kernel<256>, dim3(1), dim3(256), 0, st, p, with_tokens);
     else
         hipLaunchKernelGGL(plan_kernel<PLAN_THREADS>, dim3(1), dim3(PLAN_THREADS), 0, st, p, with_tokens);
+    const int parts = (b.max_q + 1023) / 1024, most = (1 << 22) / (b.seqs + 1); // of a sequence's tokens; workgroups that a grid has room for
     int rc = (int)hipGetLastError();
     if (rc != 0 || with_tokens)
         return rc;
-    hipLaunchKernelGGL(plan_tokens_kernel, dim3(b.seqs + 1, a.parents ? 1 : (b.max_q + 1023) / 1024), dim3(256), 0, st, p);
+    hipLaunchKernelGGL(plan_tokens_kernel, dim3(b.seqs + 1, a.parents ? 1 : parts < most ? parts : most), dim3(256), 0, st, p);
     return (int)hipGetLastError();
 }
 

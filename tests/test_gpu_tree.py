@@ -143,6 +143,18 @@ def test_long_sequences_are_split(fq, torch, heads, kv, page, n, S):
     attend(fq, torch, rng, seqs, heads, kv, page, 2, ["tree", "tree"])
 
 
+@pytest.mark.parametrize("heads, kv, page, most", [(8, 2, 16, 900), (4, 4, 64, 300), (8, 1, 32, 2500)])
+def test_many_sequences(fq, torch, heads, kv, page, most):
+    # more sequences than a wavefront has lanes, some without tokens, their lengths from none to many splits
+    rng = np.random.default_rng(most)
+    seqs = []
+    for i in range(83):
+        n = int(rng.integers(0, 22)) if i % 7 else 0
+        tail = n + (int(rng.integers(0, 60)) if i % 3 else 0)
+        seqs.append((n, tail, max(tail, int(rng.integers(0, most if i % 9 == 0 else 60)))))
+    attend(fq, torch, rng, seqs, heads, kv, page, 2, ["tree" if n == t else "beams" for n, t, _ in seqs])
+
+
 def test_rows_that_see_nothing_are_zero(fq, torch):
     rng = np.random.default_rng(4)
     attend(fq, torch, rng, [(5, 70, 70), (3, 3, 3), (2, 0, 0)], 8, 2, 16, 2, ["none", "none", "all"])
@@ -389,6 +401,26 @@ def test_commit_of_given_paths(fq, torch, page, layers):
         for l in range(layers):
             ref.keep(k[l], table[i], lengths[i] - tails[i], p, page)
             ref.keep(v[l], table[i], lengths[i] - tails[i], p, page)
+    assert np.array_equal(dk.cpu().numpy(), k) and np.array_equal(dv.cpu().numpy(), v)
+
+
+def test_commit_of_a_path_through_a_long_tail(fq, torch):
+    """More pages than a wavefront has lanes behind the tail's first, and a path of more than two of its turns."""
+    rng = np.random.default_rng(77)
+    S, tail, page = 2101, 2050, 16
+    table, pages = deal(rng, [S, 33], page)
+    k, v = (rng.normal(size=(1, pages, 3, page, 128)).astype(np.float16) for _ in range(2))
+    given = sorted(rng.choice(tail, 150, replace=False).tolist())
+    paths = np.full((2, 150), -1, dtype=np.int32)
+    paths[0], paths[1, :2] = given, [1, 3]
+    b = fq.PagedBatch([3, 1], [S, 33], table, page, pages)
+    dk, dv = dev(torch, k), dev(torch, v)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    got = fq.fq_tree_commit(b, dk, dv, tail=ints(tail, 5), path=dev(torch, paths), accepted=ints(150, 2))
+    assert got[3].tolist() == [S - tail + 150, 30]
+    for pool in (k, v):
+        ref.keep(pool[0], table[0], S - tail, given, page)
+        ref.keep(pool[0], table[1], 28, [1, 3], page)
     assert np.array_equal(dk.cpu().numpy(), k) and np.array_equal(dv.cpu().numpy(), v)
 
 

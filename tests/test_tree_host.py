@@ -74,7 +74,7 @@ PATH = {"parents": None, "drafted": None, "following": None, "bonus": None}
 @pytest.mark.parametrize("code, call, changes", [
     (-1, {}, None), (-1, {}, {"seq_len": None}), (-1, {"k": None}, {}), (-1, {"v": None}, {}), (-1, {"path": None}, {}), (-1, {"accepted": None}, {}),
     (-1, {"new_len": None}, {}), (-1, {"parents": None}, {}), (-1, {"drafted": None}, {}), (-1, {"following": None}, {}), (-2, {"tail": 0x4000}, {}),
-    (-2, dict(PATH, bonus=0x12000), {}), (-2, {"layers": 0}, {}), (-2, {"layers": 65536}, {}), (-2, {"layers": 60000, "kv": 1000}, {}), (-2, {"kv": 0}, {}),
+    (-2, dict(PATH, bonus=0x12000), {}), (-2, {"layers": 0}, {}), (-2, {"layers": 65536}, {}), (-2, {"layers": 60000, "kv": 1000}, {}), (-2, {"layers": 1 << 15, "kv": 256}, {}), (-2, {"kv": 0}, {}),
     (-2, {"stride": 0}, {}), (-2, {}, {"page": 24}), (-5, {"k": (1 << 24) + 8}, {}), (-5, {"v": (1 << 28) + 8}, {}), (-2, {"v": (1 << 24) + 4096}, {}),
     (-2, {"new_len": 0x110000}, {}), (-2, {"new_len": 0x11004}, {}), (-2, {"path": 0x1000 - 8}, {}), (-2, {"bonus": 0x3000}, {}),
     (-2, dict(PATH, tail=0x13004), {}), (-2, {"accepted": 0x120010}, {})], ids=str)
@@ -94,7 +94,7 @@ def beam(**c):
 @pytest.mark.parametrize("code, call", [
     (-1, {"logits": None}), (-1, {"scores": None}), (-1, {"parent": None}), (-1, {"token": None}), (-1, {"out": None}), (-2, {"requests": 0}), (-2, {"beams": 0}),
     (-2, {"beams": 65}), (-2, {"width": 0}), (-2, {"width": 65}), (-2, {"vocab": 0}), (-2, {"vocab": (1 << 18) + 1, "ld": 1 << 19}),
-    (-2, {"requests": 1 << 23}), (-2, {"ld": 999}), (-2, {"ld": (1 << 32) + 1}), (-2, {"eos": 1000}), (-2, {"done": 0x5000}), (-2, {"mask": 0x6000}),
+    (-2, {"requests": 1 << 23}), (-2, {"requests": 1 << 19, "beams": 1, "vocab": 1 << 18, "ld": 1 << 18}), (-2, {"ld": 999}), (-2, {"ld": (1 << 32) + 1}), (-2, {"eos": 1000}), (-2, {"done": 0x5000}), (-2, {"mask": 0x6000}),
     (-2, {"words": 1}), (-2, {"mask_out": 0x7000}), (-2, {"mask_out": 0x7000, "words": 65}), (-6, {"ws": None}), (-6, {"bytes": 100}),
     (-5, {"ws": (1 << 30) + 8}), (-5, {"logits": (1 << 24) + 1}), (-5, {"mask_out": 0x7004, "words": 1}), (-2, {"parent": 0x3000}), (-2, {"out": 0x1000}),
     (-2, {"done": 0x2000, "eos": 3}), (-2, {"mask": 0x6000, "mask_out": 0x6010, "words": 1}), (-2, {"ws": (1 << 24) + 4096}), (-2, {"tail": 0x4000})], ids=str)
