@@ -815,7 +815,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void attn_paged_merge_ker
 // The same for trees, whose rows have all splits of their sequence.  Half a wavefront has four dimensions a lane and asks for all it needs of eight splits at
 // once.  A workgroup has eight heads of a token, one each half wavefront; or with SPREAD, where there are many splits for the jobs, one head, and they deal the
 // splits.  Jobs are counted over the sequences that have several splits, and a grid of 1024 workgroups takes them in turn: to start a workgroup takes an XCD about
-// 20 clocks (704 tokens of 40 heads, 178 of them with up to 4 splits: 10.6 us with a wavefront for each head of each token, 8.7 with a workgroup for each eight).
+// 20 clocks (704 tokens of 40 heads, 178 of them with up to 4 splits: 10.6 us with a wavefront for each head of each token, 8.7 with a workgroup for each eight, so 6.0).
 template <bool SPREAD>
 __global__ __launch_bounds__(256) void attn_tree_merge_kernel(PagedAttnArgs p)
 {

@@ -8,10 +8,11 @@ namespace {
 // From lengths to the arrays of a batch.  With f pages on the stack of free ones, R given back by closed sequences and t_b taken by sequence b:
 //   stack' = stack ++ pages of closed sequences, in order;    page j that sequence b takes = stack'[f + R - 1 - (t_0 + .. + t_(b-1) + j)],
 // so that everything is prefix sums over the sequences and then work on items (pages, tokens) that find their sequence by the sums.  One workgroup does
-// the sums, and the items too where they are few: such a call is a launch and the loads that wait for each other (what the sequences have, then free pages
-// and tables), so all inputs are asked for at once, nothing that is written is read again, and few sequences take a quarter of the threads, whose barriers
-// cost less (7 sequences of a token 5.9 -> 4.3 us, kernel 3.2).  Many tokens are left to a second launch with a workgroup for 1024 of
-// a sequence.
+// the sums, and the items too where they are few: such a call is a launch, the loads that wait for each other (what the sequences have, then free pages
+// and tables) and the code on its way to the one CU that runs it.  So all inputs are asked for at once, nothing that is written is read again, loops are
+// not unrolled (eight pages at a time in flight took 14.0 instead of 7.9 for the trees of 48 sequences), and few sequences take a quarter of the
+// threads, whose barriers cost less: 7 sequences of a token 5.9 -> 4.3 us, kernel 3.1.  The tokens of many are left to a second launch with a workgroup for 1024
+// of a sequence, and the nodes of trees to one with a workgroup a tree (301 sequences, 70000 tokens and 5000 pages 12.8: 9.3 and 3.6).
 constexpr int PLAN_THREADS = 1024;
 constexpr int PLAN_TOKENS = 8192;   // that the first launch does itself
 constexpr int TREE_NODES = 64 * 64; // of a sequence: FQ_TREE_WORDS words of 64
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(256) void plan_tokens_kernel(PlanArgs p)
 // a turn, loads ahead of stores, rows in rising order for each head.  A path rises, so node path[k] is at least k: what a turn reads lies at or behind what it
 // writes, and no later turn reads what an earlier one wrote.  No other wavefront has its heads.  Bound by the chain of loads for one sequence
 // (lengths, nodes and pages, rows), by starting workgroups and the rows' way for many (29 sequences, 32 layers of 8 heads, 26 MB: a wavefront for each head of
-// keys and of values 15.6 us).
+// keys and of values 15.6 us, so 10.8: 3.1 TB/s read and written).
 constexpr int COMMIT_ITEMS = 32; // of a turn
 
 struct CommitArgs {
