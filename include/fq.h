@@ -533,7 +533,8 @@ int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void 
  *     (its table row stays as it is), seq_len[b] = held_out[b] = 0;
  *   else it has cached[b] positions in its pages and gets n = new_tokens[b] tokens (cut to max_q, to max_len - cached[b] positions and to
  *     what is left of `tokens`): seq_len[b] = cached[b] + n, and where its held[b] pages do not hold these, pages are taken from
- *     the top of the stack, sequence after sequence, all given ones being on it first.
+ *     the top of the stack, sequence after sequence, all given ones being on it first.  It keeps what it holds until it is closed, also where
+ *     fewer positions are left of it (after a commit, say).
  * q_start[b] counts the tokens ahead.  Token i: slots = its place in the pools, or -1 where no page was left for it; positions = next_position[b]
  * (NULL: cached[b]) + i.  With parents (int32 [tokens]: of each token the one that it goes on from, counted within its sequence; what is not
  * a token ahead of it, -1 for instance, makes it a root) positions = next_position[b] + its depth, and mask (or NULL), uint64
