@@ -424,6 +424,27 @@ def test_commit_of_a_path_through_a_long_tail(fq, torch):
     assert np.array_equal(dk.cpu().numpy(), k) and np.array_equal(dv.cpu().numpy(), v)
 
 
+def test_commit_in_pools_beyond_32_bits(fq, torch):
+    """Two layers of 1.15e9 elements each: the second begins behind 2^30 of them, its last pages behind 2^31."""
+    rng = np.random.default_rng(5)
+    pages, page, kv = 70000, 16, 8
+    k, v = (torch.zeros((2, pages, kv, page, 128), dtype=torch.float16, device="cuda") for _ in range(2))
+    table = np.array([[pages - 1, 3, pages - 2]])
+    rows = rng.normal(size=(2, 2, kv, 40, 128)).astype(np.float16)  # layer, keys or values, head, position
+    for which, pool in enumerate((k, v)):
+        for t in range(40):
+            pool[:, table[0, t // page], :, t % page] = dev(torch, rows[:, which, :, t])
+    b = fq.PagedBatch([30], [40], table, page, pages)
+    path = [2, 3, 9, 28, 29]
+    fq.fq_tree_commit(b, k, v, path=dev(torch, np.array([path], dtype=np.int32)), accepted=dev(torch, np.array([5], dtype=np.int32)))
+    want = rows.copy()
+    want[:, :, :, 10:15] = rows[:, :, :, [10 + p for p in path]]
+    for which, pool in enumerate((k, v)):
+        for t in range(40):
+            assert np.array_equal(pool[:, table[0, t // page], :, t % page].cpu().numpy(), want[:, which, :, t])
+        assert pool[0].count_nonzero().item() <= 40 * kv * 128 and pool[1].count_nonzero().item() <= 40 * kv * 128
+
+
 def test_commit_without_pages_and_with_bad_paths_stays_inside(fq, torch):
     rng = np.random.default_rng(3)
     b = fq.PagedBatch([20], [50], [[3, 1, 0, 2]], 16, 5)
@@ -547,6 +568,16 @@ def test_beams_that_have_ended(fq, torch, eos):
         beam_check(fq, torch, rng, logits, scores, 8, eos=eos)
 
 
+def test_rows_of_logits_beyond_32_bits(fq, torch):
+    rng = np.random.default_rng(6)
+    beams, vocab, ld = 10, 3001, (1 << 28) + 1  # rows at odd places, the last one behind 2^31 elements
+    wide = torch.empty(9 * ld + vocab, dtype=torch.float16, device="cuda")
+    rows = torch.as_strided(wide, (beams, vocab), (ld, 1))
+    logits = rng.normal(size=(beams, vocab)).astype(np.float16)
+    rows.copy_(dev(torch, logits))
+    beam_check(fq, torch, rng, logits, (-rng.random((2, 5))).astype(np.float32), 7, rows=rows)
+
+
 def test_mask_bits_outside_the_words_are_left_out(fq, torch):
     rng = np.random.default_rng(1)
     logits = rng.normal(size=(4, 50)).astype(np.float16)
@@ -638,3 +669,64 @@ def test_a_captured_beam_step_is_replayed(fq, torch):
         want = fq.fq_beam_step(x, scores, beams)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want[:3]))
+
+
+# ------------------------------------------------------------------ refusals of the binding
+def test_what_the_binding_refuses(fq, torch):
+    """Wrong types, shapes, places and batches: nothing of it reaches a launch, with outputs given and without."""
+    z = lambda *s, t=torch.float16: torch.zeros(s, dtype=t, device="cuda")
+    ints = lambda *s: z(*s, t=torch.int32)
+    b, host = (fq.PagedBatch([1, 2], [20, 9], [[0, 1], [2, -1]], 16, 4, device=d) for d in ("cuda", "cpu"))
+    q, pool, mask = z(3, 512), z(4, 2, 16, 128), z(3, 1, t=torch.int64)
+    out = z(3, 512)
+    for more in ({}, {"out": out, "workspace": z(1 << 16, t=torch.uint8)}):
+        for args, kw in (((q, host, mask, pool, pool), {}), ((q[:2], b, mask, pool, pool), {}), ((z(3, 300), b, mask, pool, pool), {}),
+                         ((q, b, mask.int(), pool, pool), {}), ((q, b, z(2, 1, t=torch.int64), pool, pool), {}), ((q, b, z(3, 65, t=torch.int64), pool, pool), {}),
+                         ((q, b, mask, pool[:3], pool[:3]), {}), ((q, b, mask, pool.float(), pool), {}), ((q, b, mask, pool, pool), {"tail": ints(3)}),
+                         ((q, b, mask, pool, pool), {"tail": z(2, t=torch.int64)}), ((q, b, mask, pool, pool), {"lse": z(3, 3, t=torch.float32)}),
+                         ((q, b, mask.cpu(), pool, pool), {})):
+            with pytest.raises((TypeError, ValueError)):
+                fq.fq_attn_tree(*args, **kw, **more)
+    with pytest.raises(fq.FqError):
+        fq.fq_attn_tree(q, b, mask, pool, pool, out=q)
+    pools = z(2, 4, 2, 16, 128), z(2, 4, 2, 16, 128)
+    three = ints(3)
+    for more in ({}, {"path": ints(2, 3), "accepted": ints(2), "bonus": ints(2), "new_len": ints(2)}):
+        for kw in ({"parents": three, "drafted": three}, {"parents": ints(2), "drafted": three, "following": three},
+                   {"parents": three.long(), "drafted": three, "following": three}, {"parents": three, "drafted": three.cpu(), "following": three}):
+            with pytest.raises((TypeError, ValueError)):
+                fq.fq_tree_commit(b, *pools, **kw, **more)
+        with pytest.raises((TypeError, ValueError)):
+            fq.fq_tree_commit(host, *pools, three, three.clone(), three.clone(), **more)
+        with pytest.raises((TypeError, ValueError)):
+            fq.fq_tree_commit(b, pools[0][:, :3], pools[1][:, :3], three, three.clone(), three.clone(), **more)
+    with pytest.raises(ValueError):
+        fq.fq_tree_commit(b, *pools)  # neither a tree nor a path
+    with pytest.raises(fq.FqError):
+        fq.fq_tree_commit(b, *pools, three, three.clone(), three.clone(), new_len=b.seq_len)
+    with pytest.raises(fq.FqError):
+        fq.fq_tree_commit(b, pools[0], pools[0], three, three.clone(), three.clone())
+    r = fq.PagedBatch.reserve(2, 6, 4, 64, 16, 9, mask_words=1)
+    for args, kw in (((ints(3), ints(2)), {}), ((ints(2), ints(2).long()), {}), ((ints(2), ints(2)), {"parents": ints(5)}), ((ints(2), ints(2)), {"held_out": ints(1)}),
+                     ((ints(2), ints(2)), {"free_out": ints(2)}), ((ints(2), ints(2)), {"next_position": ints(6)}), ((ints(2).cpu(), ints(2)), {}), ((ints(2), None), {})):
+        with pytest.raises((TypeError, ValueError)):
+            fq.fq_paged_plan(r, *args, **kw)
+    with pytest.raises(ValueError):
+        fq.fq_paged_plan(b, ints(2), ints(2))  # not a reserved one
+    with pytest.raises(fq.FqError):
+        fq.fq_paged_plan(r, r.seq_len, ints(2))
+    x, scores = z(6, 50), z(2, 3, t=torch.float32)
+    outs = {"parent": ints(2, 4), "token": ints(2, 4), "scores_out": z(2, 4, t=torch.float32), "workspace": z(1 << 16, t=torch.uint8)}
+    for more in ({}, outs):
+        for args, kw in (((x[:5], scores, 4), {}), ((x.float(), scores, 4), {}), ((x, scores.half(), 4), {}), ((x, scores, 4), {"done": ints(2, 4), "eos": 1}),
+                         ((x, scores, 4), {"mask": z(2, 4, 1, t=torch.int64)}), ((x, scores, 4), {"tail": ints(3)}), ((x.t(), scores, 4), {}),
+                         ((x, scores, 4), {"mask_out": z(2, 3, 1, t=torch.int64)}), ((x, scores.cpu(), 4), {})):
+            with pytest.raises((TypeError, ValueError)):
+                fq.fq_beam_step(*args, **kw, **more)
+        for kw in ({"eos": 50}, {"done": ints(2, 3)}):
+            with pytest.raises(fq.FqError):
+                fq.fq_beam_step(x, scores, 4, **kw, **more)
+    with pytest.raises(fq.FqError):
+        fq.fq_beam_step(x, scores, 65)
+    torch.cuda.synchronize()
+    assert (out == 0).all()
