@@ -96,6 +96,11 @@ def accept(parents, drafted, following, most):
     return path, following[path[-1]]
 
 
+def given(path, accepted, tail):
+    """The nodes that a given path means: cut to the path's room and to the tail, a node below its place taken for that place, one behind the tail for its last."""
+    return [min(max(int(node), k), tail - 1) for k, node in enumerate(path[:max(min(accepted, len(path), tail), 0)])]
+
+
 def keep(pool, table, base, path, page):
     """Rows of a path moved together in one pool [pages, heads, page, 128]; positions without a page stay out."""
     rows = {}

@@ -275,8 +275,8 @@ __global__ __launch_bounds__(256) void plan_tokens_kernel(PlanArgs p)
 // ------------------------------------------------------------------ commit
 // A workgroup for one sequence, layer and two or eight heads.  Every wavefront finds the path itself (64 nodes a step, a ballot for the children: a barrier
 // would cost as much) and takes every fourth of the items, an item being a row of the path for one head of keys or values, sixteen lanes wide.  Thirty-two items
-// a turn, loads ahead of stores, rows in rising order for each head.  A path rises, so node path[k] is at least k: what a turn reads lies at or behind what it
-// writes, and no later turn reads what an earlier one wrote.  No other wavefront has its heads.  Bound by the chain of loads for one sequence
+// a turn, loads ahead of stores, rows in rising order for each head.  Node path[k] is at least k (a path that is found rises, of a given one each node is taken so):
+// what a turn reads lies at or behind what it writes, and no later turn reads what an earlier one wrote.  No other wavefront has its heads.  Bound by the chain of loads for one sequence
 // (lengths, nodes and pages, rows), by starting workgroups and the rows' way for many (29 sequences, 32 layers of 8 heads, 26 MB: a wavefront for each head of
 // keys and of values 15.6 us, so 10.8: 3.1 TB/s read and written).
 constexpr int COMMIT_ITEMS = 32; // of a turn
@@ -346,9 +346,9 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs p)
         }
         if (walk && writes && lane < count)
             path_out[k0 + lane] = mine;
-        // Rows that stay where they are need nothing; those are the first ones of the whole path, if any.
-        const int still = k0 + count - 1 == __builtin_amdgcn_readlane(mine, count - 1) ? count
-                                                                                     : __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < count && mine != k0 + lane));
+        // Rows ahead of the first one that moves need nothing.  Others behind it may be at their places too, the last one among them: a given path need not rise.
+        const unsigned long long moves = __builtin_amdgcn_ballot_w64(lane < count && mine != k0 + lane);
+        const int still = moves ? __builtin_ctzll(moves) : count;
         // Items: rows of the path in order, for each of the wavefront's pools (keys and values of a head are two) in turn.
         const int rows = count - still, items = rows * ((2 * heads - wave + 3) / 4);
         const uint32_t inverse = rows > 1 ? 0xffffffffu / (uint32_t)rows + 1 : 0; // 2^32 / rows rounded up: item / rows, both small

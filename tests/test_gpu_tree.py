@@ -404,6 +404,30 @@ def test_commit_of_given_paths(fq, torch, page, layers):
     assert np.array_equal(dk.cpu().numpy(), k) and np.array_equal(dv.cpu().numpy(), v)
 
 
+@pytest.mark.parametrize("page, layers", [(16, 2), (64, 1)])
+@pytest.mark.parametrize("path, tail, accepted", [
+    ([1, 2, -1], 5, 3), ([7, 9], 2, 2), ([4, 0, 2], 6, 3), ([-3, 2 ** 31 - 1, 1], 40, 99), ([0, 1, 9, -2 ** 31], 4, 4), ([0, 1, 2], 3, 3), ([2, 2, 2, 2], 4, 4),
+    ([5, 6, 7], 2, 3), ([6], 30, -1), (list(range(1, 64)) + [-1], 90, 64), (list(range(1, 130)) + [-1], 129, 130), (list(range(64)) + [70, 3, 3, 3], 80, 68)], ids=str)
+def test_commit_of_given_paths_that_do_not_rise(fq, torch, page, layers, path, tail, accepted):
+    """The nodes of such a path are taken as the header says, and their rows are moved: the last of 64 nodes may be at its place with others that are not."""
+    rng = np.random.default_rng(len(path) + tail)
+    ahead = [7, 30]  # positions ahead of the tails; the second sequence has the same path
+    lengths = [a + tail for a in ahead]
+    table, pages = deal(rng, lengths, page)
+    k, v = (rng.normal(size=(layers, pages, 3, page, 128)).astype(np.float16) for _ in range(2))
+    b = fq.PagedBatch([1, 1], lengths, table, page, pages)
+    dk, dv = dev(torch, k), dev(torch, v)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    got = fq.fq_tree_commit(b, dk, dv, tail=ints(tail, tail), path=dev(torch, np.array([path, path], dtype=np.int32)), accepted=ints(accepted, accepted))
+    nodes = ref.given(path, accepted, tail)
+    assert got[3].tolist() == [a + len(nodes) for a in ahead]
+    for i in range(2):
+        for l in range(layers):
+            ref.keep(k[l], table[i], ahead[i], nodes, page)
+            ref.keep(v[l], table[i], ahead[i], nodes, page)
+    assert np.array_equal(dk.cpu().numpy(), k) and np.array_equal(dv.cpu().numpy(), v)
+
+
 def test_commit_of_a_path_through_a_long_tail(fq, torch):
     """More pages than a wavefront has lanes behind the tail's first, and a path of more than two of its turns."""
     rng = np.random.default_rng(77)

@@ -165,6 +165,11 @@ def test_reference_tree():
     assert ref.accept([-1, 0, 0, 1, 2, 2], [9, 7, 7, 8, 8, 8], [7, 8, 8, 5, 6, 6], 2) == ([0, 1], 8)
 
 
+def test_reference_given_path():
+    assert ref.given([1, 2, -1], 3, 5) == [1, 2, 2] and ref.given([7, 9], 2, 2) == [1, 1] and ref.given([3, 4], 9, 6) == [3, 4]
+    assert ref.given([3, 4], -1, 6) == [] and ref.given([3, 4], 2, 1) == [0] and ref.given([], 2, 5) == [] and ref.given([4, 0, 2], 3, 6) == [4, 1, 2]
+
+
 def test_reference_plan():
     table = np.array([[4, -1, -1], [0, 1, -1], [3, -1, -1]])
     # sequence 1 is closed and gives 0 and 1; sequence 0 grows by two pages, sequence 2 by none
