@@ -850,9 +850,8 @@ __global__ __launch_bounds__(256) void attn_tree_merge_kernel(PagedAttnArgs p)
         }
         if (at < 0) // no more of them
             return;
-        const int token = at / groups, part = at - token * groups, m = s.first + token, head = SPREAD ? part : 8 * part + half;
-        if (head >= p.heads)
-            continue;
+        const int token = at / groups, part = at - token * groups, m = s.first + token, own = SPREAD ? part : 8 * part + half;
+        const int head = min(own, p.heads - 1); // behind the last one that one again, not written: every lane comes to the next turn's sums
         const int live = (s.len + p.chunk - 1) / p.chunk, mine = SPREAD ? max((live - half + 7) / 8, 0) : live; // splits of half a wavefront, every eighth
         const size_t item = (size_t)m * p.heads + head;
         const f2 *ml = reinterpret_cast<const f2 *>(p.part_ml) + item;
@@ -904,13 +903,13 @@ __global__ __launch_bounds__(256) void attn_tree_merge_kernel(PagedAttnArgs p)
                 acc += sums[i][d] * w;
             }
             __syncthreads(); // read ahead of the next turn's
-            if (half != 0)
-                continue;
         }
-        const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-        *reinterpret_cast<h4 *>(p.out + item * PD + 4 * d) = h4{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv), (_Float16)(acc[3] * inv)};
-        if (d == 0 && p.lse)
-            p.lse[item] = (mx + log2f(l)) * LN2;
+        if (SPREAD ? half == 0 : own < p.heads) {
+            const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+            *reinterpret_cast<h4 *>(p.out + item * PD + 4 * d) = h4{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv), (_Float16)(acc[3] * inv)};
+            if (d == 0 && p.lse)
+                p.lse[item] = (mx + log2f(l)) * LN2;
+        }
     }
 }
 

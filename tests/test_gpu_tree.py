@@ -143,6 +143,41 @@ def test_long_sequences_are_split(fq, torch, heads, kv, page, n, S):
     attend(fq, torch, rng, seqs, heads, kv, page, 2, ["tree", "tree"])
 
 
+@pytest.mark.parametrize("heads, kv, page, seqs, parts", [
+    (9, 1, 64, [(550, 1500), (3, 700), (40, 90)], 4), (28, 4, 16, [(300, 3000)], 3), (13, 13, 16, [(16, 1100)] * 40, 3),
+    (5, 1, 64, [(210, 9000)], 18), (9, 1, 16, [(2, 40), (130, 9000)], 18)], ids=["one_head_left", "four_heads_left", "many_sequences", "spread", "spread_nine_heads"])
+def test_more_rows_to_join_than_workgroups(fq, torch, heads, kv, page, seqs, parts):
+    """The join has 1024 workgroups, which take eight heads of a token or one in turn: here some have two, the last heads fewer than eight.  Compared are the
+    tokens of the second turn and some of the first."""
+    rng = np.random.default_rng(heads + page)
+    lengths = [S for _, S in seqs]
+    table, pages = deal(rng, lengths, page)
+    k, v = pools(rng, pages, kv, page, table, lengths)
+    b = fq.PagedBatch([n for n, _ in seqs], lengths, table, page, pages)
+    items, bytes_ = b.tokens * heads, fq.fq_attn_tree_workspace_bytes(b, heads, kv)
+    assert abs(bytes_ - parts * items * 130 * 4) <= 256  # splits of 130 floats a row
+    jobs = [n * (heads if parts > 8 * -(-items // 1024) else -(-heads // 8)) for n, S in seqs if S > -(-max(lengths) // parts)]
+    assert 1024 < sum(jobs) <= 2048
+    q = rng.normal(size=(b.tokens, heads * 128)).astype(np.float16)
+    masks = [m for n, _ in seqs for m in ref.tree_masks(random_tree(rng, n))[0]]
+    words = -(-b.max_q // 64)
+    lse = torch.full((b.tokens, heads), 7.0, device="cuda")
+    out = torch.full((b.tokens, heads * 128), 9.0, dtype=torch.float16, device="cuda")
+    args = (dev(torch, q), b, dev(torch, ref.words_of(masks, words)), dev(torch, k), dev(torch, v))
+    fq.fq_attn_tree(*args, out=out, lse=lse)
+    second = b.tokens - -(-(sum(jobs) - 1024) * b.tokens // sum(jobs))  # the first token of the second turn, or one near
+    at = 0
+    for i, (n, S) in enumerate(seqs):
+        late = [at + j for j in range(n) if at + j >= second]
+        late = late[::max(len(late) // 12, 1)]
+        pick = sorted(set(late) | {at + int(j) for j in rng.choice(n, size=min(n, 6 if len(seqs) < 10 else 1), replace=False)})
+        check(out.cpu().numpy()[pick], lse.cpu().numpy()[pick], [(len(pick), n, S)], [masks[j] for j in pick], words, table[i:i + 1], k, v, q[pick], heads, kv,
+              128 ** -0.5)
+        at += n
+    assert torch.isfinite(out).all() and not (out == 9.0).all(1).any()
+    assert torch.equal(fq.fq_attn_tree(*args).view(torch.int16), out.view(torch.int16))
+
+
 @pytest.mark.parametrize("heads, kv, page, most", [(8, 2, 16, 900), (4, 4, 64, 300), (8, 1, 32, 2500)])
 def test_many_sequences(fq, torch, heads, kv, page, most):
     # more sequences than a wavefront has lanes, some without tokens, their lengths from none to many splits
