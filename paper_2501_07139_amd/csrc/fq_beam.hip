@@ -7,7 +7,8 @@
 //
 // Two launches.  A workgroup of the first has a part of a row in registers, read once: its maximum, its sum of exponentials, and its `width` best logits
 // in order.  They are found without sorting: the width-th of the threads' largest is a bound that at least `width` values reach, in at most
-// `width` threads, so few are left, and each of them counts those ahead of it.  A workgroup of the second has a request: lse of its beams from the
+// `width` threads if no two of those are equal and in at most BEAM_MOST if some are (the list is sized for that), so few are left, and each of them
+// counts those ahead of it.  A workgroup of the second has a request: lse of its beams from the
 // parts, and the best of the parts' lists by the same count over their heads.  Many rows are bound by the exponentials, 21 instructions a value with all
 // that goes with them, behind a first wait of all workgroups for memory (732 rows of 32000, 23.4 million values: 24 us, 2.0 TB/s, and 7 for the second
 // launch); few by two launches and their barriers (4 rows 5.6 and 5.4).  Workgroups that take several parts, the loads of the next ahead of the work on one,
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 8) void beam_rows_kernel(BeamArgs p)
         wave_sum[wave] = sum;
     __syncthreads();
     const uint32_t least = bound;
-    if (top >= least) { // at most 64 threads: all of theirs fit the list
+    if (top >= least) { // at most BEAM_MOST threads: all of theirs fit the list
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
             if (order[c] >= least) {
