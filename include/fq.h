@@ -522,7 +522,8 @@ int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void 
  * Several continuations of a sequence at once (drafted trees whose tokens the model checks in one pass, and beams).  The last `tail` positions
  * of a sequence are nodes: each has a mask of the nodes that it sees, its own bit among them where it sees itself, in words of 64 bits (bit j of
  * word w is node 64 w + j, counted from the tail's first position).  Positions ahead of the tail are seen by all.  Masks have 1 to
- * FQ_TREE_WORDS words a row.
+ * FQ_TREE_WORDS words a row, so that a tail has 4096 nodes at most that can be told apart.  A beam that has lost stays in the tail until a path is kept: 16 beams
+ * have 256 steps, 64 beams 64.
  */
 #define FQ_TREE_WORDS 64
 
@@ -539,7 +540,9 @@ int fq_cache_evict(const fq_paged_batch *batch, const void *k_pages, const void 
  * (NULL: cached[b]) + i.  With parents (int32 [tokens]: of each token the one that it goes on from, counted within its sequence; what is not
  * a token ahead of it, -1 for instance, makes it a root) positions = next_position[b] + its depth, and mask (or NULL), uint64
  * [tokens][mask_words], has its own bit and those of its ancestors; max_q at most 64 mask_words then, and 64 FQ_TREE_WORDS without a mask.  Rows of
- * positions, slots and mask behind the last token: 0, -1, 0.
+ * positions, slots and mask behind the last token: 0, -1, 0.  With parents one workgroup has a sequence's tokens and walks up from each for every word of its mask:
+ * trees of 63 nodes take 4 us, but a chain of 256 with 4 words 47 us, of 1024 with 16 words 2.1 ms, of 4096 with 64 words 135 ms (a chunk of a prompt beside
+ * trees is a chain, too; its mask is plain enough for the caller to make).
  * batch: its sizes are the bounds (tokens below 2^28); its arrays q_start, seq_len and table (all columns; those behind what is held are written as pages are
  * taken) are the output.  free_pages int32 [pages], of which the first free_count[0] are free; free_out[0] of them are free afterwards.
  * lacking[0]: pages that the stack did not have; held_out counts those that a sequence has, and the table has -1 for the others.
@@ -583,7 +586,8 @@ int fq_tree_commit(const fq_paged_batch *batch, const int32_t *tail, const int32
  * logits fp16, row (request * beams + beam) at that many times ld elements; scores fp32 [requests][beams]: -inf (or NaN) for beams that are not there.
  * done int32 [requests][beams] or NULL: beams that have ended go on as they are, with token eos and their score.  A total that is NaN (a row with a NaN or
  * +inf, or of -inf only) or -inf (a token that is masked out) is never taken; where fewer than `width` are left, parent and token are -1, the
- * score -inf, done 1 and the mask 0.
+ * score -inf, done 1 and the mask 0.  Scores are below 2^28 in magnitude, or -inf: 64 bits hold no difference of logits beside larger ones, and which of a beam's
+ * tokens are taken is not defined there (-inf, not a large number, says that a beam is not there).
  * parent, token int32 [requests][width], scores_out fp32, done_out int32 (or NULL): done[parent], or token is eos (eos < 0: no token is).
  * mask_out (or NULL) uint64 [requests][width][mask_words] = mask [requests][beams][mask_words] (NULL: zeros) of the parent, and bit tail[request]
  * (NULL: 0) + place, the node that the beam's token will be: with it the beams are a tree for fq_attn_tree, and nothing of the cache moves.
