@@ -1,6 +1,6 @@
 // Beam search: the best continuations of the beams of a request over the vocabulary, and the masks of the beams that go on.
 //
-//   total[b][v] = score[b] + logit[b][v] - lse[b],  lse[b] = log sum_v exp(logit[b][v]),
+//   total[b][v] = score[b] + (logit[b][v] - lse[b]),  lse[b] = m[b] + log sum_v exp(logit[b][v] - m[b]) with the largest logit m[b],
 // the `width` largest of beams * vocab, of equal ones the lower b * vocab + v.  Which one comes ahead of another is decided by differences of
 // totals of several beams, so lse and totals are held in 64 bits: with 32, one step in about ten over 64 requests of 16 beams would have two
 // of them the wrong way round.  That costs little here: a multiply-add of 64 bits issues as fast as one of 32.
@@ -24,9 +24,9 @@ constexpr int BEAM_LISTS = BEAM_MOST * 32;        // of a request: parts of 8192
 constexpr int BEAM_NONE = -(1 << 20); // below the power of two of any logit
 
 struct BeamPart {
-    double sum; // of exp(logit) 2^-scale; NaN where a logit is NaN or +inf
-    int scale;  // BEAM_NONE where there is none above -inf
-    int count;  // of its list
+    double sum, unit; // of exp(logit) 2^-scale, NaN where a logit is NaN or +inf; the same of the largest logit alone
+    int scale;        // BEAM_NONE where there is none above -inf
+    unsigned short largest, count; // order of the largest logit; entries of its list
 };
 
 struct BeamArgs {
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 8) void beam_rows_kernel(BeamArgs p)
     __shared__ __align__(16) uint32_t tops[BEAM_THREADS];
     __shared__ uint32_t list[BEAM_MOST * CHUNKS * 8];
     __shared__ u2v table[EXP_TABLE];
-    __shared__ double wave_sum[4];
+    __shared__ double wave_sum[4], unit;
     __shared__ uint32_t bound;
     __shared__ int listed;
     const int row = blockIdx.x / p.parts, part = blockIdx.x - row * p.parts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 8) void beam_rows_kernel(BeamArgs p)
     const bool none = all >> 16 < ORDER_LEAST;
     if (none || all >> 16 >= ORDER_INF) { // nothing but -inf, or a NaN or +inf (uniform)
         if (tid == 0)
-            *out = BeamPart{none ? 0.0 : (double)NAN, none ? BEAM_NONE : 0, 0};
+            *out = BeamPart{none ? 0.0 : (double)NAN, 1.0, none ? BEAM_NONE : 0, 0, 0};
         return;
     }
     if (wave == 0) {
@@ -205,6 +205,8 @@ __global__ __launch_bounds__(BEAM_THREADS, 8) void beam_rows_kernel(BeamArgs p)
         sum += __shfl_xor(sum, o, 64);
     if (lane == 0)
         wave_sum[wave] = sum;
+    if (tid == BEAM_THREADS - 64)
+        unit = add_exp(0.0, (double)high, terms, table);
     __syncthreads();
     const uint32_t least = bound;
     if (top >= least) { // at most BEAM_MOST threads: all of theirs fit the list
@@ -230,13 +232,13 @@ __global__ __launch_bounds__(BEAM_THREADS, 8) void beam_rows_kernel(BeamArgs p)
             to[before] = list[i];
     }
     if (tid == 0)
-        *out = BeamPart{wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3], scale, min(count, p.width)};
+        *out = BeamPart{wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3], unit, scale, (unsigned short)(all >> 16), (unsigned short)min(count, p.width)};
 }
 
-// 64 bits in the order of their values; 0 is below all numbers.
+// 64 bits in the order of their values, both zeros alike; 0 is below all numbers.
 __device__ __forceinline__ uint64_t order_of(double x)
 {
-    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x + 0.0);
     return bits >> 63 ? ~bits : bits | 1ull << 63;
 }
 __device__ __forceinline__ double value_of(uint64_t order)
@@ -284,14 +286,15 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, ui
 {
     __shared__ uint64_t heads[BEAM_LISTS], keys[BEAM_MOST * BEAM_MOST], masks[BEAM_THREADS];
     __shared__ uint32_t index[BEAM_MOST * BEAM_MOST];
-    __shared__ double offset[BEAM_MOST]; // score - lse
+    __shared__ double lse[BEAM_MOST]; // NaN of beams that do not go on
     __shared__ float scores[BEAM_MOST];
     __shared__ int parent[BEAM_MOST], ended[BEAM_MOST], chosen[BEAM_MOST], ahead_of[2][BEAM_THREADS]; // heads; what is left of the entries
     __shared__ unsigned char counts[BEAM_LISTS];
     __shared__ uint64_t bound;
     __shared__ int listed, found;
-    double *const sums = reinterpret_cast<double *>(heads);  // of the parts, until the heads are known
+    double *const sums = reinterpret_cast<double *>(heads), *const units = reinterpret_cast<double *>(keys); // of the parts, until the heads are known
     int *const scales = reinterpret_cast<int *>(index);
+    uint32_t *const largest = index + BEAM_LISTS;
     const int r = blockIdx.x, tid = threadIdx.x;
     const int row0 = r * p.beams, lists = p.beams * p.parts, entries = lists * p.width, mask_entries = p.beams * p.a.mask_words;
     const BeamPart *const parts = p.parts_out + (size_t)row0 * p.parts;
@@ -307,7 +310,9 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, ui
     for (int i = tid; i < lists; i += BEAM_THREADS) { // of beams that nobody has looked at, anything
         const BeamPart part = parts[i];
         sums[i] = part.sum;
+        units[i] = part.unit;
         scales[i] = part.scale;
+        largest[i] = (uint32_t)part.largest << 16 | i;
         counts[i] = (unsigned char)part.count;
     }
     if (tid < p.beams) {
@@ -321,32 +326,36 @@ __global__ __launch_bounds__(BEAM_THREADS) void beam_merge_kernel(BeamArgs p, ui
     }
     __syncthreads();
     if (tid < p.beams) {
+        // In units of the largest logit's term, which is one of the sum's, a row of one token has a sum of 1 and goes on with its beam's score to the last
+        // bit: beams of equal scores whose tokens are forced tie, whatever the logits.  The largest logit has the largest scale, too.
         double at = NAN;
-        if (ended[tid]) {
-            at = scores[tid];
-        } else if (alive(scores[tid])) {
+        if (!ended[tid] && alive(scores[tid])) {
             double sum = 0.0;
-            int scale = BEAM_NONE;
-            for (int j = 0; j < p.parts; ++j)
-                scale = max(scale, scales[tid * p.parts + j]);
+            const int part0 = tid * p.parts;
+            uint32_t high = 0; // and the list that it is of
 #pragma unroll 4
             for (int j = 0; j < p.parts; ++j)
-                sum += ldexp(sums[tid * p.parts + j], scales[tid * p.parts + j] - scale);
-            at = sum > 0.0 ? (double)scores[tid] - ((double)scale * 0.69314718055994530942 + log(sum)) : (double)NAN;
+                high = max(high, largest[part0 + j]);
+            const int scale = scales[high & 0xffff];
+            const double unit = units[high & 0xffff];
+#pragma unroll 4
+            for (int j = 0; j < p.parts; ++j)
+                sum += ldexp(sums[part0 + j], scales[part0 + j] - scale);
+            at = sum > 0.0 ? (double)value_of(high >> 16) + log(sum / unit) : (double)NAN;
         }
-        offset[tid] = at;
+        lse[tid] = at;
     }
     __syncthreads();
     // The order of entry j of list l, 0 where it has none that counts, and its index; c: what the list has there.
     const auto entry = [&](int l, int j, uint32_t c, uint32_t *at) -> uint64_t {
         const int b = quotient(l, per_parts), part = l - b * p.parts;
-        const double off = offset[b];
+        const double score = scores[b], total = score + ((double)value_of(c >> 16) - lse[b]);
         if (ended[b]) {
             *at = (uint32_t)b * p.vocab + p.a.eos;
-            return part == 0 && j == 0 && off > -INFINITY ? order_of(off) : 0;
+            return part == 0 && j == 0 && score > -INFINITY ? order_of(score) : 0;
         }
         *at = (uint32_t)b * p.vocab + part * p.part_chunks * 8 + (0xffff - (c & 0xffff));
-        return off > -INFINITY && j < counts[l] ? order_of(off + (double)value_of(c >> 16)) : 0;
+        return j < counts[l] && total > -INFINITY ? order_of(total) : 0;
     };
     const bool all_held = entries <= PER * BEAM_THREADS;
     const int firsts = all_held ? max(min(64 / lists, p.width), 1) : 1, firsts_all = lists * firsts; // entries of a list that the bound is taken from

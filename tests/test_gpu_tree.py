@@ -591,6 +591,23 @@ def test_equal_totals_go_by_index(fq, torch, vocab, width):
     beam_check(fq, torch, rng, steps, zero, width, rows=wider[:, 5:5 + vocab])
 
 
+@pytest.mark.parametrize("requests, beams, vocab, width", [(40, 5, 1, 5), (9, 16, 777, 20), (3, 64, 9000, 64), (1, 4, 32000, 4), (150, 8, 20000, 8), (2, 2, 262144, 3)])
+def test_beams_whose_tokens_are_forced_keep_their_scores(fq, torch, requests, beams, vocab, width):
+    """A row of one token has a log probability of 0, so its beam's total is its score to the last bit, whatever the logit: equal scores tie, and go by index, also with
+    those of beams that have ended."""
+    rng = np.random.default_rng(vocab + beams)
+    logits = np.full((requests * beams, vocab), -np.inf, dtype=np.float16)
+    value = rng.normal(size=requests * beams) * rng.choice([1e-4, 1.0, 30.0, 20000.0], size=requests * beams)
+    logits[np.arange(requests * beams), rng.integers(0, vocab, requests * beams)] = np.clip(value, -65504, 65504)
+    scores = rng.choice(np.array([0.0, -0.0, -1e-12, -0.1, -0.1, -3.7, -250.3], dtype=np.float32), size=(requests, beams))
+    got = beam_check(fq, torch, rng, logits, scores, width)
+    done = (rng.random((requests, beams)) < 0.4).astype(np.int32)
+    ended = beam_check(fq, torch, rng, logits, scores, width, done=done, eos=vocab // 2, words=1)
+    for parent, out in ((g[0].cpu().numpy(), g[2].cpu().numpy()) for g in (got, ended)):
+        kept = np.take_along_axis(scores, np.maximum(parent, 0).astype(np.int64), 1)
+        assert np.array_equal(out[parent >= 0], kept[parent >= 0]) and np.isneginf(out[parent < 0]).all()
+
+
 def test_beams_that_are_not_there_and_logits_that_are_not_finite(fq, torch):
     rng = np.random.default_rng(2)
     requests, beams, vocab = 6, 5, 3000
