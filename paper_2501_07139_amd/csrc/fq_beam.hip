@@ -10,8 +10,8 @@
 // `width` threads if no two of those are equal and in at most BEAM_MOST if some are (the list is sized for that), so few are left, and each of them
 // counts those ahead of it.  A workgroup of the second has a request: lse of its beams from the
 // parts, and the best of the parts' lists by the same count over their heads.  Many rows are bound by the exponentials, 25 vector
-// instructions a value with all that goes with them, behind a first wait of all workgroups for memory (732 rows of 32000, a twelfth of them ended: 24 us, 13.8 of them the issue of 8.45
-// million vector instructions, and 7 for the second launch); few by two launches and their barriers (4 rows 5.6 and 5.4).  Workgroups that take several parts, the loads of the next ahead of the work on one,
+// instructions a value with all that goes with them, behind a first wait of all workgroups for memory (732 rows of 32000, a twelfth of them ended: 24 us, 13.9 of them the issue of 8.52
+// million vector instructions, and 7 for the second launch); few by two launches and their barriers (4 rows 5.7 and 5.6).  Workgroups that take several parts, the loads of the next ahead of the work on one,
 // were slower (33): fewer of them fit a CU, and each waits for its own barriers.
 #include "fq_device.h"
 #include "fq_internal.h"
